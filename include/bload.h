@@ -66,7 +66,8 @@ typedef enum {
     BLOAD_EHIP = 6         /* a HIP runtime call failed (bload_last_hip_error() says which) */
 } bload_status;
 
-typedef enum { BLOAD_U8 = 0, BLOAD_F16 = 1, BLOAD_F32 = 2, BLOAD_I32 = 3 } bload_dtype;
+typedef enum { BLOAD_U8 = 0, BLOAD_F16 = 1, BLOAD_F32 = 2, BLOAD_I32 = 3,
+               BLOAD_BF16 = 4 /* bload_segment_attention*, bload_gated_scan*, bload_rotary */ } bload_dtype;
 typedef enum { BLOAD_SUM = 0, BLOAD_MEAN = 1 } bload_op;
 
 /* Human-readable name of a status (static storage, never NULL). */
@@ -374,7 +375,157 @@ bload_status bload_segment_scan(const void* d_packed, const uint8_t* d_reset,
                                 int64_t feat_dim, bload_dtype dtype, float decay, float* d_out,
                                 void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
-/* ------------------------------------------------------- strategy counts --
+/* ------------------------------------------------------ segment attention --
+ * Attention between the frames of one sequence, on the packed blocks: the start table
+ * keeps a sequence's frames from seeing its neighbours in the block, as it keeps a
+ * recurrent consumer's state from crossing a start.
+ *
+ * Tensors of queries, keys and values are [num_blocks, t_blk, heads, head_dim] with the
+ * elements of a head side by side; the other distances are free (in elements, 0 or
+ * negative ones included), so that q, k and v may be parts of one projection's result. */
+typedef struct {
+    void* d_data;                 /* element (0, 0, 0, 0), aligned to its type */
+    int64_t block_stride, slot_stride, head_stride;
+} bload_heads;
+
+#define BLOAD_ATTENTION_MAX_HEAD_DIM 128
+
+/* Who sees whom, once per batch and for every layer and pass: a slot's query sees the keys
+ * of its own sequence, which lies in the consecutive slots [f, e) of one block (found from
+ * d_reset / d_valid as bload_segment_reduce finds it).
+ *   causal = 0   all of [f, e)
+ *   causal = 1   [f, t + 1); with d_prefix also the first d_prefix[seq_id] frames of the
+ *                sequence, wherever the query stands (negative counts as 0, more than the
+ *                sequence has as all; a slot whose seq_id is outside [0, n_seq) has none)
+ * d_mask     out  int32[num_blocks, t_blk, 4], 16-byte aligned: key_lo, key_hi (the slots
+ *                 of the block that slot t's query sees), query_lo, query_hi (those whose
+ *                 queries see slot t's key); all 0 on padding
+ * d_prefix   in   int32[n_seq] or NULL;  d_seq_id is read only with it
+ * Asynchronous on `hip_stream`. */
+bload_status bload_segment_mask(const uint8_t* d_reset, const uint8_t* d_valid, const int32_t* d_seq_id,
+                                int64_t num_blocks, int32_t t_blk, int32_t causal, const int32_t* d_prefix,
+                                int64_t n_seq, int32_t* d_mask, void* hip_stream);
+
+/* For query i and key j of a head (keys and values are shared by heads_q / heads_kv
+ * consecutive heads of queries):
+ *     s = scale q_i.k_j;   with cap > 0: s = cap tanh(s / cap);   s = s - slope |i - j|
+ *     out_i = sum_j softmax_j(s) v_j over the keys that the mask lets i see
+ * A row that sees nothing (padding) is 0 and its lse -infinity.  What is not seen has no
+ * part in a result, infinite or NaN as it may be.
+ *
+ * dtype      F16, BF16 or F32 (of q, k, v and out); head_dim 1 .. BLOAD_ATTENTION_MAX_HEAD_DIM
+ * scale      > 0;  cap >= 0 (0: none);  d_slopes  in  float32[heads_q] or NULL
+ * d_mask     from bload_segment_mask.  Any other intervals do as well; they are cut to
+ *            [0, t_blk), and the backward pass needs the two of each slot to agree.
+ * d_lse      out  float32[num_blocks, heads_q, t_blk] or NULL: ln sum e^s, for the
+ *                 backward pass
+ * out_rest   out  like out, or NULL: what rounding to the type took from out (16-bit types;
+ *                 0 for F32), from which the backward pass forms do.out more exactly
+ * Products are those of the type with sums in 32 bits; probabilities are rounded to the
+ * type before they meet v.  Asynchronous on `hip_stream`, no workspace; same inputs give
+ * bit-identical outputs. */
+bload_status bload_segment_attention(const bload_heads* q, const bload_heads* k, const bload_heads* v, const int32_t* d_mask,
+                                     int64_t num_blocks, int32_t t_blk, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                     bload_dtype dtype, float scale, float cap, const float* d_slopes, const bload_heads* out,
+                                     float* d_lse, const bload_heads* out_rest, void* hip_stream);
+
+/* Gradients of sum(out * dout) by q, k and v (dk and dv summed over the heads that share
+ * them; no gradient of scale, cap and slopes).  out, d_lse and, where it was written,
+ * out_rest are those of the forward call with the same arguments; the outputs must not
+ * overlap any input.  d_workspace: >= bload_segment_attention_backward_workspace_bytes()
+ * bytes, 16-byte aligned.  Asynchronous on `hip_stream`; bit-identical like the forward pass. */
+size_t bload_segment_attention_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t heads_q);
+
+bload_status bload_segment_attention_backward(const bload_heads* dout, const bload_heads* q, const bload_heads* k,
+                                              const bload_heads* v, const bload_heads* out, const float* d_lse,
+                                              const bload_heads* out_rest, const int32_t* d_mask, int64_t num_blocks,
+                                              int32_t t_blk, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                              bload_dtype dtype, float scale, float cap, const float* d_slopes,
+                                              const bload_heads* dq, const bload_heads* dk, const bload_heads* dv,
+                                              void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The form for single tokens: one query for every sequence, which sees all of the sequence's
+ * frames; the packed blocks are the cache of keys and values.  The query stands at the
+ * sequence's last frame (for slopes).
+ * q, out          [n_seq, heads_q, head_dim]: block_stride is the distance of two sequences,
+ *                 slot_stride is not used
+ * k, v            [num_blocks, t_blk, heads_kv, head_dim]
+ * d_block_of_seq, d_offset_of_seq, d_lengths  in  int32[n_seq]: sequence i lies in the slots
+ *                 [offset, offset + length) of its block.  A sequence without frames, or one
+ *                 that does not lie inside the blocks (block -1 of another worker's share), gives 0.
+ * d_workspace     >= bload_segment_attention_decode_workspace_bytes(...) bytes, 16-byte aligned
+ *                 (may be NULL when that is 0)
+ * The rest is bload_segment_attention's.  Asynchronous on `hip_stream`. */
+size_t bload_segment_attention_decode_workspace_bytes(int64_t n_seq, int32_t t_blk, int32_t heads_q, int32_t heads_kv,
+                                                      int32_t head_dim);
+
+bload_status bload_segment_attention_decode(const bload_heads* q, const bload_heads* k, const bload_heads* v,
+                                            const int32_t* d_block_of_seq, const int32_t* d_offset_of_seq, const int32_t* d_lengths,
+                                            int64_t n_seq, int64_t num_blocks, int32_t t_blk, int32_t heads_q, int32_t heads_kv,
+                                            int32_t head_dim, bload_dtype dtype, float scale, float cap, const float* d_slopes,
+                                            const bload_heads* out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ----------------------------------------------------------- gated scan --
+ * bload_segment_scan with a gate for every element in place of one decay, a state that may be
+ * handed in and out, and a backward pass.  Per feature, along the slots of a block:
+ *     h = gate * h_prev + x   where the slot goes on: it is valid, carries no start flag and the
+ *                             slot in front of it is valid; the first slot of a block goes on
+ *                             from d_state_in, where that is given and the slot carries no flag
+ *     h = x                   where it starts a sequence
+ *     h = 0                   on padding
+ * Blocks of one slot (t_blk = 1) with a state in and out are the form for single tokens.
+ *
+ * d_gate, d_x  in   [B, t_blk, feat_dim] of `dtype` (F16, BF16 or F32), aligned to an element
+ * d_reset, d_valid  in  uint8[B, t_blk]
+ * d_state_in   in   float32[B, feat_dim] or NULL (no state: the first slot starts a sequence)
+ * d_out        out  [B, t_blk, feat_dim] of `dtype`: h; every element is written
+ * d_state_out  out  float32[B, feat_dim] or NULL: h of the last slot, unrounded; may be
+ *                   d_state_in where t_blk <= 8
+ * d_workspace       device scratch of >= bload_gated_scan_workspace_bytes(...) bytes, 16-byte
+ *                   aligned (may be NULL when that is 0); one answer for both passes
+ * States are held in 32 bits.  What is cut off by a start or by padding has no part in a
+ * result, infinite or NaN as it may be.  The product of the gates of consecutive slots has
+ * to stay inside float32 (it does where no |gate| is above 1).
+ * Asynchronous on `hip_stream`; same inputs give bit-identical outputs. */
+size_t bload_gated_scan_workspace_bytes(int64_t num_blocks, int32_t t_blk, int64_t feat_dim, bload_dtype dtype);
+
+bload_status bload_gated_scan(const void* d_gate, const void* d_x, const uint8_t* d_reset, const uint8_t* d_valid,
+                              int64_t num_blocks, int32_t t_blk, int64_t feat_dim, bload_dtype dtype, const float* d_state_in,
+                              void* d_out, float* d_state_out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of sum(out * dout) + sum(state_out * dstate_out) by gate, x and state_in.
+ * d_out, d_state_in  in   of the forward pass;  d_dstate_out  in  float32[B, feat_dim] or NULL
+ * d_dgate, d_dx      out  [B, t_blk, feat_dim] of `dtype`, every element written, overlapping no input
+ * d_dstate_in        out  float32[B, feat_dim] or NULL (0 where the first slot does not go on) */
+bload_status bload_gated_scan_backward(const void* d_dout, const void* d_gate, const void* d_out, const uint8_t* d_reset,
+                                       const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk, int64_t feat_dim,
+                                       bload_dtype dtype, const float* d_state_in, const float* d_dstate_out, void* d_dgate,
+                                       void* d_dx, float* d_dstate_in, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* --------------------------------------------------------------- rotary --
+ * Rotary positions: the pairs of the first rot_dim elements of every head (elements i and
+ * i + rot_dim / 2, or 2 i and 2 i + 1) are turned by position * d_freq[i] radians and multiplied
+ * by `scale`; the elements behind are handed through.  inverse = 1 turns back: the gradient.
+ *
+ * x, out       [num_blocks, t_blk, heads, head_dim] of F16, BF16 or F32; out may be x
+ * d_positions  in   int32[num_blocks, t_blk]: frame_idx of bload_pack, or any others; negative
+ *                   ones are padding, whose elements become 0
+ * d_freq       in   float32[rot_dim / 2], radians per frame
+ * Angles are formed in 64 bits.  Asynchronous on `hip_stream`, no workspace. */
+typedef enum { BLOAD_ROTARY_HALF = 0, BLOAD_ROTARY_INTERLEAVED = 1 } bload_rotary_layout;
+
+bload_status bload_rotary(const bload_heads* x, const int32_t* d_positions, int64_t num_blocks, int32_t t_blk, int32_t heads,
+                          int32_t head_dim, bload_dtype dtype, const float* d_freq, int32_t rot_dim, bload_rotary_layout layout,
+                          float scale, int32_t inverse, const bload_heads* out, void* hip_stream);
+
+/* base^(-2 i / rot_dim) for the pairs i, stretched for contexts `factor` times as long as the
+ * model was trained on: with trained = 0 all are divided by factor; with trained > 0 (in frames)
+ * those of fewer than `slow` turns over that length are divided, those of more than `fast` kept,
+ * and the ones between mixed in proportion (slow < fast).  Host only. */
+bload_status bload_rotary_frequencies(int32_t rot_dim, double base, double factor, int64_t trained, double slow, double fast,
+                                      float* h_freq);
+
+/* -------------------------------------------------------- strategy counts --
  * Problem Statement and Table 1 (rows "padding amount" and "# frames deleted"):
  * what the strategies compared there cost on a given set of lengths, counted in
  * frames, without materialising anything.

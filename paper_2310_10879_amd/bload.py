@@ -92,6 +92,43 @@ _lib.bload_segment_reduce.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i64, ctyp
                                       ctypes.c_int, _i64, _vp, _vp, _sz, _vp]
 
 
+class Heads(ctypes.Structure):
+    """bload_heads"""
+    _fields_ = [("d_data", _vp), ("block_stride", _i64), ("slot_stride", _i64), ("head_stride", _i64)]
+
+
+_hp, _int, _f32 = ctypes.POINTER(Heads), ctypes.c_int, ctypes.c_float
+ATTENTION_MAX_HEAD_DIM = 128
+# element types of the operators from bload_segment_attention on, which go by the tensors' own
+TYPE_CODE = {torch.float16: 1, torch.float32: 2, torch.bfloat16: 4}
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+
+_lib.bload_segment_mask.restype = _int
+_lib.bload_segment_mask.argtypes = [_vp, _vp, _vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp]
+_lib.bload_segment_attention.restype = _int
+_lib.bload_segment_attention.argtypes = [_hp, _hp, _hp, _vp, _i64, _i32, _i32, _i32, _i32, _int, _f32, _f32, _vp, _hp, _vp, _hp, _vp]
+_lib.bload_segment_attention_backward_workspace_bytes.restype = _sz
+_lib.bload_segment_attention_backward_workspace_bytes.argtypes = [_i64, _i32, _i32]
+_lib.bload_segment_attention_backward.restype = _int
+_lib.bload_segment_attention_backward.argtypes = [_hp, _hp, _hp, _hp, _hp, _vp, _hp, _vp, _i64, _i32, _i32, _i32, _i32, _int, _f32,
+                                                  _f32, _vp, _hp, _hp, _hp, _vp, _sz, _vp]
+_lib.bload_segment_attention_decode_workspace_bytes.restype = _sz
+_lib.bload_segment_attention_decode_workspace_bytes.argtypes = [_i64, _i32, _i32, _i32, _i32]
+_lib.bload_segment_attention_decode.restype = _int
+_lib.bload_segment_attention_decode.argtypes = [_hp, _hp, _hp, _vp, _vp, _vp, _i64, _i64, _i32, _i32, _i32, _i32, _int, _f32, _f32,
+                                                _vp, _hp, _vp, _sz, _vp]
+_lib.bload_gated_scan_workspace_bytes.restype = _sz
+_lib.bload_gated_scan_workspace_bytes.argtypes = [_i64, _i32, _i64, _int]
+_lib.bload_gated_scan.restype = _int
+_lib.bload_gated_scan.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i64, _int, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.bload_gated_scan_backward.restype = _int
+_lib.bload_gated_scan_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.bload_rotary.restype = _int
+_lib.bload_rotary.argtypes = [_hp, _vp, _i64, _i32, _i32, _i32, _int, _vp, _i32, _int, _f32, _i32, _hp, _vp]
+_lib.bload_rotary_frequencies.restype = _int
+_lib.bload_rotary_frequencies.argtypes = [_i32, ctypes.c_double, ctypes.c_double, _i64, ctypes.c_double, ctypes.c_double, _vp]
+
+
 class BloadError(RuntimeError):
     def __init__(self, status: int):
         self.status = status
@@ -418,3 +455,217 @@ def bload_pack_tile_bytes(n_seq: int, num_blocks: int, t_blk: int, frame_bytes: 
     """4096 if ``bload_pack`` cuts the packed tensor into 4 KiB tiles for these sizes
     (pack_wide_kernel, pack_direct_kernel), 0 if into tiles of 1024 slots (pack_narrow_kernel, pack_narrow_direct_kernel)."""
     return int(_lib.bload_pack_tile_bytes(n_seq, num_blocks, t_blk, frame_bytes, int(src_aligned_16)))
+
+
+# ---- operators on packed blocks whose element type is the tensors' own -------------------------
+
+
+def _heads(t: torch.Tensor, shape, dtype, name: str) -> Heads:
+    """A tensor [B, T, heads, D] of any strides with the elements of a head side by side."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and shape[3] > 1:
+        raise ValueError(f"{name}: the elements of a head have to lie side by side")
+    return Heads(t.data_ptr(), sb, st, sh)
+
+
+def _sized(t: torch.Tensor | None, numel: int, dtype, name: str) -> int:
+    if t is not None and t.numel() != numel:
+        raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
+    return _ptr(t, dtype)
+
+
+def _type_code(t: torch.Tensor) -> int:
+    code = TYPE_CODE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"expected float16, bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+def bload_segment_mask(reset: torch.Tensor, valid: torch.Tensor, causal: bool = True, prefix: torch.Tensor | None = None,
+                       seq_id: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Who sees whom in attention inside the sequences of packed blocks: int32[B, T, 4], per slot the interval of
+    keys that its query sees and the interval of queries that see its key.  reset, valid: uint8[B, T].
+    causal: a query sees its own frame and those in front of it, and with prefix (int32[n_seq], needs seq_id:
+    int32[B, T]) the first prefix[i] frames of its sequence i.  Asynchronous on the current stream."""
+    B, T = valid.shape
+    if reset.shape != valid.shape or (seq_id is not None and seq_id.shape != valid.shape):
+        raise ValueError("reset, valid and seq_id differ in shape")
+    if out is None:
+        out = torch.empty((B, T, 4), dtype=torch.int32, device=valid.device)
+    n = 0 if prefix is None else prefix.shape[0]
+    _check(_lib.bload_segment_mask(_ptr(reset, torch.uint8), _ptr(valid, torch.uint8),
+                                   0 if prefix is None else _ptr(seq_id, torch.int32), B, T, int(causal), _ptr(prefix, torch.int32),
+                                   n, _sized(out, B * T * 4, torch.int32, "out"), _stream()))
+    return out
+
+
+@dataclass
+class Saved:
+    """What ``bload_segment_attention`` leaves for its backward pass."""
+    lse: torch.Tensor                 # float32[B, heads_q, T]
+    rest: torch.Tensor | None         # [B, T, heads_q, D]: what rounding took from the result (None for float32)
+
+
+def bload_segment_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, mask: torch.Tensor, scale: float | None = None,
+                            cap: float = 0.0, slopes: torch.Tensor | None = None, training: bool = False,
+                            out: torch.Tensor | None = None):
+    """Attention inside the sequences of packed blocks.  q: [B, T, heads_q, D], k and v: [B, T, heads_kv, D] of float16,
+    bfloat16 or float32, any strides with the elements of a head side by side; mask from ``bload_segment_mask``;
+    scale: 1 / sqrt(D) by default; cap > 0: scores are cap tanh(s / cap); slopes (float32[heads_q]): minus slope times the
+    distance in frames.  Returns the result [B, T, heads_q, D], and with ``training`` what
+    ``bload_segment_attention_backward`` needs beside it.  Asynchronous on the current stream."""
+    B, T, Hq, D = q.shape
+    Hkv, dtype = k.shape[2], q.dtype
+    code = _type_code(q)
+    shape = (B, T, Hkv, D)
+    hq, hk, hv = _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v")
+    if out is None:
+        out = torch.empty((B, T, Hq, D), dtype=dtype, device=q.device)
+    saved = hr = None
+    if training:
+        saved = Saved(torch.empty((B, Hq, T), dtype=torch.float32, device=q.device),
+                      None if dtype == torch.float32 else torch.empty((B, T, Hq, D), dtype=dtype, device=q.device))
+        hr = None if saved.rest is None else _heads(saved.rest, q.shape, dtype, "rest")
+    _check(_lib.bload_segment_attention(hq, hk, hv, _sized(mask, B * T * 4, torch.int32, "mask"), B, T, Hq, Hkv, D, code,
+                                        D ** -0.5 if scale is None else scale, cap, _sized(slopes, Hq, torch.float32, "slopes"),
+                                        _heads(out, q.shape, dtype, "out"), saved.lse.data_ptr() if training else 0, hr, _stream()))
+    return (out, saved) if training else out
+
+
+def bload_segment_attention_backward_workspace_bytes(num_blocks: int, t_blk: int, heads_q: int) -> int:
+    return int(_lib.bload_segment_attention_backward_workspace_bytes(num_blocks, t_blk, heads_q))
+
+
+def bload_segment_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                                     saved: Saved, mask: torch.Tensor, scale: float | None = None, cap: float = 0.0,
+                                     slopes: torch.Tensor | None = None, grads=None, workspace: torch.Tensor | None = None):
+    """Gradients (dq, dk, dv) of sum(out * dout); out and saved are the forward call's.  grads: three tensors to
+    write into (any strides).  Asynchronous on the current stream."""
+    B, T, Hq, D = q.shape
+    Hkv, dtype = k.shape[2], q.dtype
+    code = _type_code(q)
+    shape = (B, T, Hkv, D)
+    if grads is None:
+        grads = tuple(torch.empty((B, T, h, D), dtype=dtype, device=q.device) for h in (Hq, Hkv, Hkv))
+    dq, dk, dv = grads
+    if workspace is None:
+        workspace = torch.empty(max(16, bload_segment_attention_backward_workspace_bytes(B, T, Hq)), dtype=torch.uint8, device=q.device)
+    hr = None if saved.rest is None else _heads(saved.rest, q.shape, dtype, "rest")
+    _check(_lib.bload_segment_attention_backward(
+        _heads(dout, q.shape, dtype, "dout"), _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
+        _heads(out, q.shape, dtype, "out"), _sized(saved.lse, B * Hq * T, torch.float32, "lse"), hr,
+        _sized(mask, B * T * 4, torch.int32, "mask"), B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
+        _sized(slopes, Hq, torch.float32, "slopes"), _heads(dq, q.shape, dtype, "dq"), _heads(dk, shape, dtype, "dk"),
+        _heads(dv, shape, dtype, "dv"), _ptr(workspace), _room(workspace), _stream()))
+    return dq, dk, dv
+
+
+def bload_segment_attention_decode_workspace_bytes(n_seq: int, t_blk: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
+    return int(_lib.bload_segment_attention_decode_workspace_bytes(n_seq, t_blk, heads_q, heads_kv, head_dim))
+
+
+def bload_segment_attention_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, block_of_seq: torch.Tensor,
+                                   offset_of_seq: torch.Tensor, lengths: torch.Tensor, scale: float | None = None, cap: float = 0.0,
+                                   slopes: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                                   workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """One query per sequence, q: [n_seq, heads_q, D], over the packed blocks k, v: [B, T, heads_kv, D] as a cache: sequence i
+    lies in slots [offset_of_seq[i], + lengths[i]) of block block_of_seq[i] (int32[n_seq] each, a plan's tables), and the query
+    stands at its last frame.  Returns [n_seq, heads_q, D].  Asynchronous on the current stream."""
+    n, Hq, D = q.shape
+    B, T, Hkv, _ = k.shape
+    dtype = q.dtype
+    code = _type_code(q)
+    if out is None:
+        out = torch.empty((n, Hq, D), dtype=dtype, device=q.device)
+    if workspace is None:
+        need = bload_segment_attention_decode_workspace_bytes(n, T, Hq, Hkv, D)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    shape, flat = (B, T, Hkv, D), (n, 1, Hq, D)
+    _check(_lib.bload_segment_attention_decode(
+        _heads(q.unsqueeze(1), flat, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
+        _sized(block_of_seq, n, torch.int32, "block_of_seq"), _sized(offset_of_seq, n, torch.int32, "offset_of_seq"),
+        _sized(lengths, n, torch.int32, "lengths"), n, B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
+        _sized(slopes, Hq, torch.float32, "slopes"), _heads(out.unsqueeze(1), flat, dtype, "out"), _ptr(workspace), _room(workspace),
+        _stream()))
+    return out
+
+
+def bload_gated_scan_workspace_bytes(num_blocks: int, t_blk: int, feat_dim: int, dtype: torch.dtype) -> int:
+    return int(_lib.bload_gated_scan_workspace_bytes(num_blocks, t_blk, feat_dim, TYPE_CODE[dtype]))
+
+
+def _gated_workspace(workspace, B, T, D, code, device):
+    if workspace is None:
+        need = _lib.bload_gated_scan_workspace_bytes(B, T, D, code)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    return workspace
+
+
+def bload_gated_scan(gate: torch.Tensor, x: torch.Tensor, reset: torch.Tensor, valid: torch.Tensor, h0: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, state: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """h = gate * h_prev + x inside the sequences of packed blocks, x at their starts, 0 on padding.  gate, x: contiguous
+    [B, T, D] of float16, bfloat16 or float32; h0 (float32[B, D]): the state in front of the blocks.  Returns h and
+    the state behind the last slots (float32[B, D]).  Asynchronous on the current stream."""
+    B, T, D = x.shape
+    dtype, code, n = x.dtype, _type_code(x), x.numel()
+    if out is None:
+        out = torch.empty((B, T, D), dtype=dtype, device=x.device)
+    if state is None:
+        state = torch.empty((B, D), dtype=torch.float32, device=x.device)
+    workspace = _gated_workspace(workspace, B, T, D, code, x.device)
+    _check(_lib.bload_gated_scan(_sized(gate, n, dtype, "gate"), _ptr(x), _sized(reset, B * T, torch.uint8, "reset"),
+                                 _sized(valid, B * T, torch.uint8, "valid"), B, T, D, code, _sized(h0, B * D, torch.float32, "h0"),
+                                 _sized(out, n, dtype, "out"), _sized(state, B * D, torch.float32, "state"), _ptr(workspace),
+                                 _room(workspace), _stream()))
+    return out, state
+
+
+def bload_gated_scan_backward(dout: torch.Tensor, gate: torch.Tensor, out: torch.Tensor, reset: torch.Tensor, valid: torch.Tensor,
+                              h0: torch.Tensor | None = None, dstate: torch.Tensor | None = None, grads=None,
+                              workspace: torch.Tensor | None = None):
+    """Gradients (dgate, dx, dh0) of sum(out * dout) + sum(state * dstate); out is the forward call's result.
+    grads: three tensors to write into.  Asynchronous on the current stream."""
+    B, T, D = dout.shape
+    dtype, code, n = dout.dtype, _type_code(dout), dout.numel()
+    if grads is None:
+        grads = (torch.empty((B, T, D), dtype=dtype, device=dout.device), torch.empty((B, T, D), dtype=dtype, device=dout.device),
+                 torch.empty((B, D), dtype=torch.float32, device=dout.device))
+    dgate, dx, dh0 = grads
+    workspace = _gated_workspace(workspace, B, T, D, code, dout.device)
+    _check(_lib.bload_gated_scan_backward(_ptr(dout), _sized(gate, n, dtype, "gate"), _sized(out, n, dtype, "out"),
+                                          _sized(reset, B * T, torch.uint8, "reset"), _sized(valid, B * T, torch.uint8, "valid"),
+                                          B, T, D, code, _sized(h0, B * D, torch.float32, "h0"),
+                                          _sized(dstate, B * D, torch.float32, "dstate"), _sized(dgate, n, dtype, "dgate"),
+                                          _sized(dx, n, dtype, "dx"), _sized(dh0, B * D, torch.float32, "dh0"), _ptr(workspace),
+                                          _room(workspace), _stream()))
+    return dgate, dx, dh0
+
+
+def bload_rotary_frequencies(rot_dim: int, base: float = 10000.0, factor: float = 1.0, trained: int = 0, slow: float = 1.0,
+                             fast: float = 32.0) -> torch.Tensor:
+    """float32[rot_dim / 2] on the host: base^(-2 i / rot_dim), stretched for contexts ``factor`` times as long as the
+    ``trained`` frames (0: all alike; else only the frequencies of few turns over that length)."""
+    out = torch.empty(max(0, rot_dim // 2), dtype=torch.float32)
+    _check(_lib.bload_rotary_frequencies(rot_dim, base, factor, trained, slow, fast, out.data_ptr()))
+    return out
+
+
+def bload_rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Tensor, layout: str = "half", scale: float = 1.0,
+                 inverse: bool = False, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The first 2 * len(frequencies) elements of every head of x [B, T, heads, D] turned by positions * frequencies
+    (int32[B, T], negative: padding, zeros; float32 radians per frame); inverse: turned back, the gradient.  out may
+    be x.  Asynchronous on the current stream."""
+    B, T, H, D = x.shape
+    code = _type_code(x)
+    if out is None:
+        out = torch.empty((B, T, H, D), dtype=x.dtype, device=x.device)
+    _check(_lib.bload_rotary(_heads(x, x.shape, x.dtype, "x"), _sized(positions, B * T, torch.int32, "positions"), B, T, H, D, code,
+                             _ptr(frequencies, torch.float32), 2 * frequencies.shape[0], ROTARY_LAYOUTS[layout], scale, int(inverse),
+                             _heads(out, x.shape, x.dtype, "out"), _stream()))
+    return out

@@ -1,0 +1,235 @@
+// bload_segment_attention: attention inside the sequences of packed blocks, forward.
+//
+// For query i of head h, over the keys j of the interval that the mask gives it:
+//     s_j = cap tanh(scale q.k_j / cap) - slope_h |i - j|,  p = softmax(s),  out = sum p_j v_j,
+//     lse = ln sum e^s_j
+// in one pass over the keys with a running maximum m and sum l: a tile of keys with scores s takes
+// m' = max(m, s), O = O 2^(m - m') + 2^(s - m') V, l likewise; O / l in the end.
+#include "bload_attention.hpp"
+#include "bload_attention_host.hpp"
+
+namespace bload {
+namespace {
+
+constexpr int kKeys = 64;              // keys of a tile
+
+// One query again, key by key in plain 32-bit arithmetic.  The matrix product adds 0 * v for what the
+// mask hides, which is NaN where a hidden v is infinite or NaN; rows that come out not finite are
+// computed here, from visible keys alone.
+template <typename T>
+__device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
+{
+    const int D = a.D, kv = head / a.G;
+    const Score score(a, head);
+    float q[2], acc[2] = {0.0f, 0.0f}, m = -INFINITY, l = 0.0f;
+    load_row2(att_at<T>(a.q, b, i, head), D, q);
+    for (int j = span.lo; j < span.hi; ++j) {
+        float k[2], v[2];
+        load_row2(att_at<T>(a.k, b, j, kv), D, k);
+        load_row2(att_at<T>(a.v, b, j, kv), D, v);
+        const float s = score.of<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, nullptr);
+        const float up = fmaxf(m, s), base = up == -INFINITY ? 0.0f : up;
+        const float f = exp2_fast(m - base), p = exp2_fast(s - base);
+        m = up;
+        l = l * f + p;
+        acc[0] = acc[0] * f + p * v[0];
+        acc[1] = acc[1] * f + p * v[1];
+    }
+    const float inv = 1.0f / l, o0 = acc[0] * inv, o1 = acc[1] * inv;
+    store_row2(att_at<T>(a.out, b, i, head), D, o0, o1);
+    if (a.rest.p) store_row2(att_at<T>(a.rest, b, i, head), D, o0 - (float)(T)o0, o1 - (float)(T)o1);
+    if (a.lse && lane_id() == 0) a.lse[((int64_t)b * a.Hq + head) * a.T + i] = (m + log2f(l)) * kLn2;
+}
+
+// A workgroup takes 128 queries of one head, a wavefront 32 of them (they stay in its registers, as does O^T);
+// tiles of 64 keys and values go through LDS, two tiles deep, the next one on its way from memory
+// while the present one is multiplied.
+template <typename T, int DP, bool MOD>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttArgs a)
+{
+    using L = Tile<T, DP>;
+    constexpr int kSteps = DP / 16, kParts = DP / 32;
+    __shared__ T ks[2][kKeys * DP], vs[2][kKeys * DP];
+    __shared__ int hull[2][kThreads / kWave];
+    const int lane = lane_id(), wave = wave_id();
+
+    // heads that share keys side by side, the latest queries (causally the longest) first
+    const uint32_t item = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int g = (int)(item % a.G), tile = a.tiles - 1 - (int)((item / a.G) % a.tiles);
+    const int kv = (int)((item / a.G / a.tiles) % a.Hkv), b = (int)(item / a.G / a.tiles / a.Hkv);
+    const int head = kv * a.G + g, D = a.D, T_ = a.T;
+    const int row = tile * 128 + wave * 32 + (lane & 31);
+
+    Span span = {0, 0};
+    if (row < T_) {
+        const int4 r = a.mask[(int64_t)b * T_ + row];
+        span = clamp_span(r.x, r.y, T_);
+    }
+    SpanRange range;
+    range.of_wave(span);
+    if (lane == 0) {
+        hull[0][wave] = range.lo;
+        hull[1][wave] = range.hi;
+    }
+    __syncthreads();
+    const int lo = min(min(hull[0][0], hull[0][1]), min(hull[0][2], hull[0][3]));
+    const int hi = max(max(hull[1][0], hull[1][1]), max(hull[1][2], hull[1][3]));
+
+    frag8<T> q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = frag8<T>{};
+    if (row < T_) {
+        const T* p = att_at<T>(a.q, b, row, head);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = load_frag(p, 16 * s + 8 * (lane >> 5), D);
+    }
+    const Score score(a, head);
+    const float c = MOD ? 1.0f : a.scale * kLog2e;
+
+    f32x16 o[kParts];
+#pragma unroll
+    for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    const T* kp = att_at<T>(a.k, b, 0, kv);
+    const T* vp = att_at<T>(a.v, b, 0, kv);
+    Stage<T, DP, kKeys> next_k, next_v;
+    if (lo < hi) {
+        next_k.load(kp, a.k.st, lo, hi, D);
+        next_v.load(vp, a.v.st, lo, hi, D);
+    }
+    int buf = 0;
+    for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
+        next_k.store(ks[buf]);
+        next_v.store(vs[buf]);
+        __syncthreads();
+        if (k0 + kKeys < hi) {
+            next_k.load(kp, a.k.st, k0 + kKeys, hi, D);
+            next_v.load(vp, a.v.st, k0 + kKeys, hi, D);
+        }
+        if (!range.meets(k0, kKeys)) continue;
+        f32x16 x[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            x[t] = f32x16{};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) x[t] = mma(L::row_frag(ks[buf], 32 * t + (lane & 31), s), q[s], x[t]);
+        }
+        const int key0 = k0 + 4 * (lane >> 5);
+        if constexpr (MOD) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[t][i] = score.of<T>(x[t][i], row - (key0 + 32 * t + 8 * (i / 4) + i % 4), nullptr);
+        }
+        if (!range.full(k0, kKeys)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = key0 + 32 * t + 8 * (i / 4) + i % 4;
+                    x[t][i] = key >= span.lo && key < span.hi ? x[t][i] : -INFINITY;
+                }
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
+        top = fmaxf(top, other_half(top));
+        const float up = fmaxf(m, top * c), base = up == -INFINITY ? 0.0f : up;
+        const float f = exp2_fast(m - base);
+        m = up;
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[t][i] = exp2_fast(fmaf(x[t][i], c, -base));
+                sum += x[t][i];
+            }
+        l = l * f + sum;
+        if (__any(f != 1.0f)) {
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) o[d] *= f;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const frag8<T> p = pack8<T>(x[t >> 1], 8 * (t & 1));
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs[buf], 16 * t, 32 * d), p, o[d]);
+        }
+    }
+    l += other_half(l);
+    const float inv = span.hi > span.lo ? 1.0f / l : 0.0f;
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < kParts; ++d) {
+        o[d] *= inv;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bad |= not_finite(o[d][i]);
+        if (span.hi <= span.lo) o[d] = f32x16{};           // a row that sees nothing is 0, whatever lies around it
+    }
+    if (row < T_) {
+        T* p = att_at<T>(a.out, b, row, head);
+#pragma unroll
+        for (int d = 0; d < kParts; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 y = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                store4(p, 32 * d + 8 * i + 4 * (lane >> 5), D, y);
+            }
+        if (a.rest.p) {
+            T* p = att_at<T>(a.rest, b, row, head);
+#pragma unroll
+            for (int d = 0; d < kParts; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f32x4 y;
+                    for (int j = 0; j < 4; ++j) y[j] = o[d][4 * i + j] - (float)(T)o[d][4 * i + j];
+                    store4(p, 32 * d + 8 * i + 4 * (lane >> 5), D, y);
+                }
+        }
+        if (a.lse && lane < 32)
+            a.lse[((int64_t)b * a.Hq + head) * T_ + row] = span.hi > span.lo ? (m + log2f(l)) * kLn2 : -INFINITY;
+    }
+    uint64_t again = __ballot(bad && span.hi > span.lo);
+    again = (again | (again >> 32)) & 0xffffffffu;
+    while (again) {
+        const int r = __ffsll((unsigned long long)again) - 1;
+        again &= again - 1;
+        forward_row<T>(a, b, head, tile * 128 + wave * 32 + r, {__shfl(span.lo, r), __shfl(span.hi, r)});
+    }
+}
+
+template <typename T, int DP>
+void launch(const AttArgs& a, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((int64_t)a.B * a.Hq * a.tiles)), block(kThreads);
+    if (a.cap > 0.0f || a.slopes) attention_forward_kernel<T, DP, true><<<grid, block, 0, stream>>>(a);
+    else attention_forward_kernel<T, DP, false><<<grid, block, 0, stream>>>(a);
+}
+
+}  // namespace
+}  // namespace bload
+
+using namespace bload;
+
+extern "C" bload_status bload_segment_attention(const bload_heads* q, const bload_heads* k, const bload_heads* v, const int32_t* d_mask,
+                                                int64_t num_blocks, int32_t t_blk, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                                bload_dtype dtype, float scale, float cap, const float* d_slopes, const bload_heads* out,
+                                                float* d_lse, const bload_heads* out_rest, void* hip_stream)
+{
+    AttArgs a = {};
+    bload_status st = att_args(a, num_blocks, t_blk, heads_q, heads_kv, head_dim, dtype, scale, cap, d_slopes, d_mask, 128);
+    if (st != BLOAD_OK) return st;
+    if (num_blocks == 0) return BLOAD_OK;
+    if ((st = att_tensor(a.q, q, dtype)) || (st = att_tensor(a.k, k, dtype)) || (st = att_tensor(a.v, v, dtype)) ||
+        (st = att_tensor(a.out, out, dtype)))
+        return st;
+    if (out_rest && (st = att_tensor(a.rest, out_rest, dtype))) return st;
+    if (!aligned_to(d_lse, 4)) return BLOAD_EALIGN;
+    a.lse = d_lse;
+    att_dispatch(dtype, head_dim, [&](auto type, auto dim) { launch<typename decltype(type)::type, decltype(dim)::value>(a, (hipStream_t)hip_stream); });
+    return launch_status();
+}

@@ -1,0 +1,317 @@
+// What the attention kernels share: element types, tiles in LDS, fragments of the matrix
+// instructions, scores.
+//
+// Every product goes through v_mfma_f32_32x32x16: a wavefront multiplies A (32 rows x 16) with
+// B (16 x 32 columns); lane l holds 8 elements of A's row l % 32 and 8 of B's column l % 32, at the
+// places 8 (l / 32) + j of the 16; of the result it holds column l % 32 and rows
+// 8 (i / 4) + 4 (l / 32) + i % 4, i = 0..15.  The order of the 16 is free as long as A and B agree.
+//
+// The operand that stays (queries forward, keys in the gradient of the keys) is B, held in registers for the whole
+// kernel; what streams past it is A, read from LDS.  So a product of scores S^T = K Q^T leaves each lane
+// the scores of ONE query with half of the tile's keys: the softmax needs no exchange but with
+// lane ^ 32, and the probabilities are already the B fragments of O^T = V^T P^T, with the keys
+// {4 h + 0..3, 8 + 4 h + 0..3} of every 16 in lane half h.  V^T's A fragments in that order are two
+// transposing LDS reads (ds_read_b64_tr_b16) of the row-major tile.
+#pragma once
+
+#include <type_traits>
+
+#include "bload_common.hpp"
+
+namespace bload {
+
+typedef _Float16 att_half;
+typedef __bf16 att_bf16;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+template <typename T> using frag8 = T __attribute__((ext_vector_type(8)));
+template <typename T> using frag4 = T __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// [B, T, heads, D]: elements of a head side by side, any distance (in elements) between the rest.
+struct AttTensor {
+    const void* p;
+    int64_t sb, st, sh;
+};
+
+struct AttArgs {
+    AttTensor q, k, v, out, rest, dout, dq, dk, dv;
+    float *lse, *delta;              // [B, Hq, T]
+    const int4* mask;                // [B, T]: key_lo, key_hi, query_lo, query_hi
+    const float* slopes;             // [Hq] or null
+    float scale, cap;
+    int32_t B, T, Hq, Hkv, G, D, tiles;
+};
+
+template <typename T>
+__device__ __forceinline__ T* att_at(const AttTensor& t, int64_t b, int64_t slot, int64_t head)
+{
+    return reinterpret_cast<T*>(const_cast<void*>(t.p)) + b * t.sb + slot * t.st + head * t.sh;
+}
+
+__device__ __forceinline__ f32x16 mma(frag8<att_half> a, frag8<att_half> b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(frag8<att_bf16> a, frag8<att_bf16> b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(frag8<float> a, frag8<float> b, f32x16 c)
+{
+    // eight products of depth 2: lane half h supplies place h of the j-th
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// N elements from or to memory that is aligned to an element only (one access of the full width).
+template <typename T, int N>
+__device__ __forceinline__ void load_any(const T* p, T (&x)[N]) { __builtin_memcpy(&x, p, sizeof(x)); }
+
+// 16 bytes of a row of D elements from element d on; zeros beyond the row.
+template <typename T>
+__device__ __forceinline__ vec16 load_chunk(const T* row, int d, int D)
+{
+    constexpr int N = 16 / sizeof(T);
+    vec16 r = {0, 0, 0, 0};
+    if (d + N <= D) {
+        __builtin_memcpy(&r, row + d, 16);
+    } else if (d < D) {
+        T x[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = d + j < D ? row[d + j] : (T)0.0f;
+        __builtin_memcpy(&r, &x, 16);
+    }
+    return r;
+}
+
+// A B fragment straight from memory: elements d .. d + 7 of a row; zeros beyond the row.
+template <typename T>
+__device__ __forceinline__ frag8<T> load_frag(const T* row, int d, int D)
+{
+    frag8<T> f;
+    vec16 c[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) c[i] = load_chunk(row, d + i * (16 / (int)sizeof(T)), D);
+    __builtin_memcpy(&f, &c, sizeof(f));
+    return f;
+}
+
+// Four results side by side, d .. d + 3 of a row of D.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int d, int D, f32x4 x)
+{
+    T y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = (T)x[j];
+    if (d + 4 <= D) {
+        __builtin_memcpy(row + d, &y, sizeof(y));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (d + j < D) row[d + j] = y[j];
+    }
+}
+
+// Rows of DP elements in LDS, in chunks of 16 bytes.  A chunk's place in its row is XORed with a
+// number of the row, such that neither eight rows at one chunk (row_frag) nor four rows at four
+// chunks (col_frag) meet in one bank.
+template <typename T, int DP>
+struct Tile {
+    static constexpr int kElems = 16 / (int)sizeof(T);
+    static constexpr int kChunks = DP / kElems;
+
+    __device__ static __forceinline__ int swizzle(int row)
+    {
+        if constexpr (kChunks == 16) return ((row & 1) << 2) | ((row & 2) << 2) | ((row >> 1) & 1) | ((row >> 1) & 2);
+        else if constexpr (kChunks == 8) return ((row & 1) << 2) | ((row >> 1) & 3);
+        else if constexpr (kChunks == 24 || kChunks == 32) return row & 7;
+        else return (row >> 1) & 3;
+    }
+    __device__ static __forceinline__ int at(int row, int chunk)       // in elements
+    {
+        return (row * kChunks + (chunk ^ swizzle(row))) * kElems;
+    }
+    // elements 16 s + 8 (lane / 32) .. + 7 of row `row`
+    __device__ static __forceinline__ frag8<T> row_frag(const T* tile, int row, int s)
+    {
+        const int c = (2 * s + (lane_id() >> 5)) * (8 / kElems);
+        frag8<T> f;
+        vec16 x[8 / kElems];
+#pragma unroll
+        for (int i = 0; i < 8 / kElems; ++i) __builtin_memcpy(&x[i], tile + at(row, c + i), 16);
+        __builtin_memcpy(&f, &x, sizeof(f));
+        return f;
+    }
+    // element d0 + lane % 32 of the rows r0 + {4 h + 0..3, 8 + 4 h + 0..3}, h = lane / 32
+    __device__ static __forceinline__ frag8<T> col_frag(const T* tile, int r0, int d0)
+    {
+        const int lane = lane_id();
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes read four rows of 16 elements, 4 elements a lane, and get a column of four each
+            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+            const int r = r0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
+            const int d = d0 + (lane & 16) + 4 * (lane & 3);
+            s16x4 x[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + at(r + 8 * i, d / kElems) + d % kElems));
+            frag8<T> f;
+            __builtin_memcpy(&f, &x, sizeof(f));
+            return f;
+        } else {
+            const int r = r0 + 4 * (lane >> 5), d = d0 + (lane & 31);
+            frag8<T> f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int row = r + (j & 3) + 8 * (j >> 2);
+                f[j] = tile[at(row, d / kElems) + d % kElems];
+            }
+            return f;
+        }
+    }
+};
+
+// R rows on their way from memory to LDS through the registers of `THREADS` threads (a workgroup, or each of its
+// wavefronts for itself).
+template <typename T, int DP, int R, int THREADS = kThreads>
+struct Stage {
+    using L = Tile<T, DP>;
+    static constexpr int kAll = R * L::kChunks, kEach = (kAll + THREADS - 1) / THREADS;
+    vec16 x[kEach];
+
+    // rows row0 .. row0 + R - 1 of [.., D], st elements apart; rows from `limit` on are zeros
+    __device__ __forceinline__ void load(const T* base, int64_t st, int row0, int limit, int D)
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int n = (int)threadIdx.x % THREADS + i * THREADS, row = row0 + n / L::kChunks;
+            x[i] = vec16{0, 0, 0, 0};
+            if ((kAll % THREADS == 0 || n < kAll) && row < limit)
+                x[i] = load_chunk(base + row * st, (n % L::kChunks) * L::kElems, D);
+        }
+    }
+    __device__ __forceinline__ void store(T* tile) const
+    {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int n = (int)threadIdx.x % THREADS + i * THREADS;
+            if (kAll % THREADS == 0 || n < kAll) __builtin_memcpy(tile + L::at(n / L::kChunks, n % L::kChunks), &x[i], 16);
+        }
+    }
+};
+
+// Eight scores in 32 bits to a B fragment.  16-bit types: rounded to nearest, which is the one rounding between
+// the inputs and the output (half a step of the type on each probability; sums and states stay in 32 bits).
+template <typename T>
+__device__ __forceinline__ frag8<T> pack8(const f32x16& x, int from)
+{
+    f32x8 y;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = x[from + j];
+    return __builtin_convertvector(y, frag8<T>);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh: for 16-bit types 1 - 2 / (1 + e^2x), whose absolute error of some 1e-7 is far below what the
+// rounded inputs leave of a score; for float the library's.
+template <typename T>
+__device__ __forceinline__ float cap_tanh(float x)
+{
+    if constexpr (sizeof(T) == 2) return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + exp2_fast(2.0f * kLog2e * x));
+    else return tanhf(x);
+}
+
+// A raw product q.k as a score in units of ln 2: cap tanh(scale q.k / cap) - slope |i - j|.
+struct Score {
+    float scale, cap, inv_cap, slope;
+    __device__ __forceinline__ Score(const AttArgs& a, int head)
+        : scale(a.scale), cap(a.cap), inv_cap(a.cap > 0.0f ? a.scale / a.cap : 0.0f), slope(a.slopes ? a.slopes[head] : 0.0f) {}
+    // `keep` (may be null): the derivative of the capped score by the scaled one
+    template <typename T>
+    __device__ __forceinline__ float of(float qk, int distance, float* keep) const
+    {
+        float s = qk * scale;
+        if (cap > 0.0f) {
+            const float t = cap_tanh<T>(qk * inv_cap);
+            s = cap * t;
+            if (keep) *keep = 1.0f - t * t;
+        } else if (keep) {
+            *keep = 1.0f;
+        }
+        return (s - slope * fabsf((float)distance)) * kLog2e;
+    }
+};
+
+// of lane ^ 32
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+__device__ __forceinline__ float wave_sum(float x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
+    return x;
+}
+__device__ __forceinline__ int wave_min(int x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x = min(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x)
+{
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x = max(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// What one lane's row may look at, inside [0, T); an empty interval is [0, 0).
+struct Span {
+    int lo, hi;
+};
+__device__ __forceinline__ Span clamp_span(int lo, int hi, int T)
+{
+    Span s = {max(lo, 0), min(hi, T)};
+    if (s.lo >= s.hi) s = {0, 0};
+    return s;
+}
+
+// Intervals of all rows of a wavefront together: the hull, and the part that every row sees.
+struct SpanRange {
+    int lo, hi, in_lo, in_hi;
+    __device__ __forceinline__ void of_wave(Span s)
+    {
+        lo = wave_min(s.hi > s.lo ? s.lo : 0x7fffffff);
+        hi = wave_max(s.hi);
+        in_lo = wave_max(s.lo);
+        in_hi = wave_min(s.hi);
+    }
+    __device__ __forceinline__ bool meets(int k, int n) const { return k < hi && k + n > lo; }
+    __device__ __forceinline__ bool full(int k, int n) const { return k >= in_lo && k + n <= in_hi; }
+};
+
+// Row D elements of a tensor in a wavefront's lanes, lane l holding elements l and l + 64 (D <= 128).
+template <typename T>
+__device__ __forceinline__ void load_row2(const T* row, int D, float (&x)[2])
+{
+    const int l = lane_id();
+    x[0] = l < D ? (float)row[l] : 0.0f;
+    x[1] = l + 64 < D ? (float)row[l + 64] : 0.0f;
+}
+template <typename T>
+__device__ __forceinline__ void store_row2(T* row, int D, float x0, float x1)
+{
+    const int l = lane_id();
+    if (l < D) row[l] = (T)x0;
+    if (l + 64 < D) row[l + 64] = (T)x1;
+}
+
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
+
+}  // namespace bload

@@ -1,0 +1,276 @@
+// bload_segment_attention_decode: one query per sequence over the packed blocks as a cache.
+//
+// The formulas are those of bload_attention.hip with one query; its heads that share keys are the 32
+// columns of the matrix products (fewer heads leave columns idle: the products are a tenth of the time that
+// the keys and values take from memory, which bounds this kernel).  A sequence's keys are cut
+// into `splits` shares, a workgroup to each, and a share into tiles of 32 keys that the four wavefronts take
+// in turn, each through its own part of LDS and without a barrier.  Two parts of the keys
+// with (m1, l1, O1) and (m2, l2, O2) join to m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m), O likewise: in LDS
+// over the wavefronts, in a second launch over the shares.
+#include <algorithm>
+
+#include "bload_attention.hpp"
+#include "bload_attention_host.hpp"
+
+namespace bload {
+namespace {
+
+constexpr int kTileKeys = 32;
+
+struct DecodeArgs {
+    AttArgs a;
+    const int32_t *block, *offset, *length;
+    float* part;                     // [n_seq, Hq, splits, D + 2]: m, l and O of a share
+    int64_t n_seq, blocks;
+    int32_t splits, column_groups;
+};
+
+__device__ __forceinline__ int decode_length(const DecodeArgs& p, int64_t seq, int64_t& block, int& offset)
+{
+    block = p.block[seq];
+    offset = p.offset[seq];
+    const int n = p.length[seq];
+    return block >= 0 && block < p.blocks && offset >= 0 && n > 0 && n <= p.a.T - offset ? n : 0;
+}
+
+// One share of one sequence for up to 32 heads of queries.
+template <typename T, int DP, bool MOD>
+__global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p)
+{
+    using L = Tile<T, DP>;
+    constexpr int kSteps = DP / 16, kParts = DP / 32, kWaves = kThreads / kWave;
+    constexpr int kTile = kTileKeys * DP;
+    // tiles of keys and values, later the wavefronts' results
+    __shared__ __attribute__((aligned(16))) char raw[std::max<size_t>(2 * kWaves * kTile * sizeof(T), kWaves * 32 * DP * sizeof(float))];
+    __shared__ float tops[kWaves][32], sums[kWaves][32];
+    const AttArgs& a = p.a;
+    const int lane = lane_id(), wave = wave_id(), D = a.D;
+    T* ks = reinterpret_cast<T*>(raw) + wave * 2 * kTile;
+    T* vs = ks + kTile;
+
+    uint32_t item = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int cg = (int)(item % p.column_groups);
+    item /= p.column_groups;
+    const int split = (int)(item % p.splits);
+    item /= p.splits;
+    const int kv = (int)(item % a.Hkv);
+    const int64_t seq = item / a.Hkv;
+    int64_t b;
+    int off;
+    const int n = decode_length(p, seq, b, off);
+    const int share = ((n + p.splits - 1) / p.splits + kTileKeys - 1) & ~(kTileKeys - 1);
+    const int lo = min(split * share, n), hi = min(lo + share, n);
+
+    const int column = cg * 32 + (lane & 31), head = kv * a.G + min(column, a.G - 1);
+    frag8<T> q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = frag8<T>{};
+    if (column < a.G && n > 0) {
+        const T* pq = att_at<T>(a.q, seq, 0, head);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = load_frag(pq, 16 * s + 8 * (lane >> 5), D);
+    }
+    const Score score(a, head);
+    const float c = MOD ? 1.0f : a.scale * kLog2e;
+    f32x16 o[kParts];
+#pragma unroll
+    for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    const T* kp = n > 0 ? att_at<T>(a.k, b, off, kv) : nullptr;
+    const T* vp = n > 0 ? att_at<T>(a.v, b, off, kv) : nullptr;
+    Stage<T, DP, kTileKeys, kWave> next_k, next_v;
+    int k0 = lo + wave * kTileKeys;
+    if (k0 < hi) {
+        next_k.load(kp, a.k.st, k0, hi, D);
+        next_v.load(vp, a.v.st, k0, hi, D);
+    }
+    for (; k0 < hi; k0 += kWaves * kTileKeys) {
+        next_k.store(ks);
+        next_v.store(vs);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int k1 = k0 + kWaves * kTileKeys;
+        if (k1 < hi) {
+            next_k.load(kp, a.k.st, k1, hi, D);
+            next_v.load(vp, a.v.st, k1, hi, D);
+        }
+        f32x16 x = {};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks, lane & 31, s), q[s], x);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int key = k0 + 4 * (lane >> 5) + 8 * (i / 4) + i % 4;
+            if constexpr (MOD) x[i] = score.of<T>(x[i], n - 1 - key, nullptr);
+            x[i] = key < hi ? x[i] : -INFINITY;
+            top = fmaxf(top, x[i]);
+        }
+        top = fmaxf(top, other_half(top));
+        const float up = fmaxf(m, top * c), base = up == -INFINITY ? 0.0f : up;
+        const float f = exp2_fast(m - base);
+        m = up;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x[i] = exp2_fast(fmaf(x[i], c, -base));
+            sum += x[i];
+        }
+        l = l * f + sum;
+        if (__any(f != 1.0f)) {
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) o[d] *= f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const frag8<T> w = pack8<T>(x, 8 * u);
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs, 16 * u, 32 * d), w, o[d]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    l += other_half(l);
+
+    // the wavefronts' parts to one
+    __syncthreads();
+    float (*acc)[32][DP] = reinterpret_cast<float (*)[32][DP]>(raw);
+    if (column < a.G) {
+#pragma unroll
+        for (int d = 0; d < kParts; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 y = {o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                __builtin_memcpy(&acc[wave][lane & 31][32 * d + 8 * i + 4 * (lane >> 5)], &y, 16);
+            }
+    }
+    if (lane < 32) {
+        tops[wave][lane] = m;
+        sums[wave][lane] = l;
+    }
+    __syncthreads();
+    const int columns = min(a.G - cg * 32, 32);
+    for (int e = (int)threadIdx.x; e < columns * D; e += kThreads) {
+        const int col = e / D, d = e - col * D, h = kv * a.G + cg * 32 + col;
+        float up = tops[0][col];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) up = fmaxf(up, tops[w][col]);
+        const float base = up == -INFINITY ? 0.0f : up;
+        float y = 0.0f, z = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = exp2_fast(tops[w][col] - base);
+            y += f * acc[w][col][d];
+            z += f * sums[w][col];
+        }
+        if (p.splits == 1) {
+            att_at<T>(a.out, seq, 0, h)[d] = (T)(n > 0 ? y / z : 0.0f);
+        } else {
+            float* to = p.part + ((seq * a.Hq + h) * p.splits + split) * (D + 2);
+            to[2 + d] = y;
+            if (d == 0) {
+                to[0] = up;
+                to[1] = z;
+            }
+        }
+    }
+}
+
+// The shares of one sequence and head to one: a wavefront each.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(DecodeArgs p)
+{
+    const AttArgs& a = p.a;
+    const int64_t at = (int64_t)blockIdx.x * (kThreads / kWave) + wave_id();
+    if (at >= p.n_seq * a.Hq) return;
+    const int64_t seq = at / a.Hq;
+    const int head = (int)(at - seq * a.Hq), lane = lane_id(), D = a.D;
+    int64_t b;
+    int off;
+    const int n = decode_length(p, seq, b, off);
+    const float* part = p.part + at * p.splits * (D + 2);
+    float up = -INFINITY;
+    for (int s = lane; s < p.splits; s += kWave) up = fmaxf(up, part[(int64_t)s * (D + 2)]);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) up = fmaxf(up, __shfl_xor(up, d));
+    const float base = up == -INFINITY ? 0.0f : up;
+    float y[2] = {0.0f, 0.0f}, z = 0.0f;
+    for (int s = 0; s < p.splits; ++s) {
+        const float* q = part + (int64_t)s * (D + 2);
+        const float f = exp2_fast(q[0] - base);
+        z += f * q[1];
+        if (lane < D) y[0] += f * q[2 + lane];
+        if (lane + kWave < D) y[1] += f * q[2 + lane + kWave];
+    }
+    const float inv = n > 0 ? 1.0f / z : 0.0f;
+    if (n == 0) y[0] = y[1] = 0.0f;
+    store_row2(att_at<T>(a.out, seq, 0, head), D, y[0] * inv, y[1] * inv);
+}
+
+// Shares: as many as make eight workgroups for each CU, of at least 256 keys of the longest sequence that a block can hold.
+inline int decode_splits(int64_t n_seq, int32_t t_blk, int32_t heads_kv, int32_t groups)
+{
+    const int64_t alone = n_seq * heads_kv * groups;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2048, alone), ceil_div(t_blk, 256), 128}));
+}
+
+template <typename T, int DP>
+void launch(const DecodeArgs& p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(p.n_seq * p.a.Hkv * p.splits * p.column_groups)), block(kThreads);
+    if (p.a.cap > 0.0f || p.a.slopes) attention_decode_kernel<T, DP, true><<<grid, block, 0, stream>>>(p);
+    else attention_decode_kernel<T, DP, false><<<grid, block, 0, stream>>>(p);
+    if (p.splits > 1)
+        attention_join_kernel<T><<<dim3((unsigned)ceil_div(p.n_seq * p.a.Hq, kThreads / kWave)), block, 0, stream>>>(p);
+}
+
+}  // namespace
+}  // namespace bload
+
+using namespace bload;
+
+extern "C" size_t bload_segment_attention_decode_workspace_bytes(int64_t n_seq, int32_t t_blk, int32_t heads_q, int32_t heads_kv,
+                                                                 int32_t head_dim)
+{
+    if (n_seq <= 0 || n_seq > BLOAD_MAX_SEQ || t_blk < 1 || heads_q < 1 || heads_kv < 1 || heads_q % heads_kv || head_dim < 1 ||
+        head_dim > BLOAD_ATTENTION_MAX_HEAD_DIM)
+        return 0;
+    const int splits = decode_splits(n_seq, t_blk, heads_kv, (int)ceil_div(heads_q / heads_kv, 32));
+    return splits == 1 ? 0 : round_up((size_t)n_seq * heads_q * splits * (head_dim + 2) * sizeof(float), 16);
+}
+
+extern "C" bload_status bload_segment_attention_decode(const bload_heads* q, const bload_heads* k, const bload_heads* v,
+                                                       const int32_t* d_block_of_seq, const int32_t* d_offset_of_seq,
+                                                       const int32_t* d_lengths, int64_t n_seq, int64_t num_blocks, int32_t t_blk,
+                                                       int32_t heads_q, int32_t heads_kv, int32_t head_dim, bload_dtype dtype, float scale,
+                                                       float cap, const float* d_slopes, const bload_heads* out, void* d_workspace,
+                                                       size_t workspace_bytes, void* hip_stream)
+{
+    DecodeArgs p = {};
+    bload_status st = att_args(p.a, 0, t_blk, heads_q, heads_kv, head_dim, dtype, scale, cap, d_slopes, nullptr, t_blk);
+    if (st != BLOAD_OK) return st;
+    if (n_seq < 0 || num_blocks < 0) return BLOAD_EINVAL;
+    if (n_seq > BLOAD_MAX_SEQ || num_blocks >= ((int64_t)1 << 40) / t_blk) return BLOAD_EOVERFLOW;
+    if (n_seq == 0) return BLOAD_OK;
+    if ((st = att_tensor(p.a.q, q, dtype)) || (st = att_tensor(p.a.out, out, dtype))) return st;
+    if (num_blocks > 0 && ((st = att_tensor(p.a.k, k, dtype)) || (st = att_tensor(p.a.v, v, dtype)))) return st;
+    if (!d_block_of_seq || !d_offset_of_seq || !d_lengths) return BLOAD_EINVAL;
+    if (!aligned_to(d_block_of_seq, 4) || !aligned_to(d_offset_of_seq, 4) || !aligned_to(d_lengths, 4)) return BLOAD_EALIGN;
+    p.column_groups = (int32_t)ceil_div(p.a.G, 32);
+    p.splits = decode_splits(n_seq, t_blk, heads_kv, p.column_groups);
+    if (n_seq > (int64_t)0x7fffffff / heads_kv / p.splits / p.column_groups || n_seq > (int64_t)0x7fffffff / heads_q) return BLOAD_EOVERFLOW;
+    const size_t need = bload_segment_attention_decode_workspace_bytes(n_seq, t_blk, heads_q, heads_kv, head_dim);
+    if (need) {
+        if (!d_workspace) return BLOAD_EINVAL;
+        if (!aligned_to(d_workspace, 16)) return BLOAD_EALIGN;
+        if (workspace_bytes < need) return BLOAD_EWORKSPACE;
+    }
+    p.block = d_block_of_seq;
+    p.offset = d_offset_of_seq;
+    p.length = d_lengths;
+    p.part = static_cast<float*>(d_workspace);
+    p.n_seq = n_seq;
+    p.blocks = num_blocks;
+    att_dispatch(dtype, head_dim, [&](auto type, auto dim) { launch<typename decltype(type)::type, decltype(dim)::value>(p, (hipStream_t)hip_stream); });
+    return launch_status();
+}
