@@ -56,7 +56,7 @@ def build(verbose: bool = True) -> str:
         api, scan = os.path.join(CSRC, "bload_api.hip"), os.path.join(CSRC, "bload_scan.hip")
         jobs = [(scan, "nowait.o", ["-DBLOAD_SCAN_POLLS=0"])] + \
             [(src, os.path.basename(src) + ".o", OWN_FLAGS.get(os.path.basename(src), [])) for src in sources()] + [(YS_SRC, "yardsticks.o", [])]
-        jobs.sort(key=lambda job: -os.path.getsize(job[0]))          # the longest first
+        jobs.sort(key=lambda job: ("attention" not in job[0], -os.path.getsize(job[0])))          # the longest first
         with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
             objects = dict(zip((job[1] for job in jobs), pool.map(compile_one, jobs)))
         for lib, parts in ((LIB, [os.path.basename(src) + ".o" for src in sources()]), (YS_LIB, ["yardsticks.o"]),

@@ -44,7 +44,7 @@ __device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 // A workgroup takes 128 queries of one head, a wavefront 32 of them (they stay in its registers, as does O^T);
 // tiles of 64 keys and values go through LDS, two tiles deep, the next one on its way from memory
 // while the present one is multiplied.
-template <typename T, int DP, bool MOD>
+template <typename T, int DP, bool MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
@@ -55,8 +55,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
 
     // heads that share keys side by side, the latest queries (causally the longest) first
     const uint32_t item = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int g = (int)(item % a.G), tile = a.tiles - 1 - (int)((item / a.G) % a.tiles);
-    const int kv = (int)((item / a.G / a.tiles) % a.Hkv), b = (int)(item / a.G / a.tiles / a.Hkv);
+    const int g = (int)(item % a.G), kv = (int)((item / a.G) % a.Hkv);
+    const int tile = a.tiles - 1 - (int)((item / a.Hq) % a.tiles), b = (int)(item / a.Hq / a.tiles);
     const int head = kv * a.G + g, D = a.D, T_ = a.T;
     const int row = tile * 128 + wave * 32 + (lane & 31);
 
@@ -83,6 +83,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = load_frag(p, 16 * s + 8 * (lane >> 5), D);
     }
+    arrived(q);
     const Score score(a, head);
     const float c = MOD ? 1.0f : a.scale * kLog2e;
 
@@ -91,29 +92,33 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    const T* kp = att_at<T>(a.k, b, 0, kv);
-    const T* vp = att_at<T>(a.v, b, 0, kv);
-    Stage<T, DP, kKeys> next_k, next_v;
+    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
     if (lo < hi) {
-        next_k.load(kp, a.k.st, lo, hi, D);
-        next_v.load(vp, a.v.st, lo, hi, D);
+        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
+        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
+        next_k.load(lo, hi);
+        next_v.load(lo, hi);
     }
+    typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
+        if constexpr (sizeof(T) == 4) keep_sums(o);
         next_k.store(ks[buf]);
         next_v.store(vs[buf]);
         __syncthreads();
         if (k0 + kKeys < hi) {
-            next_k.load(kp, a.k.st, k0 + kKeys, hi, D);
-            next_v.load(vp, a.v.st, k0 + kKeys, hi, D);
+            next_k.load(k0 + kKeys, hi);
+            next_v.load(k0 + kKeys, hi);
         }
+        by_row.renew();
+        by_col.renew();
         if (!range.meets(k0, kKeys)) continue;
         f32x16 x[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             x[t] = f32x16{};
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) x[t] = mma(L::row_frag(ks[buf], 32 * t + (lane & 31), s), q[s], x[t]);
+            for (int s = 0; s < kSteps; ++s) x[t] = mma(L::row_frag(ks[buf], by_row, 32 * t, s), q[s], x[t]);
         }
         const int key0 = k0 + 4 * (lane >> 5);
         if constexpr (MOD) {
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         for (int t = 0; t < 4; ++t) {
             const frag8<T> p = pack8<T>(x[t >> 1], 8 * (t & 1));
 #pragma unroll
-            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs[buf], 16 * t, 32 * d), p, o[d]);
+            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs[buf], by_col, 16 * t, 32 * d), p, o[d]);
         }
     }
     l += other_half(l);
@@ -206,8 +211,7 @@ template <typename T, int DP>
 void launch(const AttArgs& a, hipStream_t stream)
 {
     const dim3 grid((unsigned)((int64_t)a.B * a.Hq * a.tiles)), block(kThreads);
-    if (a.cap > 0.0f || a.slopes) attention_forward_kernel<T, DP, true><<<grid, block, 0, stream>>>(a);
-    else attention_forward_kernel<T, DP, false><<<grid, block, 0, stream>>>(a);
+    att_variant<T>(a, [&](auto mod, auto odd) { attention_forward_kernel<T, DP, mod.value, odd.value><<<grid, block, 0, stream>>>(a); });
 }
 
 }  // namespace

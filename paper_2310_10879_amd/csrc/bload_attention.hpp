@@ -137,74 +137,164 @@ struct Tile {
     {
         return (row * kChunks + (chunk ^ swizzle(row))) * kElems;
     }
-    // elements 16 s + 8 (lane / 32) .. + 7 of row `row`
-    __device__ static __forceinline__ frag8<T> row_frag(const T* tile, int row, int s)
+    // Where a lane reads, in bytes: `off` and, XORed with what is the same for all lanes, `place`.  Both are the
+    // same for all tiles of a kernel; `renew` keeps the compiler from holding every XOR of theirs in a register.
+    struct Reader {
+        int off, place;
+        __device__ __forceinline__ void renew() { asm volatile("" : "+v"(off), "+v"(place)); }
+    };
+    __device__ static __forceinline__ Reader rows()
     {
-        const int c = (2 * s + (lane_id() >> 5)) * (8 / kElems);
+        const int row = lane_id() & 31, h = lane_id() >> 5;
+        return {row * kChunks * 16, ((h * (8 / kElems)) ^ swizzle(row)) * 16};
+    }
+    // elements 16 s + 8 (lane / 32) .. + 7 of row r0 + lane % 32; r0: a multiple of 32
+    __device__ static __forceinline__ frag8<T> row_frag(const T* tile, Reader r, int r0, int s)
+    {
         frag8<T> f;
         vec16 x[8 / kElems];
 #pragma unroll
-        for (int i = 0; i < 8 / kElems; ++i) __builtin_memcpy(&x[i], tile + at(row, c + i), 16);
+        for (int i = 0; i < 8 / kElems; ++i)
+            __builtin_memcpy(&x[i], reinterpret_cast<const char*>(tile) + r.off + (((s * (16 / kElems) + i) * 16) ^ r.place) + r0 * kChunks * 16, 16);
         __builtin_memcpy(&f, &x, sizeof(f));
         return f;
     }
-    // element d0 + lane % 32 of the rows r0 + {4 h + 0..3, 8 + 4 h + 0..3}, h = lane / 32
-    __device__ static __forceinline__ frag8<T> col_frag(const T* tile, int r0, int d0)
+    __device__ static __forceinline__ Reader columns()
     {
         const int lane = lane_id();
         if constexpr (sizeof(T) == 2) {
             // 16 lanes read four rows of 16 elements, 4 elements a lane, and get a column of four each
+            const int r = 4 * (lane >> 5) + ((lane & 15) >> 2);
+            return {r * kChunks * 16 + (lane & 1) * 8, ((((lane & 16) >> 3) | ((lane & 3) >> 1)) ^ swizzle(r)) * 16};
+        } else {
+            return {0, 0};
+        }
+    }
+    // element d0 + lane % 32 of the rows r0 + {4 h + 0..3, 8 + 4 h + 0..3}, h = lane / 32; r0: a multiple of 16, d0 of 32
+    __device__ static __forceinline__ frag8<T> col_frag(const T* tile, Reader r, int r0, int d0)
+    {
+        if constexpr (sizeof(T) == 2) {
             typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-            const int r = r0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
-            const int d = d0 + (lane & 16) + 4 * (lane & 3);
             s16x4 x[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + at(r + 8 * i, d / kElems) + d % kElems));
+                x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_ptr)(reinterpret_cast<const char*>(tile) + r.off + ((d0 / kElems * 16) ^ r.place) + (r0 + 8 * i) * kChunks * 16));
             frag8<T> f;
             __builtin_memcpy(&f, &x, sizeof(f));
             return f;
         } else {
-            const int r = r0 + 4 * (lane >> 5), d = d0 + (lane & 31);
+            const int lane = lane_id(), row = r0 + 4 * (lane >> 5), d = d0 + (lane & 31);
             frag8<T> f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = r + (j & 3) + 8 * (j >> 2);
-                f[j] = tile[at(row, d / kElems) + d % kElems];
-            }
+            for (int j = 0; j < 8; ++j) f[j] = tile[at(row + (j & 3) + 8 * (j >> 2), d / kElems) + d % kElems];
             return f;
         }
     }
 };
 
-// R rows on their way from memory to LDS through the registers of `THREADS` threads (a workgroup, or each of its
-// wavefronts for itself).
-template <typename T, int DP, int R, int THREADS = kThreads>
+// R rows of D elements on their way from memory to LDS through the registers of `THREADS` threads (a workgroup, or each
+// of its wavefronts for itself).  A thread keeps one place of a row and goes down the rows with it.  Nothing beyond a row
+// is read, and nothing depends on the alignment of rows: where D is no whole number of chunks (ODD), the 16 bytes that hold a
+// row's end are taken from D - 16 / sizeof(T) on and shifted down.
+template <typename T, int DP, int R, bool ODD, int THREADS = kThreads>
 struct Stage {
     using L = Tile<T, DP>;
-    static constexpr int kAll = R * L::kChunks, kEach = (kAll + THREADS - 1) / THREADS;
+    static constexpr int N = L::kElems, kWide = L::kChunks <= 4 ? 4 : L::kChunks <= 8 ? 8 : L::kChunks <= 16 ? 16 : 32;
+    static constexpr int kRows = THREADS / kWide, kEach = R > kRows ? R / kRows : 1;
     vec16 x[kEach];
+    int64_t st;                      // in elements: of two rows
+    const T* at;                     // this thread's place of the next rows
+    int row, place, from, D;
 
-    // rows row0 .. row0 + R - 1 of [.., D], st elements apart; rows from `limit` on are zeros
-    __device__ __forceinline__ void load(const T* base, int64_t st, int row0, int limit, int D)
+    __device__ __forceinline__ Stage(int64_t st_, int D_) : st(st_), D(D_)
     {
+        const int t = (int)threadIdx.x % THREADS;
+        row = min(t / kWide, R - 1);
+        place = t % kWide;
+        from = ODD && D < N ? 0 : min(place * N, D - N);
+    }
+    __device__ __forceinline__ void begin(const T* base, int row0) { at = base + (row0 + row) * st + from; }
+    __device__ __forceinline__ void skip(int rows) { at += rows * st; }
+    __device__ __forceinline__ vec16 get(const T* p) const
+    {
+        vec16 r;
+        if (!ODD || D >= N) {
+            __builtin_memcpy(&r, p, 16);
+        } else {                                           // a row is shorter than 16 bytes
+            T y[N];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int n = (int)threadIdx.x % THREADS + i * THREADS, row = row0 + n / L::kChunks;
-            x[i] = vec16{0, 0, 0, 0};
-            if ((kAll % THREADS == 0 || n < kAll) && row < limit)
-                x[i] = load_chunk(base + row * st, (n % L::kChunks) * L::kElems, D);
+            for (int j = 0; j < N; ++j) y[j] = p[min(j, D - 1)];
+            __builtin_memcpy(&r, &y, 16);
         }
+        return r;
+    }
+    // the R rows from row0 on, where begin() or the last load() left off; in the place of rows from `limit` on, the last one in
+    // front of it (what they give is masked)
+    __device__ __forceinline__ void load(int row0, int limit)
+    {
+        if (row0 + R <= limit) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) x[i] = get(at + i * kRows * st);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) x[i] = get(at + (i * kRows - max(row0 + row + i * kRows - (limit - 1), 0)) * st);
+        }
+        at += R * st;
+    }
+    __device__ __forceinline__ vec16 whole(vec16 v) const
+    {
+        const int d = place * N;
+        if (!ODD) return d < D ? v : vec16{0, 0, 0, 0};
+        const int over = D < N ? d : d - from;             // elements in front of this place
+        uint64_t y[2];
+        __builtin_memcpy(&y, &v, 16);
+        if (D < N) {                                       // (repeats of the last element behind the row)
+            const int bits = D * (int)sizeof(T) * 8;
+            y[1] = bits <= 64 ? 0 : y[1] & ((1ull << (bits - 64)) - 1);
+            y[0] = bits >= 64 ? y[0] : y[0] & ((1ull << bits) - 1);
+        }
+        const int bits = min(over * (int)sizeof(T) * 8, 127);
+        const uint64_t lo = bits >= 64 ? y[1] >> (bits & 63) : (y[0] >> bits) | (y[1] << 1 << (63 - (bits & 63)));
+        const uint64_t hi = bits >= 64 ? 0 : y[1] >> bits;
+        y[0] = d < D ? lo : 0;
+        y[1] = d < D ? hi : 0;
+        __builtin_memcpy(&v, &y, 16);
+        return v;
     }
     __device__ __forceinline__ void store(T* tile) const
     {
+        if (kWide != L::kChunks && place >= L::kChunks) return;
+        if (kRows > R && (int)threadIdx.x % THREADS / kWide >= R) return;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int n = (int)threadIdx.x % THREADS + i * THREADS;
-            if (kAll % THREADS == 0 || n < kAll) __builtin_memcpy(tile + L::at(n / L::kChunks, n % L::kChunks), &x[i], 16);
+            const vec16 y = D == DP ? x[i] : whole(x[i]);
+            __builtin_memcpy(tile + L::at(row + i * kRows, place), &y, 16);
         }
     }
 };
+
+// Sums over a loop of matrix products stay in accumulation registers: said at the top of every step, or the compiler keeps
+// them in others and copies them there and back around the products.  For kernels of one wave a SIMD, which
+// have accumulation registers apart from the 256 others.
+template <int N>
+__device__ __forceinline__ void keep_sums(f32x16 (&x)[N])
+{
+#pragma unroll
+    for (int d = 0; d < N; ++d) asm volatile("" : "+a"(x[d]));
+}
+
+// Nothing moves across: what stands in front is issued in front.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// Operands that were loaded in front of a loop have arrived: without this the compiler waits for them inside the loop,
+// and there for everything that is on its way from memory, at every step.
+template <typename F, int N>
+__device__ __forceinline__ void arrived(F (&x)[N])
+{
+#pragma unroll
+    for (int s = 0; s < N; ++s) asm volatile("" : "+v"(x[s]));
+}
 
 // Eight scores in 32 bits to a B fragment.  16-bit types: rounded to nearest, which is the one rounding between
 // the inputs and the output (half a step of the type on each probability; sums and states stay in 32 bits).

@@ -13,8 +13,6 @@
 namespace bload {
 namespace {
 
-// ------------------------------------------------------------------ dq
-
 constexpr int kKeys = 64;
 
 // One row of dq from visible keys alone (see forward_row in bload_attention.hip): for rows that come
@@ -44,7 +42,7 @@ __device__ void dq_row(const AttArgs& a, int b, int head, int i, Span span)
 // A workgroup takes 128 queries of one head, a wavefront 32: q and do stay in registers as B fragments, dq^T as
 // the result; keys and values stream through LDS as in the forward kernel, the keys read by rows
 // (for the scores) and by columns (for dq).
-template <typename T, int DP, bool MOD>
+template <typename T, int DP, bool MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
@@ -54,8 +52,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     const int lane = lane_id(), wave = wave_id();
 
     const uint32_t item = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int g = (int)(item % a.G), tile = a.tiles - 1 - (int)((item / a.G) % a.tiles);
-    const int kv = (int)((item / a.G / a.tiles) % a.Hkv), b = (int)(item / a.G / a.tiles / a.Hkv);
+    const int g = (int)(item % a.G), kv = (int)((item / a.G) % a.Hkv);
+    const int tile = a.tiles - 1 - (int)((item / a.Hq) % a.tiles), b = (int)(item / a.Hq / a.tiles);
     const int head = kv * a.G + g, D = a.D, T_ = a.T;
     const int row = tile * 128 + wave * 32 + (lane & 31);
 
@@ -102,51 +100,67 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     }
     delta += other_half(delta);
     if (row < T_ && lane < 32) a.delta[((int64_t)b * a.Hq + head) * T_ + row] = delta;
+    arrived(q);
+    arrived(go);
     const Score score(a, head);
-    const float c = MOD ? 1.0f : a.scale * kLog2e;
+    const float c = a.scale * kLog2e;
 
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
-    const T* kp = att_at<T>(a.k, b, 0, kv);
-    const T* vp = att_at<T>(a.v, b, 0, kv);
-    Stage<T, DP, kKeys> next_k, next_v;
+    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
     if (lo < hi) {
-        next_k.load(kp, a.k.st, lo, hi, D);
-        next_v.load(vp, a.v.st, lo, hi, D);
+        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
+        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
+        next_k.load(lo, hi);
+        next_v.load(lo, hi);
     }
+    typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
+        if constexpr (sizeof(T) == 4) keep_sums(o);
         next_k.store(ks[buf]);
         next_v.store(vs[buf]);
         __syncthreads();
         if (k0 + kKeys < hi) {
-            next_k.load(kp, a.k.st, k0 + kKeys, hi, D);
-            next_v.load(vp, a.v.st, k0 + kKeys, hi, D);
+            next_k.load(k0 + kKeys, hi);
+            next_v.load(k0 + kKeys, hi);
         }
+        by_row.renew();
+        by_col.renew();
 #pragma unroll
         for (int t = 0; t < kKeys / 32; ++t) {
             if (!range.meets(k0 + 32 * t, 32)) continue;
             f32x16 x = {}, y = {};
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks[buf], 32 * t + (lane & 31), s), q[s], x);
+            for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks[buf], by_row, 32 * t, s), q[s], x);
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) y = mma(L::row_frag(vs[buf], 32 * t + (lane & 31), s), go[s], y);
+            for (int s = 0; s < kSteps; ++s) y = mma(L::row_frag(vs[buf], by_row, 32 * t, s), go[s], y);
             const int key0 = k0 + 32 * t + 4 * (lane >> 5);
-            const bool full = range.full(k0 + 32 * t, 32);
+            if (!MOD && !range.full(k0 + 32 * t, 32)) {    // what is hidden gets probability 0
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = key0 + 8 * (i / 4) + i % 4;
+                    x[i] = key >= span.lo && key < span.hi ? x[i] : -INFINITY;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int key = key0 + 8 * (i / 4) + i % 4;
                 float keep = 1.0f;
-                const float s = MOD ? score.of<T>(x[i], row - key, &keep) : x[i];
-                const float ds = exp2_fast(fmaf(s, c, -lse)) * (y[i] - delta) * keep;
-                x[i] = full || (key >= span.lo && key < span.hi) ? ds : 0.0f;
+                if constexpr (MOD) {                       // (a cap makes a finite score of -infinity: hidden here)
+                    const int key = key0 + 8 * (i / 4) + i % 4;
+                    const float s = score.of<T>(x[i], row - key, &keep);
+                    x[i] = key >= span.lo && key < span.hi ? exp2_fast(s - lse) : 0.0f;
+                } else {
+                    x[i] = exp2_fast(fmaf(x[i], c, -lse));
+                }
+                x[i] *= (y[i] - delta) * keep;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const frag8<T> p = pack8<T>(x, 8 * u);
 #pragma unroll
-                for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(ks[buf], 32 * t + 16 * u, 32 * d), p, o[d]);
+                for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(ks[buf], by_col, 32 * t + 16 * u, 32 * d), p, o[d]);
             }
         }
     }
@@ -177,190 +191,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     }
 }
 
-// ------------------------------------------------------------------ dk, dv
-
-// One row of dk and dv from the queries that see it alone.
-template <typename T>
-__device__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
-{
-    const int D = a.D;
-    float k[2], v[2], dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    load_row2(att_at<T>(a.k, b, j, kv), D, k);
-    load_row2(att_at<T>(a.v, b, j, kv), D, v);
-    for (int g = 0; g < a.G; ++g) {
-        const int head = kv * a.G + g;
-        const Score score(a, head);
-        const int64_t at = ((int64_t)b * a.Hq + head) * a.T;
-        for (int i = span.lo; i < span.hi; ++i) {
-            float q[2], go[2], keep;
-            load_row2(att_at<T>(a.q, b, i, head), D, q);
-            load_row2(att_at<T>(a.dout, b, i, head), D, go);
-            const float s = score.of<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, &keep);
-            const float p = exp2_fast(s - a.lse[at + i] * kLog2e);
-            const float ds = p * (wave_sum(go[0] * v[0] + go[1] * v[1]) - a.delta[at + i]) * keep;
-            for (int n = 0; n < 2; ++n) {
-                dv[n] += p * go[n];
-                dk[n] += ds * q[n];
-            }
-        }
-    }
-    store_row2(att_at<T>(a.dk, b, j, kv), D, dk[0] * a.scale, dk[1] * a.scale);
-    store_row2(att_at<T>(a.dv, b, j, kv), D, dv[0], dv[1]);
-}
-
-constexpr int kQueries = 32;           // queries of a tile
-
-// A workgroup takes 128 keys of one head of keys, a wavefront 32: k and v stay in registers as B fragments, dk^T and
-// dv^T as results; tiles of 32 queries with their do stream through LDS, head after head of those that
-// share the keys, read by rows for the scores and by columns for dk and dv.
-template <typename T, int DP, bool MOD>
-__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(AttArgs a)
-{
-    using L = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kParts = DP / 32;
-    __shared__ T qs[2][kQueries * DP], gs[2][kQueries * DP];
-    __shared__ float sums[2][2][kQueries];                 // lse (in units of ln 2) and delta of the tile's queries
-    __shared__ int hull[2][kThreads / kWave];
-    const int lane = lane_id(), wave = wave_id(), tid = (int)threadIdx.x;
-
-    const uint32_t item = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int tile = (int)(item % a.tiles);
-    const int kv = (int)((item / a.tiles) % a.Hkv), b = (int)(item / a.tiles / a.Hkv);
-    const int D = a.D, T_ = a.T;
-    const int row = tile * 128 + wave * 32 + (lane & 31);
-
-    Span span = {0, 0};
-    if (row < T_) {
-        const int4 r = a.mask[(int64_t)b * T_ + row];
-        span = clamp_span(r.z, r.w, T_);
-    }
-    SpanRange range;
-    range.of_wave(span);
-    if (lane == 0) {
-        hull[0][wave] = range.lo;
-        hull[1][wave] = range.hi;
-    }
-    __syncthreads();
-    const int lo = min(min(hull[0][0], hull[0][1]), min(hull[0][2], hull[0][3]));
-    const int hi = max(max(hull[1][0], hull[1][1]), max(hull[1][2], hull[1][3]));
-    const int steps = lo < hi ? (hi - lo + kQueries - 1) / kQueries : 0;
-
-    frag8<T> k[kSteps], v[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[s] = v[s] = frag8<T>{};
-    if (row < T_) {
-        const T* pk = att_at<T>(a.k, b, row, kv);
-        const T* pv = att_at<T>(a.v, b, row, kv);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            k[s] = load_frag(pk, 16 * s + 8 * (lane >> 5), D);
-            v[s] = load_frag(pv, 16 * s + 8 * (lane >> 5), D);
-        }
-    }
-    f32x16 dk[kParts], dv[kParts];
-#pragma unroll
-    for (int d = 0; d < kParts; ++d) dk[d] = dv[d] = f32x16{};
-
-    Stage<T, DP, kQueries> next_q, next_g;
-    float next_sum = 0.0f;
-    auto load = [&](int n) {
-        const int head = kv * a.G + n / steps, q0 = lo + (n % steps) * kQueries;
-        next_q.load(att_at<T>(a.q, b, 0, head), a.q.st, q0, hi, D);
-        next_g.load(att_at<T>(a.dout, b, 0, head), a.dout.st, q0, hi, D);
-        if (tid < 2 * kQueries) {
-            const int i = q0 + (tid & (kQueries - 1));
-            const int64_t at = ((int64_t)b * a.Hq + head) * T_ + i;
-            next_sum = i < hi ? (tid < kQueries ? a.lse[at] * kLog2e : a.delta[at]) : 0.0f;
-        }
-    };
-    const int all = steps * a.G;
-    if (all > 0) load(0);
-    int buf = 0;
-    for (int n = 0; n < all; ++n, buf ^= 1) {
-        next_q.store(qs[buf]);
-        next_g.store(gs[buf]);
-        if (tid < 2 * kQueries) sums[buf][tid / kQueries][tid & (kQueries - 1)] = next_sum;
-        __syncthreads();
-        if (n + 1 < all) load(n + 1);
-        const int q0 = lo + (n % steps) * kQueries;
-        if (!range.meets(q0, kQueries)) continue;
-        const Score score(a, kv * a.G + n / steps);
-        const float c = MOD ? 1.0f : a.scale * kLog2e;
-        f32x16 x = {}, y = {};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(qs[buf], lane & 31, s), k[s], x);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) y = mma(L::row_frag(gs[buf], lane & 31, s), v[s], y);
-        const bool full = range.full(q0, kQueries);
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            const int at = 8 * i4 + 4 * (lane >> 5);
-            f32x4 lse, delta;
-            __builtin_memcpy(&lse, &sums[buf][0][at], 16);
-            __builtin_memcpy(&delta, &sums[buf][1][at], 16);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = 4 * i4 + j, query = q0 + at + j;
-                float keep = 1.0f;
-                const float s = MOD ? score.of<T>(x[i], query - row, &keep) : x[i];
-                const bool sees = full || (query >= span.lo && query < span.hi);
-                const float p = exp2_fast(fmaf(s, c, -lse[j]));
-                x[i] = sees ? p : 0.0f;
-                y[i] = sees ? p * (y[i] - delta[j]) * keep : 0.0f;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const frag8<T> p = pack8<T>(x, 8 * u), ds = pack8<T>(y, 8 * u);
-#pragma unroll
-            for (int d = 0; d < kParts; ++d) {
-                dv[d] = mma(L::col_frag(gs[buf], 16 * u, 32 * d), p, dv[d]);
-                dk[d] = mma(L::col_frag(qs[buf], 16 * u, 32 * d), ds, dk[d]);
-            }
-        }
-    }
-    bool bad = false;
-#pragma unroll
-    for (int d = 0; d < kParts; ++d) {
-        dk[d] *= a.scale;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) bad |= not_finite(dk[d][i]) || not_finite(dv[d][i]);
-        if (span.hi <= span.lo) dk[d] = dv[d] = f32x16{};
-    }
-    if (row < T_) {
-        T* pk = att_at<T>(a.dk, b, row, kv);
-        T* pv = att_at<T>(a.dv, b, row, kv);
-#pragma unroll
-        for (int d = 0; d < kParts; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = 32 * d + 8 * i + 4 * (lane >> 5);
-                const f32x4 y = {dk[d][4 * i], dk[d][4 * i + 1], dk[d][4 * i + 2], dk[d][4 * i + 3]};
-                const f32x4 z = {dv[d][4 * i], dv[d][4 * i + 1], dv[d][4 * i + 2], dv[d][4 * i + 3]};
-                store4(pk, at, D, y);
-                store4(pv, at, D, z);
-            }
-    }
-    uint64_t again = __ballot(bad && span.hi > span.lo);
-    again = (again | (again >> 32)) & 0xffffffffu;
-    while (again) {
-        const int r = __ffsll((unsigned long long)again) - 1;
-        again &= again - 1;
-        dkv_row<T>(a, b, kv, tile * 128 + wave * 32 + r, {__shfl(span.lo, r), __shfl(span.hi, r)});
-    }
-}
-
 template <typename T, int DP>
-void launch(const AttArgs& a, hipStream_t stream)
+void launch_dq(const AttArgs& a, hipStream_t stream)
 {
-    const dim3 block(kThreads), by_query((unsigned)((int64_t)a.B * a.Hq * a.tiles)), by_key((unsigned)((int64_t)a.B * a.Hkv * a.tiles));
-    if (a.cap > 0.0f || a.slopes) {
-        attention_dq_kernel<T, DP, true><<<by_query, block, 0, stream>>>(a);
-        attention_dkv_kernel<T, DP, true><<<by_key, block, 0, stream>>>(a);
-    } else {
-        attention_dq_kernel<T, DP, false><<<by_query, block, 0, stream>>>(a);
-        attention_dkv_kernel<T, DP, false><<<by_key, block, 0, stream>>>(a);
-    }
+    const dim3 grid((unsigned)((int64_t)a.B * a.Hq * a.tiles)), block(kThreads);
+    att_variant<T>(a, [&](auto mod, auto odd) { attention_dq_kernel<T, DP, mod.value, odd.value><<<grid, block, 0, stream>>>(a); });
 }
 
 }  // namespace
@@ -396,6 +231,7 @@ extern "C" bload_status bload_segment_attention_backward(const bload_heads* dout
     if (workspace_bytes < bload_segment_attention_backward_workspace_bytes(num_blocks, t_blk, heads_q)) return BLOAD_EWORKSPACE;
     a.lse = const_cast<float*>(d_lse);
     a.delta = static_cast<float*>(d_workspace);
-    att_dispatch(dtype, head_dim, [&](auto type, auto dim) { launch<typename decltype(type)::type, decltype(dim)::value>(a, (hipStream_t)hip_stream); });
-    return launch_status();
+    att_dispatch(dtype, head_dim, [&](auto type, auto dim) { launch_dq<typename decltype(type)::type, decltype(dim)::value>(a, (hipStream_t)hip_stream); });
+    if ((st = launch_status()) != BLOAD_OK) return st;
+    return attention_dkv(a, dtype, (hipStream_t)hip_stream);
 }

@@ -34,7 +34,7 @@ __device__ __forceinline__ int decode_length(const DecodeArgs& p, int64_t seq, i
 }
 
 // One share of one sequence for up to 32 heads of queries.
-template <typename T, int DP, bool MOD>
+template <typename T, int DP, bool MOD, bool ODD>
 __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p)
 {
     using L = Tile<T, DP>;
@@ -70,6 +70,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = load_frag(pq, 16 * s + 8 * (lane >> 5), D);
     }
+    arrived(q);
     const Score score(a, head);
     const float c = MOD ? 1.0f : a.scale * kLog2e;
     f32x16 o[kParts];
@@ -77,13 +78,14 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
     float m = -INFINITY, l = 0.0f;
 
-    const T* kp = n > 0 ? att_at<T>(a.k, b, off, kv) : nullptr;
-    const T* vp = n > 0 ? att_at<T>(a.v, b, off, kv) : nullptr;
-    Stage<T, DP, kTileKeys, kWave> next_k, next_v;
+    Stage<T, DP, kTileKeys, ODD, kWave> next_k(a.k.st, D), next_v(a.v.st, D);
+    typename L::Reader by_row = L::rows(), by_col = L::columns();
     int k0 = lo + wave * kTileKeys;
     if (k0 < hi) {
-        next_k.load(kp, a.k.st, k0, hi, D);
-        next_v.load(vp, a.v.st, k0, hi, D);
+        next_k.begin(att_at<T>(a.k, b, off, kv), k0);
+        next_v.begin(att_at<T>(a.v, b, off, kv), k0);
+        next_k.load(k0, hi);
+        next_v.load(k0, hi);
     }
     for (; k0 < hi; k0 += kWaves * kTileKeys) {
         next_k.store(ks);
@@ -93,12 +95,16 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         const int k1 = k0 + kWaves * kTileKeys;
         if (k1 < hi) {
-            next_k.load(kp, a.k.st, k1, hi, D);
-            next_v.load(vp, a.v.st, k1, hi, D);
+            next_k.skip((kWaves - 1) * kTileKeys);
+            next_v.skip((kWaves - 1) * kTileKeys);
+            next_k.load(k1, hi);
+            next_v.load(k1, hi);
         }
+        by_row.renew();
+        by_col.renew();
         f32x16 x = {};
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks, lane & 31, s), q[s], x);
+        for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks, by_row, 0, s), q[s], x);
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -126,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
         for (int u = 0; u < 2; ++u) {
             const frag8<T> w = pack8<T>(x, 8 * u);
 #pragma unroll
-            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs, 16 * u, 32 * d), w, o[d]);
+            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs, by_col, 16 * u, 32 * d), w, o[d]);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -218,8 +224,7 @@ template <typename T, int DP>
 void launch(const DecodeArgs& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)(p.n_seq * p.a.Hkv * p.splits * p.column_groups)), block(kThreads);
-    if (p.a.cap > 0.0f || p.a.slopes) attention_decode_kernel<T, DP, true><<<grid, block, 0, stream>>>(p);
-    else attention_decode_kernel<T, DP, false><<<grid, block, 0, stream>>>(p);
+    att_variant<T>(p.a, [&](auto mod, auto odd) { attention_decode_kernel<T, DP, mod.value, odd.value><<<grid, block, 0, stream>>>(p); });
     if (p.splits > 1)
         attention_join_kernel<T><<<dim3((unsigned)ceil_div(p.n_seq * p.a.Hq, kThreads / kWave)), block, 0, stream>>>(p);
 }

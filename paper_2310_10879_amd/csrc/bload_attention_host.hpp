@@ -13,6 +13,9 @@ inline size_t att_elem_bytes(bload_dtype dtype) { return dtype == BLOAD_F32 ? 4 
 
 inline bool att_dtype(bload_dtype dtype) { return dtype == BLOAD_F16 || dtype == BLOAD_BF16 || dtype == BLOAD_F32; }
 
+// bload_attention_dkv.hip: dk and dv, behind the kernel that leaves delta.
+bload_status attention_dkv(const AttArgs& a, bload_dtype dtype, hipStream_t stream);
+
 // Everything but the tensors.  `rows`: slots of a workgroup's tile.
 inline bload_status att_args(AttArgs& a, int64_t num_blocks, int32_t t_blk, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
                              bload_dtype dtype, float scale, float cap, const float* d_slopes, const int32_t* d_mask, int rows)
@@ -64,6 +67,16 @@ inline void att_dispatch(bload_dtype dtype, int32_t D, F f)
     if (dtype == BLOAD_F16) att_dispatch_dim<att_half>(D, f);
     else if (dtype == BLOAD_BF16) att_dispatch_dim<att_bf16>(D, f);
     else att_dispatch_dim<float>(D, f);
+}
+
+// A kernel's variant: with the cap and the slopes compiled in, and for heads that are no whole number of 16 bytes (which come
+// with cap and slopes only, to be looked at as the kernel runs: fewer instances of what loads slowly anyway).
+template <typename T, typename F>
+inline void att_variant(const AttArgs& a, F f)
+{
+    if (a.D % (16 / (int)sizeof(T))) f(std::true_type(), std::true_type());
+    else if (a.cap > 0.0f || a.slopes) f(std::true_type(), std::false_type());
+    else f(std::false_type(), std::false_type());
 }
 
 }  // namespace bload

@@ -2119,6 +2119,7 @@ extern "C" bload_status bload_segment_reduce(const void* d_packed, const int32_t
         case BLOAD_F16: launch_reduce<half_bits>(p, a, stream); break;
         case BLOAD_F32: launch_reduce<float>(p, a, stream); break;
         case BLOAD_I32: launch_reduce<int32_t>(p, a, stream); break;
+        case BLOAD_BF16: return BLOAD_EINVAL;      // (refused above)
     }
     return launch_status();
 }
