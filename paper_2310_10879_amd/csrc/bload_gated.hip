@@ -47,65 +47,57 @@ __device__ __forceinline__ int slot_code(const GatedArgs& a, const uint8_t* rese
     return (t == 0 ? has_state : valid[t - 1] != 0) ? 2 : 1;
 }
 
-template <typename T>
-__device__ __forceinline__ vec16 row16(const void* base, int64_t row, int D, int d)
-{
-    return load_chunk(reinterpret_cast<const T*>(base) + row * D, d, D);
-}
-
+// V elements side by side, as they lie in memory; any alignment.  A lane whose V elements would pass the end of a row takes the
+// row's last V instead (some of them are its neighbour's too, which computes and stores the same).
 template <typename T, int V>
-__device__ __forceinline__ void widen(vec16 c, float (&x)[V])
-{
-    T t[V];
-    __builtin_memcpy(&t, &c, 16);
+struct Piece {
+    static constexpr int kWords = V * sizeof(T) >= 4 ? V * (int)sizeof(T) / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const void* base, int64_t row, int D, int d)
+    {
+        __builtin_memcpy(&w, reinterpret_cast<const T*>(base) + row * D + d, V * sizeof(T));
+    }
+    __device__ __forceinline__ void widen(float (&x)[V]) const
+    {
+        T t[V];
+        __builtin_memcpy(&t, &w, sizeof(t));
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = (float)t[v];
-}
+        for (int v = 0; v < V; ++v) x[v] = (float)t[v];
+    }
+};
 
 template <typename T, int V>
-__device__ __forceinline__ void store16(void* base, int64_t row, int D, int d, const float (&x)[V])
+__device__ __forceinline__ void store_piece(void* base, int64_t row, int D, int d, const float (&x)[V])
 {
     T t[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) t[v] = (T)x[v];
-    T* p = reinterpret_cast<T*>(base) + row * D + d;
-    if (d + V <= D) {
-        __builtin_memcpy(p, &t, 16);
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (d + v < D) p[v] = t[v];
-    }
+    __builtin_memcpy(reinterpret_cast<T*>(base) + row * D + d, &t, sizeof(t));
 }
 
 template <int V>
 __device__ __forceinline__ void load_state(const float* base, int64_t b, int D, int d, float (&x)[V])
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = base && d + v < D ? base[b * D + d + v] : 0.0f;
+    for (int v = 0; v < V; ++v) x[v] = base ? base[b * D + d + v] : 0.0f;
 }
 
-// K slots of one lane, `n` of them inside the chunk, in the order of the recurrence: slot i is row
-// first + i forward, first - i backward.
-template <typename T, int K, bool BACK>
+// K slots of one lane in the order of the recurrence: slot i is row first + i forward, first - i backward, and the chunk's last
+// one, `end`, in the place of those behind it (nothing becomes of them).
+template <typename T, int V, int K, bool BACK>
 struct Run {
-    static constexpr int V = 16 / (int)sizeof(T);
-    vec16 gate[K], x[K], h[BACK ? K : 1];
+    Piece<T, V> gate[K], x[K], h[BACK ? K : 1];
 
-    __device__ __forceinline__ void load(const GatedArgs& a, int64_t b, int first, int n, int d, bool want_h)
+    __device__ __forceinline__ void load(const GatedArgs& a, int64_t b, int first, int end, int d, bool want_h)
     {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            gate[i] = x[i] = vec16{0, 0, 0, 0};
-            if constexpr (BACK) h[i] = vec16{0, 0, 0, 0};
-            if (i < n && d < a.D) {
-                const int t = BACK ? first - i : first + i;
-                const int64_t row = b * a.T + t;
-                gate[i] = row16<T>(a.gate, row, a.D, d);
-                x[i] = row16<T>(a.x, row, a.D, d);
-                if constexpr (BACK)
-                    if (want_h && t > 0) h[i] = row16<T>(a.h, row - 1, a.D, d);
-            }
+            const int t = BACK ? max(first - i, end) : min(first + i, end);
+            const int64_t row = b * a.T + t;
+            gate[i].load(a.gate, row, a.D, d);
+            x[i].load(a.x, row, a.D, d);
+            if constexpr (BACK)
+                if (want_h) h[i].load(a.h, t > 0 ? row - 1 : row, a.D, d);
         }
     }
 };
@@ -138,20 +130,20 @@ struct Map {
     }
 };
 
-template <typename T, int K, bool BACK, int MODE>
+template <typename T, int V, int K, bool BACK, int MODE>
 __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
 {
-    using R = Run<T, K, BACK>;
-    constexpr int V = R::V, kWaves = kThreads / kWave;
+    constexpr int kWaves = kThreads / kWave;
     __shared__ uint8_t code[2][kThreads * K];
     __shared__ float total[2][kWaves][2][kWave * V];       // of a wave's lanes together, by feature
-    __shared__ int cuts[2][kWaves];
+    __shared__ int cuts[2][kWaves], folded[8];
 
     const int lane = lane_id(), wave = wave_id(), tid = (int)threadIdx.x;
     const int F = a.F, runs = kThreads / F, f = tid & (F - 1), run = tid / F;
     const int slice = (int)(blockIdx.x % a.slices), chunk = (int)((blockIdx.x / a.slices) % a.chunks);
     const int64_t b = blockIdx.x / a.slices / a.chunks;
-    const int d = (slice * F + f) * V;
+    const bool mine = (slice * F + f) * V < a.D;
+    const int d = min((slice * F + f) * V, a.D - V);
     // chunk c holds the slots c * chunk .. of the block in the order of the recurrence
     const int c0 = chunk * a.chunk, c1 = min(c0 + a.chunk, a.T);
     const uint8_t* reset = a.reset + b * a.T;
@@ -161,18 +153,52 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
     // what enters the chunk
     float in[V];
     load_state<V>(a.in, b, a.D, d, in);
-    if (MODE == kApply)
-        for (int c = 0; c < chunk; ++c) {
-            Map<V> m;
-            const float* p = a.maps + (b * a.chunks + c) * 2 * a.D;
-            m.cut = a.cut[b * a.chunks + c];
+    if (MODE == kApply && chunk > 0) {
+        // the maps of the chunks in front, an eighth of them to each of eight runs (four loads on their way at a time), then
+        // those eight one after another
+        const int folds = min(runs, 8), each = (chunk + folds - 1) / folds;
+        float (*fold)[2][kWave * V / 2] = reinterpret_cast<float (*)[2][kWave * V / 2]>(&total[0][0][0][0]);
+        if (run < folds) {
+            Map<V> all;
+            all.one();
+            for (int c = run * each; c < min((run + 1) * each, chunk); c += 4) {
+                Map<V> m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t at = b * a.chunks + min(c + i, chunk - 1);
+                    m[i].cut = a.cut[at];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        m[i].A[v] = a.maps[at * 2 * a.D + d + v];
+                        m[i].H[v] = a.maps[(at * 2 + 1) * a.D + d + v];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c + i < min((run + 1) * each, chunk)) {
+                        m[i].after(all);
+                        all = m[i];
+                    }
+            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                m.A[v] = d + v < a.D ? p[d + v] : 0.0f;
-                m.H[v] = d + v < a.D ? p[a.D + d + v] : 0.0f;
+                fold[run][0][f * V + v] = all.A[v];
+                fold[run][1][f * V + v] = all.H[v];
+            }
+            if (f == 0) folded[run] = all.cut;
+        }
+        __syncthreads();
+        for (int r = 0; r < folds; ++r) {
+            Map<V> m;
+            m.cut = folded[r];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                m.A[v] = fold[r][0][f * V + v];
+                m.H[v] = fold[r][1][f * V + v];
             }
             m.apply(in);
         }
+    }
     Map<V> sum;                                            // kMaps: of the chunk so far
     sum.one();
 
@@ -186,17 +212,13 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
     auto slots_left = [&](int s) { return min(max(c1 - (s + run * K), 0), K); };
     auto first_slot = [&](int s) { return BACK ? a.T - 1 - (s + run * K) : s + run * K; };
 
-    R now, next;
-    next.load(a, b, first_slot(c0), slots_left(c0), d, MODE == kApply);
+    Run<T, V, K, BACK> now;
     load_code(c0, 0);
     int buf = 0;
     for (int s = c0; s < c1; s += span, buf ^= 1) {
-        now = next;
+        now.load(a, b, first_slot(s), BACK ? a.T - c1 : c1 - 1, d, MODE == kApply);
         __syncthreads();                                   // code[buf] is there
-        if (s + span < c1) {
-            next.load(a, b, first_slot(s + span), slots_left(s + span), d, MODE == kApply);
-            load_code(s + span, buf ^ 1);
-        }
+        if (s + span < c1) load_code(s + span, buf ^ 1);
         int what[K];
 #pragma unroll
         for (int i = 0; i < K; ++i) what[i] = code[buf][run * K + i];        // 3 behind the chunk's end: nothing happens
@@ -205,8 +227,8 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             float g[V], x[V];
-            widen<T, V>(now.gate[i], g);
-            widen<T, V>(now.x[i], x);
+            now.gate[i].widen(g);
+            now.x[i].widen(x);
             if (what[i] == 3) continue;
             if constexpr (!BACK) {
 #pragma unroll
@@ -279,18 +301,18 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
         const int n = slots_left(s), first = first_slot(s);
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            if (i >= n || d >= a.D) continue;
+            if (i >= n || !mine) continue;
             const int64_t row = b * a.T + (BACK ? first - i : first + i);
             float g[V], x[V];
-            widen<T, V>(now.gate[i], g);
-            widen<T, V>(now.x[i], x);
+            now.gate[i].widen(g);
+            now.x[i].widen(x);
             if constexpr (!BACK) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) at[v] = what[i] == 2 ? fmaf(g[v], at[v], x[v]) : (what[i] == 1 ? x[v] : 0.0f);
-                store16<T, V>(a.y, row, a.D, d, at);
+                store_piece<T, V>(a.y, row, a.D, d, at);
             } else {
                 float h[V], dg[V];
-                if (first - i > 0) widen<T, V>(now.h[i], h);
+                if (first - i > 0) now.h[i].widen(h);
                 else load_state<V>(a.h0, b, a.D, d, h);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
@@ -298,25 +320,23 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
                     dg[v] = what[i] == 2 ? x[v] * h[v] : 0.0f;
                     at[v] = what[i] == 2 ? g[v] * x[v] : 0.0f;
                 }
-                store16<T, V>(a.y, row, a.D, d, x);
-                store16<T, V>(a.dgate, row, a.D, d, dg);
+                store_piece<T, V>(a.y, row, a.D, d, x);
+                store_piece<T, V>(a.dgate, row, a.D, d, dg);
             }
         }
     }
-    if (d >= a.D || run != 0) return;
+    if (!mine || run != 0) return;
     if (MODE == kMaps) {
         float* p = a.maps + (b * a.chunks + chunk) * 2 * a.D;
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (d + v < a.D) {
-                p[d + v] = sum.A[v];
-                p[a.D + d + v] = sum.H[v];
-            }
+        for (int v = 0; v < V; ++v) {
+            p[d + v] = sum.A[v];
+            p[a.D + d + v] = sum.H[v];
+        }
         if (d == 0) a.cut[b * a.chunks + chunk] = (uint8_t)(sum.cut != 0);
     } else if (chunk == a.chunks - 1 && a.last) {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (d + v < a.D) a.last[b * a.D + d + v] = in[v];
+        for (int v = 0; v < V; ++v) a.last[b * a.D + d + v] = in[v];
     }
 }
 
@@ -324,14 +344,13 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
 // to its last.
 constexpr int kShort = 8;
 
-template <typename T, bool BACK>
+template <typename T, int V, bool BACK>
 __global__ __launch_bounds__(kThreads) void gated_short_kernel(GatedArgs a, int64_t lanes)
 {
-    constexpr int V = 16 / (int)sizeof(T);
     const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (n >= lanes) return;
     const int64_t b = n / a.slices;
-    const int d = (int)(n - b * a.slices) * V;
+    const int d = min((int)(n - b * a.slices) * V, a.D - V);
     const bool has_state = (BACK ? a.h0 : a.in) != nullptr;
     const uint8_t* reset = a.reset + b * a.T;
     const uint8_t* valid = a.valid + b * a.T;
@@ -342,30 +361,36 @@ __global__ __launch_bounds__(kThreads) void gated_short_kernel(GatedArgs a, int6
         const int64_t row = b * a.T + t;
         const int what = slot_code(a, reset, valid, t, has_state);
         float g[V], x[V];
-        widen<T, V>(row16<T>(a.gate, row, a.D, d), g);
-        widen<T, V>(row16<T>(a.x, row, a.D, d), x);
+        Piece<T, V> piece;
+        piece.load(a.gate, row, a.D, d);
+        piece.widen(g);
+        piece.load(a.x, row, a.D, d);
+        piece.widen(x);
         if constexpr (!BACK) {
 #pragma unroll
             for (int v = 0; v < V; ++v) at[v] = what == 2 ? fmaf(g[v], at[v], x[v]) : (what == 1 ? x[v] : 0.0f);
-            store16<T, V>(a.y, row, a.D, d, at);
+            store_piece<T, V>(a.y, row, a.D, d, at);
         } else {
             float h[V], dg[V];
-            if (t > 0) widen<T, V>(row16<T>(a.h, row - 1, a.D, d), h);
-            else load_state<V>(a.h0, b, a.D, d, h);
+            if (t > 0) {
+                piece.load(a.h, row - 1, a.D, d);
+                piece.widen(h);
+            } else {
+                load_state<V>(a.h0, b, a.D, d, h);
+            }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 x[v] = what ? x[v] + at[v] : 0.0f;
                 dg[v] = what == 2 ? x[v] * h[v] : 0.0f;
                 at[v] = what == 2 ? g[v] * x[v] : 0.0f;
             }
-            store16<T, V>(a.y, row, a.D, d, x);
-            store16<T, V>(a.dgate, row, a.D, d, dg);
+            store_piece<T, V>(a.y, row, a.D, d, x);
+            store_piece<T, V>(a.dgate, row, a.D, d, dg);
         }
     }
     if (a.last)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (d + v < a.D) a.last[b * a.D + d + v] = at[v];
+        for (int v = 0; v < V; ++v) a.last[b * a.D + d + v] = at[v];
 }
 
 struct GatedPlan {
@@ -374,20 +399,23 @@ struct GatedPlan {
     size_t maps, bytes;              // of the chunks' maps alone, of the workspace
 };
 
-constexpr int kForwardSlots = 8, kBackwardSlots = 4;      // of a lane at a time
+// Elements and slots of a lane at a time.  What the lanes exchange goes by the elements, so few elements and many slots cost
+// least of it.
+constexpr int kPiece = 4;                                  // (1 where a row has fewer than 4)
+constexpr int kSlots = 8;
 
-// Features across 32 lanes (512 bytes of a row), fewer where a row is shorter; a block to a workgroup, or where that
-// makes fewer than two workgroups for each CU, chunks of whole steps.
-inline GatedPlan gated_plan(int64_t B, int32_t T, int64_t D, size_t elem, bool back)
+// Features across 32 lanes, fewer where a row is shorter; a block to a workgroup, or where that
+// makes fewer workgroups than there are CUs, chunks of whole steps.
+inline GatedPlan gated_plan(int64_t B, int32_t T, int64_t D)
 {
     GatedPlan p = {};
-    const int64_t lanes = ceil_div(D, 16 / (int64_t)elem);
+    const int64_t lanes = D < kPiece ? D : ceil_div(D, kPiece);
     p.F = 1;
     while (p.F < 32 && p.F < lanes) p.F *= 2;
     p.slices = (int32_t)ceil_div(lanes, p.F);
-    const int64_t step = (int64_t)(kThreads / p.F) * (back ? kBackwardSlots : kForwardSlots);
+    const int64_t step = (int64_t)(kThreads / p.F) * kSlots;
     const int64_t steps = ceil_div(T, step), alone = B * p.slices;
-    int64_t chunks = alone < 512 ? std::min<int64_t>({ceil_div(1024, alone), steps, 64}) : 1;
+    int64_t chunks = alone < 256 ? std::min<int64_t>({ceil_div(1024, alone), steps, 64}) : 1;
     p.chunk = (int32_t)(ceil_div(steps, chunks) * step);
     p.chunks = (int32_t)ceil_div(T, p.chunk);
     p.groups = alone * p.chunks;
@@ -407,25 +435,28 @@ inline bload_status gated_check(int64_t num_blocks, int32_t t_blk, int64_t feat_
     return BLOAD_OK;
 }
 
-template <typename T, int K, bool BACK>
+template <typename T, int V, bool BACK>
 void gated_launch(const GatedArgs& a, const GatedPlan& p, hipStream_t stream)
 {
     const dim3 grid((unsigned)p.groups), block(kThreads);
-    if (p.chunks > 1) gated_kernel<T, K, BACK, kMaps><<<grid, block, 0, stream>>>(a);
-    gated_kernel<T, K, BACK, kApply><<<grid, block, 0, stream>>>(a);
+    if (p.chunks > 1) gated_kernel<T, V, kSlots, BACK, kMaps><<<grid, block, 0, stream>>>(a);
+    gated_kernel<T, V, kSlots, BACK, kApply><<<grid, block, 0, stream>>>(a);
 }
 
 template <typename T, bool BACK>
 bload_status gated_run(GatedArgs a, int64_t B, void* workspace, size_t room, hipStream_t stream)
 {
     if (a.T <= kShort) {
-        a.slices = (int32_t)ceil_div(a.D, 16 / (int64_t)sizeof(T));
+        const int V = a.D < kPiece ? 1 : kPiece;
+        a.slices = (int32_t)ceil_div(a.D, V);
         const int64_t lanes = B * a.slices, groups = ceil_div(lanes, kThreads);
         if (groups > 0x7fffffff) return BLOAD_EOVERFLOW;
-        gated_short_kernel<T, BACK><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a, lanes);
+        const dim3 grid((unsigned)groups), block(kThreads);
+        if (V == 1) gated_short_kernel<T, 1, BACK><<<grid, block, 0, stream>>>(a, lanes);
+        else gated_short_kernel<T, kPiece, BACK><<<grid, block, 0, stream>>>(a, lanes);
         return launch_status();
     }
-    const GatedPlan p = gated_plan(B, a.T, a.D, sizeof(T), BACK);
+    const GatedPlan p = gated_plan(B, a.T, a.D);
     if (p.groups > 0x7fffffff) return BLOAD_EOVERFLOW;
     if (p.bytes) {
         if (!workspace) return BLOAD_EINVAL;
@@ -438,7 +469,8 @@ bload_status gated_run(GatedArgs a, int64_t B, void* workspace, size_t room, hip
     a.slices = p.slices;
     a.chunks = p.chunks;
     a.chunk = p.chunk;
-    gated_launch<T, BACK ? kBackwardSlots : kForwardSlots, BACK>(a, p, stream);
+    if (a.D < kPiece) gated_launch<T, 1, BACK>(a, p, stream);
+    else gated_launch<T, kPiece, BACK>(a, p, stream);
     return launch_status();
 }
 
@@ -458,8 +490,7 @@ using namespace bload;
 extern "C" size_t bload_gated_scan_workspace_bytes(int64_t num_blocks, int32_t t_blk, int64_t feat_dim, bload_dtype dtype)
 {
     if (num_blocks <= 0 || gated_check(num_blocks, t_blk, feat_dim, dtype) != BLOAD_OK || t_blk <= kShort) return 0;
-    return std::max(gated_plan(num_blocks, t_blk, feat_dim, att_elem_bytes(dtype), false).bytes,
-                    gated_plan(num_blocks, t_blk, feat_dim, att_elem_bytes(dtype), true).bytes);
+    return gated_plan(num_blocks, t_blk, feat_dim).bytes;
 }
 
 extern "C" bload_status bload_gated_scan(const void* d_gate, const void* d_x, const uint8_t* d_reset, const uint8_t* d_valid,
