@@ -507,11 +507,13 @@ bload_status bload_gated_scan_backward(const void* d_dout, const void* d_gate, c
  * i + rot_dim / 2, or 2 i and 2 i + 1) are turned by position * d_freq[i] radians and multiplied
  * by `scale`; the elements behind are handed through.  inverse = 1 turns back: the gradient.
  *
- * x, out       [num_blocks, t_blk, heads, head_dim] of F16, BF16 or F32; out may be x
+ * x, out       [num_blocks, t_blk, heads, head_dim] of F16, BF16 or F32; out may be x;
+ *              rot_dim even, 2 .. BLOAD_ROTARY_MAX_DIM, head_dim up to 65536
  * d_positions  in   int32[num_blocks, t_blk]: frame_idx of bload_pack, or any others; negative
  *                   ones are padding, whose elements become 0
  * d_freq       in   float32[rot_dim / 2], radians per frame
  * Angles are formed in 64 bits.  Asynchronous on `hip_stream`, no workspace. */
+#define BLOAD_ROTARY_MAX_DIM 4096
 typedef enum { BLOAD_ROTARY_HALF = 0, BLOAD_ROTARY_INTERLEAVED = 1 } bload_rotary_layout;
 
 bload_status bload_rotary(const bload_heads* x, const int32_t* d_positions, int64_t num_blocks, int32_t t_blk, int32_t heads,
