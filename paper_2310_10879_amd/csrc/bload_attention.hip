@@ -48,7 +48,7 @@ template <typename T, int DP, bool MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kParts = DP / 32;
+    constexpr int kSteps = DP / 16, kParts = DP / 32, kAhead = sizeof(T) == 2 ? 3 : 1;      // fragments on their way from LDS
     __shared__ T ks[2][kKeys * DP], vs[2][kKeys * DP];
     __shared__ int hull[2][kThreads / kWave];
     const int lane = lane_id(), wave = wave_id();
@@ -90,7 +90,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
-    float m = -INFINITY, l = 0.0f;
+    Maximum max;
+    float l = 0.0f;
 
     Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
     if (lo < hi) {
@@ -113,13 +114,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         by_row.renew();
         by_col.renew();
         if (!range.meets(k0, kKeys)) continue;
-        f32x16 x[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            x[t] = f32x16{};
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) x[t] = mma(L::row_frag(ks[buf], by_row, 32 * t, s), q[s], x[t]);
-        }
+        f32x16 x[2] = {{}, {}};
+        ahead<2 * kSteps, kAhead>([&](int n) { return L::row_frag(ks[buf], by_row, 32 * (n / kSteps), n % kSteps); },
+                                  [&](int n, frag8<T> f) { x[n / kSteps] = mma(f, q[n % kSteps], x[n / kSteps]); });
         const int key0 = k0 + 4 * (lane >> 5);
         if constexpr (MOD) {
 #pragma unroll
@@ -141,31 +138,31 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
-        top = fmaxf(top, other_half(top));
-        const float up = fmaxf(m, top * c), base = up == -INFINITY ? 0.0f : up;
-        const float f = exp2_fast(m - base);
-        m = up;
-        float sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                x[t][i] = exp2_fast(fmaf(x[t][i], c, -base));
-                sum += x[t][i];
-            }
-        l = l * f + sum;
-        if (__any(f != 1.0f)) {
+        float f, sum = 0.0f;
+        if (max.moves(halves_max(top) * c, f)) {
+            l *= f;
 #pragma unroll
             for (int d = 0; d < kParts; ++d) o[d] *= f;
         }
+        const float base = max.base();
+        auto probability = [&](int t, int i) {
+            x[t][i] = exp2_fast(fmaf(x[t][i], c, -base));
+            sum += x[t][i];
+        };
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const frag8<T> p = pack8<T>(x[t >> 1], 8 * (t & 1));
+        for (int i = 0; i < 16; ++i) probability(0, i);
+        // the second half's probabilities between the products of the first
+        ahead<4 * kParts, kAhead>([&](int n) { return L::col_frag(vs[buf], by_col, 16 * (n / kParts), 32 * (n % kParts)); },
+                                  [&](int n, frag8<T> f) {
+                                      const int t = n / kParts, d = n % kParts;
+                                      o[d] = mma(f, pack8<T>(x[t >> 1], 8 * (t & 1)), o[d]);
+                                      if (n < 2 * kParts)
 #pragma unroll
-            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs[buf], by_col, 16 * t, 32 * d), p, o[d]);
-        }
+                                          for (int i = 8 * n / kParts; i < 8 * (n + 1) / kParts; ++i) probability(1, i);
+                                  });
+        l += sum;
     }
-    l += other_half(l);
+    l = halves_sum(l);
     const float inv = span.hi > span.lo ? 1.0f / l : 0.0f;
     bool bad = false;
 #pragma unroll
@@ -196,7 +193,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
                 }
         }
         if (a.lse && lane < 32)
-            a.lse[((int64_t)b * a.Hq + head) * T_ + row] = span.hi > span.lo ? (m + log2f(l)) * kLn2 : -INFINITY;
+            a.lse[((int64_t)b * a.Hq + head) * T_ + row] = span.hi > span.lo ? (max.m + log2f(l)) * kLn2 : -INFINITY;
     }
     uint64_t again = __ballot(bad && span.hi > span.lo);
     again = (again | (again >> 32)) & 0xffffffffu;

@@ -167,7 +167,8 @@ struct Tile {
             const int r = 4 * (lane >> 5) + ((lane & 15) >> 2);
             return {r * kChunks * 16 + (lane & 1) * 8, ((((lane & 16) >> 3) | ((lane & 3) >> 1)) ^ swizzle(r)) * 16};
         } else {
-            return {0, 0};
+            const int d = lane & 31, r = 4 * (lane >> 5);
+            return {r * kChunks * 16 + (d & 3) * 4, ((d >> 2) ^ swizzle(r)) * 16};
         }
     }
     // element d0 + lane % 32 of the rows r0 + {4 h + 0..3, 8 + 4 h + 0..3}, h = lane / 32; r0: a multiple of 16, d0 of 32
@@ -184,10 +185,12 @@ struct Tile {
             __builtin_memcpy(&f, &x, sizeof(f));
             return f;
         } else {
-            const int lane = lane_id(), row = r0 + 4 * (lane >> 5), d = d0 + (lane & 31);
+            // (the swizzle is linear: that of row 4 h + j is that of 4 h XOR that of j)
             frag8<T> f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = tile[at(row + (j & 3) + 8 * (j >> 2), d / kElems) + d % kElems];
+            for (int j = 0; j < 8; ++j)
+                f[j] = *reinterpret_cast<const T*>(reinterpret_cast<const char*>(tile) + r.off + (((d0 / 4) ^ swizzle(j & 3)) * 16 ^ r.place) +
+                                                   (r0 + (j & 3) + 8 * (j >> 2)) * kChunks * 16);
             return f;
         }
     }
@@ -287,6 +290,22 @@ __device__ __forceinline__ void keep_sums(f32x16 (&x)[N])
 // Nothing moves across: what stands in front is issued in front.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
+// use(n, get(n)) for n = 0 .. N - 1 with `AHEAD` fragments on their way from LDS in front of the one that is used.
+template <int N, int AHEAD, typename Get, typename Use>
+__device__ __forceinline__ void ahead(Get get, Use use)
+{
+    constexpr int kRing = AHEAD + 1;
+    decltype(get(0)) f[kRing];
+#pragma unroll
+    for (int n = 0; n < AHEAD && n < N; ++n) f[n] = get(n);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n + AHEAD < N) f[(n + AHEAD) % kRing] = get(n + AHEAD);
+        in_order();
+        use(n, f[n % kRing]);
+    }
+}
+
 // Operands that were loaded in front of a loop have arrived: without this the compiler waits for them inside the loop,
 // and there for everything that is on its way from memory, at every step.
 template <typename F, int N>
@@ -339,8 +358,45 @@ struct Score {
     }
 };
 
-// of lane ^ 32
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// Sum and maximum over a lane and lane ^ 32: one instruction hands each half of the wavefront the other's.
+struct Halves {
+    float low, high;
+    __device__ __forceinline__ Halves(float x)
+    {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        low = __uint_as_float(r[0]);
+        high = __uint_as_float(r[1]);
+    }
+};
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const Halves h(x);
+    return h.low + h.high;
+}
+__device__ __forceinline__ float halves_max(float x)
+{
+    const Halves h(x);
+    return fmaxf(h.low, h.high);
+}
+
+// The running maximum of a softmax, in units of ln 2.  It follows the scores only where one passes it by more than kSlack: until
+// then probabilities may be up to 2^kSlack, which costs no accuracy (they are floating point, and the sum that
+// divides them has the same factor), and the sums need not be scaled.
+constexpr float kSlack = 8.0f;
+
+struct Maximum {
+    float m = -INFINITY;
+    __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }
+    // `top`: the largest of the new scores.  Whether some lane's maximum moved; then `f` is what each lane's sums shrink by.
+    __device__ __forceinline__ bool moves(float top, float& f)
+    {
+        if (!__any(top > m + kSlack)) return false;
+        const float up = fmaxf(m, top);
+        f = up == -INFINITY ? 1.0f : exp2_fast(m - up);
+        m = up;
+        return true;
+    }
+};
 
 __device__ __forceinline__ float wave_sum(float x)
 {

@@ -46,7 +46,7 @@ template <typename T, int DP, bool MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kParts = DP / 32;
+    constexpr int kSteps = DP / 16, kParts = DP / 32, kAhead = 1;      // fragments on their way from LDS
     __shared__ T ks[2][kKeys * DP], vs[2][kKeys * DP];
     __shared__ int hull[2][kThreads / kWave];
     const int lane = lane_id(), wave = wave_id();
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
         }
         lse = a.lse[((int64_t)b * a.Hq + head) * T_ + row] * kLog2e;
     }
-    delta += other_half(delta);
+    delta = halves_sum(delta);
     if (row < T_ && lane < 32) a.delta[((int64_t)b * a.Hq + head) * T_ + row] = delta;
     arrived(q);
     arrived(go);
@@ -132,10 +132,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
         for (int t = 0; t < kKeys / 32; ++t) {
             if (!range.meets(k0 + 32 * t, 32)) continue;
             f32x16 x = {}, y = {};
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks[buf], by_row, 32 * t, s), q[s], x);
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) y = mma(L::row_frag(vs[buf], by_row, 32 * t, s), go[s], y);
+            ahead<2 * kSteps, kAhead>([&](int n) { return n < kSteps ? L::row_frag(ks[buf], by_row, 32 * t, n) : L::row_frag(vs[buf], by_row, 32 * t, n - kSteps); },
+                                      [&](int n, frag8<T> f) {
+                                          if (n < kSteps) x = mma(f, q[n], x);
+                                          else y = mma(f, go[n - kSteps], y);
+                                      });
             const int key0 = k0 + 32 * t + 4 * (lane >> 5);
             if (!MOD && !range.full(k0 + 32 * t, 32)) {    // what is hidden gets probability 0
 #pragma unroll
@@ -156,12 +157,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                 }
                 x[i] *= (y[i] - delta) * keep;
             }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const frag8<T> p = pack8<T>(x, 8 * u);
-#pragma unroll
-                for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(ks[buf], by_col, 32 * t + 16 * u, 32 * d), p, o[d]);
-            }
+            ahead<2 * kParts, kAhead>([&](int n) { return L::col_frag(ks[buf], by_col, 32 * t + 16 * (n / kParts), 32 * (n % kParts)); },
+                                      [&](int n, frag8<T> f) { o[n % kParts] = mma(f, pack8<T>(x, 8 * (n / kParts)), o[n % kParts]); });
         }
     }
     bool bad = false;

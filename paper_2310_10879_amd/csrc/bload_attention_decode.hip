@@ -76,7 +76,8 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
-    float m = -INFINITY, l = 0.0f;
+    Maximum max;
+    float l = 0.0f;
 
     Stage<T, DP, kTileKeys, ODD, kWave> next_k(a.k.st, D), next_v(a.v.st, D);
     typename L::Reader by_row = L::rows(), by_col = L::columns();
@@ -103,8 +104,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
         by_row.renew();
         by_col.renew();
         f32x16 x = {};
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) x = mma(L::row_frag(ks, by_row, 0, s), q[s], x);
+        ahead<kSteps, 1>([&](int n) { return L::row_frag(ks, by_row, 0, n); }, [&](int n, frag8<T> f) { x = mma(f, q[n], x); });
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -113,30 +113,24 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
             x[i] = key < hi ? x[i] : -INFINITY;
             top = fmaxf(top, x[i]);
         }
-        top = fmaxf(top, other_half(top));
-        const float up = fmaxf(m, top * c), base = up == -INFINITY ? 0.0f : up;
-        const float f = exp2_fast(m - base);
-        m = up;
-        float sum = 0.0f;
+        float f, sum = 0.0f;
+        if (max.moves(halves_max(top) * c, f)) {
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < kParts; ++d) o[d] *= f;
+        }
+        const float base = max.base();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x[i] = exp2_fast(fmaf(x[i], c, -base));
             sum += x[i];
         }
-        l = l * f + sum;
-        if (__any(f != 1.0f)) {
-#pragma unroll
-            for (int d = 0; d < kParts; ++d) o[d] *= f;
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const frag8<T> w = pack8<T>(x, 8 * u);
-#pragma unroll
-            for (int d = 0; d < kParts; ++d) o[d] = mma(L::col_frag(vs, by_col, 16 * u, 32 * d), w, o[d]);
-        }
+        l += sum;
+        ahead<2 * kParts, 1>([&](int n) { return L::col_frag(vs, by_col, 16 * (n / kParts), 32 * (n % kParts)); },
+                             [&](int n, frag8<T> f) { o[n % kParts] = mma(f, pack8<T>(x, 8 * (n / kParts)), o[n % kParts]); });
         __builtin_amdgcn_wave_barrier();
     }
-    l += other_half(l);
+    l = halves_sum(l);
 
     // the wavefronts' parts to one
     __syncthreads();
@@ -151,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
             }
     }
     if (lane < 32) {
-        tops[wave][lane] = m;
+        tops[wave][lane] = max.m;
         sums[wave][lane] = l;
     }
     __syncthreads();

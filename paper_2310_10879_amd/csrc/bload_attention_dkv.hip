@@ -39,7 +39,7 @@ __device__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
 // share the keys, and are read by rows for the scores and by columns for dk and dv.  128 sums, 64 registers of operands and
 // the scores leave room for one wave a SIMD, which has to overlap its own work: the order of its instructions is written out.
 template <typename T, int DP, bool MOD, bool ODD>
-__global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(AttArgs a)
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attention_dkv_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
     constexpr int kSteps = DP / 16, kParts = DP / 32, kQueries = sizeof(T) == 2 ? 64 : 32;
@@ -114,8 +114,10 @@ __global__ __launch_bounds__(kThreads, 1) void attention_dkv_kernel(AttArgs a)
         load(q0);
     }
     for (int buf = 0; left > 0; buf ^= 1) {
-        keep_sums(dk);
-        keep_sums(dv);
+        if constexpr (!(sizeof(T) == 2 && DP <= 64)) {
+            keep_sums(dk);
+            keep_sums(dv);
+        }
         next_q.store(qs[buf]);
         next_g.store(gs[buf]);
         if (tid < 2 * kQueries) {
