@@ -11,7 +11,9 @@
 namespace bload {
 namespace {
 
-constexpr int kKeys = 64;              // keys of a tile
+// Keys of a tile: 64, of float 32, so that two workgroups share a CU (LDS and registers) and one multiplies while the other
+// waits at its barrier or forms probabilities.
+template <typename T> constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
 
 // One query again, key by key in plain 32-bit arithmetic.  The matrix product adds 0 * v for what the
 // mask hides, which is NaN where a hidden v is infinite or NaN; rows that come out not finite are
@@ -42,12 +44,13 @@ __device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 }
 
 // A workgroup takes 128 queries of one head, a wavefront 32 of them (they stay in its registers, as does O^T);
-// tiles of 64 keys and values go through LDS, two tiles deep, the next one on its way from memory
+// tiles of keys and values go through LDS, two tiles deep, the next one on its way from memory
 // while the present one is multiplied.
 template <typename T, int DP, bool MOD, bool ODD>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_forward_kernel(AttArgs a)
+__global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
+    constexpr int kKeys = kTileKeys<T>, kHalves = kKeys / 32;
     constexpr int kSteps = DP / 16, kParts = DP / 32, kAhead = sizeof(T) == 2 ? 3 : 1;      // fragments on their way from LDS
     __shared__ T ks[2][kKeys * DP], vs[2][kKeys * DP];
     __shared__ int hull[2][kThreads / kWave];
@@ -65,6 +68,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         const int4 r = a.mask[(int64_t)b * T_ + row];
         span = clamp_span(r.x, r.y, T_);
     }
+    frag8<T> q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = frag8<T>{};
+    if (row < T_) {
+        const T* p = att_at<T>(a.q, b, row, head);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = load_frag<T, ODD>(p, 16 * s + 8 * (lane >> 5), D);
+    }
     SpanRange range;
     range.of_wave(span);
     if (lane == 0) {
@@ -75,13 +86,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
     const int lo = min(min(hull[0][0], hull[0][1]), min(hull[0][2], hull[0][3]));
     const int hi = max(max(hull[1][0], hull[1][1]), max(hull[1][2], hull[1][3]));
 
-    frag8<T> q[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) q[s] = frag8<T>{};
-    if (row < T_) {
-        const T* p = att_at<T>(a.q, b, row, head);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[s] = load_frag(p, 16 * s + 8 * (lane >> 5), D);
+    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
+    if (lo < hi) {
+        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
+        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
+        next_k.load(lo, hi);
+        next_v.load(lo, hi);
     }
     arrived(q);
     const Score score(a, head);
@@ -93,17 +103,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
     Maximum max;
     float l = 0.0f;
 
-    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
-    if (lo < hi) {
-        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
-        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
-        next_k.load(lo, hi);
-        next_v.load(lo, hi);
-    }
     typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
-        if constexpr (sizeof(T) == 4) keep_sums(o);
         next_k.store(ks[buf]);
         next_v.store(vs[buf]);
         __syncthreads();
@@ -114,19 +116,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         by_row.renew();
         by_col.renew();
         if (!range.meets(k0, kKeys)) continue;
-        f32x16 x[2] = {{}, {}};
-        ahead<2 * kSteps, kAhead>([&](int n) { return L::row_frag(ks[buf], by_row, 32 * (n / kSteps), n % kSteps); },
+        f32x16 x[kHalves] = {};
+        ahead<kHalves * kSteps, kAhead>([&](int n) { return L::row_frag(ks[buf], by_row, 32 * (n / kSteps), n % kSteps); },
                                   [&](int n, frag8<T> f) { x[n / kSteps] = mma(f, q[n % kSteps], x[n / kSteps]); });
         const int key0 = k0 + 4 * (lane >> 5);
         if constexpr (MOD) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kHalves; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[t][i] = score.of<T>(x[t][i], row - (key0 + 32 * t + 8 * (i / 4) + i % 4), nullptr);
         }
         if (!range.full(k0, kKeys)) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < kHalves; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = key0 + 32 * t + 8 * (i / 4) + i % 4;
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
         }
         float top = x[0][0];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < kHalves; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[t][i]);
         float f, sum = 0.0f;
@@ -152,13 +154,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_fo
 #pragma unroll
         for (int i = 0; i < 16; ++i) probability(0, i);
         // the second half's probabilities between the products of the first
-        ahead<4 * kParts, kAhead>([&](int n) { return L::col_frag(vs[buf], by_col, 16 * (n / kParts), 32 * (n % kParts)); },
+        ahead<2 * kHalves * kParts, kAhead>([&](int n) { return L::col_frag(vs[buf], by_col, 16 * (n / kParts), 32 * (n % kParts)); },
                                   [&](int n, frag8<T> f) {
                                       const int t = n / kParts, d = n % kParts;
                                       o[d] = mma(f, pack8<T>(x[t >> 1], 8 * (t & 1)), o[d]);
-                                      if (n < 2 * kParts)
+                                      if (kHalves == 2 && n < 2 * kParts)
 #pragma unroll
-                                          for (int i = 8 * n / kParts; i < 8 * (n + 1) / kParts; ++i) probability(1, i);
+                                          for (int i = 8 * n / kParts; i < 8 * (n + 1) / kParts; ++i) probability(kHalves - 1, i);
                                   });
         l += sum;
     }

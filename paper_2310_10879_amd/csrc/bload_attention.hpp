@@ -73,15 +73,15 @@ __device__ __forceinline__ f32x16 mma(frag8<float> a, frag8<float> b, f32x16 c)
 template <typename T, int N>
 __device__ __forceinline__ void load_any(const T* p, T (&x)[N]) { __builtin_memcpy(&x, p, sizeof(x)); }
 
-// 16 bytes of a row of D elements from element d on; zeros beyond the row.
-template <typename T>
+// 16 bytes of a row of D elements from element d on; zeros beyond the row (which, unless ODD, is a whole number of them long).
+template <typename T, bool ODD>
 __device__ __forceinline__ vec16 load_chunk(const T* row, int d, int D)
 {
     constexpr int N = 16 / sizeof(T);
     vec16 r = {0, 0, 0, 0};
     if (d + N <= D) {
         __builtin_memcpy(&r, row + d, 16);
-    } else if (d < D) {
+    } else if (ODD && d < D) {
         T x[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = d + j < D ? row[d + j] : (T)0.0f;
@@ -91,13 +91,13 @@ __device__ __forceinline__ vec16 load_chunk(const T* row, int d, int D)
 }
 
 // A B fragment straight from memory: elements d .. d + 7 of a row; zeros beyond the row.
-template <typename T>
+template <typename T, bool ODD>
 __device__ __forceinline__ frag8<T> load_frag(const T* row, int d, int D)
 {
     frag8<T> f;
     vec16 c[sizeof(T) / 2];
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) c[i] = load_chunk(row, d + i * (16 / (int)sizeof(T)), D);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) c[i] = load_chunk<T, ODD>(row, d + i * (16 / (int)sizeof(T)), D);
     __builtin_memcpy(&f, &c, sizeof(f));
     return f;
 }

@@ -62,6 +62,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
         const int4 r = a.mask[(int64_t)b * T_ + row];
         span = clamp_span(r.x, r.y, T_);
     }
+    frag8<T> q[kSteps], go[kSteps], y[kSteps], z[kSteps];
+    float lse = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = go[s] = y[s] = z[s] = frag8<T>{};
+    if (row < T_) {
+        const T* pq = att_at<T>(a.q, b, row, head);
+        const T* pg = att_at<T>(a.dout, b, row, head);
+        const T* po = att_at<T>(a.out, b, row, head);
+        const T* pr = a.rest.p ? att_at<T>(a.rest, b, row, head) : nullptr;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = 16 * s + 8 * (lane >> 5);
+            q[s] = load_frag<T, ODD>(pq, d, D);
+            go[s] = load_frag<T, ODD>(pg, d, D);
+            y[s] = load_frag<T, ODD>(po, d, D);
+            if (pr) z[s] = load_frag<T, ODD>(pr, d, D);
+        }
+        lse = a.lse[((int64_t)b * a.Hq + head) * T_ + row] * kLog2e;
+    }
     SpanRange range;
     range.of_wave(span);
     if (lane == 0) {
@@ -72,32 +91,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     const int lo = min(min(hull[0][0], hull[0][1]), min(hull[0][2], hull[0][3]));
     const int hi = max(max(hull[1][0], hull[1][1]), max(hull[1][2], hull[1][3]));
 
-    frag8<T> q[kSteps], go[kSteps];
-    float delta = 0.0f, lse = 0.0f;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) q[s] = go[s] = frag8<T>{};
-    if (row < T_) {
-        const T* pq = att_at<T>(a.q, b, row, head);
-        const T* pg = att_at<T>(a.dout, b, row, head);
-        const T* po = att_at<T>(a.out, b, row, head);
-        const T* pr = a.rest.p ? att_at<T>(a.rest, b, row, head) : nullptr;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = 16 * s + 8 * (lane >> 5);
-            q[s] = load_frag(pq, d, D);
-            go[s] = load_frag(pg, d, D);
-            const frag8<T> y = load_frag(po, d, D);
-            if (pr) {
-                const frag8<T> z = load_frag(pr, d, D);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) delta += (float)go[s][j] * ((float)y[j] + (float)z[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) delta += (float)go[s][j] * (float)y[j];
-            }
-        }
-        lse = a.lse[((int64_t)b * a.Hq + head) * T_ + row] * kLog2e;
+    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
+    if (lo < hi) {
+        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
+        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
+        next_k.load(lo, hi);
+        next_v.load(lo, hi);
     }
+    float delta = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta += (float)go[s][j] * ((float)y[s][j] + (float)z[s][j]);
     delta = halves_sum(delta);
     if (row < T_ && lane < 32) a.delta[((int64_t)b * a.Hq + head) * T_ + row] = delta;
     arrived(q);
@@ -108,13 +113,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
-    Stage<T, DP, kKeys, ODD> next_k(a.k.st, D), next_v(a.v.st, D);
-    if (lo < hi) {
-        next_k.begin(att_at<T>(a.k, b, 0, kv), lo);
-        next_v.begin(att_at<T>(a.v, b, 0, kv), lo);
-        next_k.load(lo, hi);
-        next_v.load(lo, hi);
-    }
     typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     if (column < a.G && n > 0) {
         const T* pq = att_at<T>(a.q, seq, 0, head);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[s] = load_frag(pq, 16 * s + 8 * (lane >> 5), D);
+        for (int s = 0; s < kSteps; ++s) q[s] = load_frag<T, ODD>(pq, 16 * s + 8 * (lane >> 5), D);
     }
     arrived(q);
     const Score score(a, head);

@@ -59,6 +59,18 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
         const int4 r = a.mask[(int64_t)b * T_ + row];
         span = clamp_span(r.z, r.w, T_);
     }
+    frag8<T> k[kSteps], v[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) k[s] = v[s] = frag8<T>{};
+    if (row < T_) {
+        const T* pk = att_at<T>(a.k, b, row, kv);
+        const T* pv = att_at<T>(a.v, b, row, kv);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            k[s] = load_frag<T, ODD>(pk, 16 * s + 8 * (lane >> 5), D);
+            v[s] = load_frag<T, ODD>(pv, 16 * s + 8 * (lane >> 5), D);
+        }
+    }
     SpanRange range;
     range.of_wave(span);
     if (lane == 0) {
@@ -69,20 +81,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
     const int lo = min(min(hull[0][0], hull[0][1]), min(hull[0][2], hull[0][3]));
     const int hi = max(max(hull[1][0], hull[1][1]), max(hull[1][2], hull[1][3]));
 
-    frag8<T> k[kSteps], v[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) k[s] = v[s] = frag8<T>{};
-    if (row < T_) {
-        const T* pk = att_at<T>(a.k, b, row, kv);
-        const T* pv = att_at<T>(a.v, b, row, kv);
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            k[s] = load_frag(pk, 16 * s + 8 * (lane >> 5), D);
-            v[s] = load_frag(pv, 16 * s + 8 * (lane >> 5), D);
-        }
-    }
-    arrived(k);
-    arrived(v);
     f32x16 dk[kParts], dv[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) dk[d] = dv[d] = f32x16{};
@@ -113,6 +111,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
         begin();
         load(q0);
     }
+    arrived(k);
+    arrived(v);
     for (int buf = 0; left > 0; buf ^= 1) {
         if constexpr (!(sizeof(T) == 2 && DP <= 64)) {
             keep_sums(dk);
