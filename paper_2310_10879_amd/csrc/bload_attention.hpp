@@ -119,16 +119,19 @@ __device__ __forceinline__ void store4(T* row, int d, int D, f32x4 x)
 }
 
 // Rows of DP elements in LDS, in chunks of 16 bytes.  A chunk's place in its row is XORed with a
-// number of the row, such that neither eight rows at one chunk (row_frag) nor four rows at four
-// chunks (col_frag) meet in one bank.
+// number of the row, such that neither the rows of 16 lanes at one chunk (row_frag; of 16-bit types, whose rows are read most) nor
+// four rows at four chunks (col_frag) meet in one bank.  The number is linear: that of a XOR b is that of a XOR that of b.
 template <typename T, int DP>
 struct Tile {
     static constexpr int kElems = 16 / (int)sizeof(T);
     static constexpr int kChunks = DP / kElems;
+    static constexpr bool kByEight = sizeof(T) == 2 && (kChunks == 16 || kChunks == 8);      // rows 8 apart lie differently
 
     __device__ static __forceinline__ int swizzle(int row)
     {
-        if constexpr (kChunks == 16) return ((row & 1) << 2) | ((row & 2) << 2) | ((row >> 1) & 1) | ((row >> 1) & 2);
+        if constexpr (kByEight && kChunks == 16) return ((row & 3) << 2) | ((row & 4) >> 1) | ((row & 8) >> 3);
+        else if constexpr (kByEight) return ((row & 2) << 1) | ((row & 4) >> 1) | ((row & 8) >> 3);
+        else if constexpr (kChunks == 16) return ((row & 1) << 2) | ((row & 2) << 2) | ((row >> 1) & 1) | ((row >> 1) & 2);
         else if constexpr (kChunks == 8) return ((row & 1) << 2) | ((row >> 1) & 3);
         else if constexpr (kChunks == 24 || kChunks == 32) return row & 7;
         else return (row >> 1) & 3;
@@ -180,7 +183,7 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 x[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_ptr)(reinterpret_cast<const char*>(tile) + r.off + ((d0 / kElems * 16) ^ r.place) + (r0 + 8 * i) * kChunks * 16));
+                    (lds_ptr)(reinterpret_cast<const char*>(tile) + r.off + (((d0 / kElems + (kByEight ? i : 0)) * 16) ^ r.place) + (r0 + 8 * i) * kChunks * 16));
             frag8<T> f;
             __builtin_memcpy(&f, &x, sizeof(f));
             return f;
@@ -265,14 +268,18 @@ struct Stage {
         __builtin_memcpy(&v, &y, 16);
         return v;
     }
+    __device__ __forceinline__ void put(T* tile, int i, vec16 y) const { __builtin_memcpy(tile + L::at(row + i * kRows, place), &y, 16); }
     __device__ __forceinline__ void store(T* tile) const
     {
         if (kWide != L::kChunks && place >= L::kChunks) return;
         if (kRows > R && (int)threadIdx.x % THREADS / kWide >= R) return;
+        if (D == DP) {
+            asm volatile("");                              // (a branch: by selection instead it costs every 16 bytes four of them)
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const vec16 y = D == DP ? x[i] : whole(x[i]);
-            __builtin_memcpy(tile + L::at(row + i * kRows, place), &y, 16);
+            for (int i = 0; i < kEach; ++i) put(tile, i, x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) put(tile, i, whole(x[i]));
         }
     }
 };
