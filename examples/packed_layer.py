@@ -1,0 +1,172 @@
+"""A sequence model's layer on packed blocks, from ragged recordings to a served frame.
+
+    python examples/packed_layer.py [steps]
+
+Recordings of unequal length are planned and packed into blocks; a layer of rotary positions, attention inside the
+sequences and a gated recurrence learns to say each recording's next frame; then every recording's last frame is
+answered again as a stream would ask for it: one query over the cached keys and values, one step of the recurrence from
+the state in front of it.  Neither a neighbour in the block nor padding reaches a recording on any of these ways.
+"""
+from __future__ import annotations
+
+import math
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+from paper_2310_10879_amd import bload  # noqa: E402
+
+
+class Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, positions, frequencies):
+        ctx.save_for_backward(positions, frequencies)
+        return bload.bload_rotary(x, positions, frequencies)
+
+    @staticmethod
+    def backward(ctx, dout):
+        return bload.bload_rotary(dout, *ctx.saved_tensors, inverse=True), None, None
+
+
+class SegmentAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, mask):
+        out, ctx.kept = bload.bload_segment_attention(q, k, v, mask, training=True)
+        ctx.save_for_backward(q, k, v, out, mask)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, mask = ctx.saved_tensors
+        return (*bload.bload_segment_attention_backward(dout, q, k, v, out, ctx.kept, mask), None)
+
+
+class GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate, x, reset, valid):
+        h, _ = bload.bload_gated_scan(gate, x, reset, valid)
+        ctx.save_for_backward(gate, h, reset, valid)
+        return h
+
+    @staticmethod
+    def backward(ctx, dout):
+        gate, h, reset, valid = ctx.saved_tensors
+        dgate, dx, _ = bload.bload_gated_scan_backward(dout.contiguous(), gate, h, reset, valid)
+        return dgate, dx, None, None
+
+
+class Batch:
+    """Recordings (float [frames, feat], one behind the other) in blocks, with what every layer reads of the start table."""
+
+    def __init__(self, frames: torch.Tensor, lengths: torch.Tensor, t_blk: int, seed: int):
+        feat = frames.shape[1]
+        self.lengths = lengths
+        self.plan = bload.bload_plan(lengths, t_blk, seed)
+        first = torch.cumsum(lengths.long(), 0) - lengths
+        packed = bload.bload_pack(frames.view(torch.uint8), torch.cat([first, first[-1:] + lengths[-1:]]), lengths, self.plan,
+                                  feat * frames.element_size())
+        self.x = packed.packed.view(frames.dtype).view(self.plan.num_blocks, t_blk, feat)
+        self.positions, self.reset, self.valid = packed.frame_idx, packed.reset, packed.valid
+        self.mask = bload.bload_segment_mask(self.reset, self.valid)
+
+
+class Layer:
+    def __init__(self, feat: int, heads_q: int, heads_kv: int, head_dim: int, dtype: torch.dtype, device, seed: int = 0):
+        g = torch.Generator(device=device).manual_seed(seed)
+
+        def weight(rows, columns):
+            w = torch.empty((rows, columns), device=device).normal_(std=rows ** -0.5, generator=g)
+            return w.to(dtype).requires_grad_()
+        self.heads_q, self.heads_kv, self.head_dim = heads_q, heads_kv, head_dim
+        self.qkv = weight(feat, (heads_q + 2 * heads_kv) * head_dim)
+        self.mix = weight(heads_q * head_dim, feat)
+        self.gate = weight(feat, feat)
+        self.say = weight(feat, feat)
+        self.weights = [self.qkv, self.mix, self.gate, self.say]
+        self.frequencies = bload.bload_rotary_frequencies(head_dim).to(device)
+
+    def project(self, x, positions):
+        """Rotated queries and keys, and values: [B, T, heads, head_dim] each."""
+        B, T, _ = x.shape
+        qkv = (x @ self.qkv).view(B, T, -1, self.head_dim)
+        turned = Rotary.apply(qkv[:, :, :self.heads_q + self.heads_kv], positions, self.frequencies)
+        return turned[:, :, :self.heads_q], turned[:, :, self.heads_q:], qkv[:, :, self.heads_q + self.heads_kv:]
+
+    def gates(self, x):
+        return torch.sigmoid((x @ self.gate).float() + 1.0).to(x.dtype)
+
+    def forward(self, b: Batch):
+        """The next frame of every slot, and what a stream goes on from: keys, values and states."""
+        q, k, v = self.project(b.x, b.positions)
+        seen = SegmentAttention.apply(q, k, v, b.mask)
+        h = GatedScan.apply(self.gates(b.x), seen.flatten(2) @ self.mix, b.reset, b.valid)
+        return h @ self.say, (k, v, h)
+
+    @torch.no_grad()
+    def last_frames(self, b: Batch, k, v, states):
+        """The same answer for the last frame of every recording, asked one frame at a time: k and v as the cache,
+        states [n_seq, feat] (float32) of the frames in front."""
+        at = last_slots(b)
+        x, position = b.x.flatten(0, 1)[at][:, None], b.positions.flatten()[at][:, None]
+        q, _, _ = self.project(x, position)
+        seen = bload.bload_segment_attention_decode(q[:, 0], k, v, b.plan.block_of_seq, b.plan.offset_of_seq, b.lengths)
+        fresh = (b.lengths == 1).to(torch.uint8)[:, None]                # nothing in front of it
+        h, _ = bload.bload_gated_scan(self.gates(x), (seen.flatten(1) @ self.mix)[:, None], fresh, torch.ones_like(fresh), h0=states)
+        return h[:, 0] @ self.say
+
+
+def last_slots(b: Batch) -> torch.Tensor:
+    return b.plan.block_of_seq.long() * b.plan.t_blk + b.plan.offset_of_seq + b.lengths - 1
+
+
+def recordings(n: int, longest: int, feat: int, dtype: torch.dtype, device, seed: int = 0):
+    """n recordings of 1 .. longest frames: slow oscillations, so that the next frame can be learnt."""
+    g = torch.Generator().manual_seed(seed)
+    lengths = torch.randint(1, longest + 1, (n,), generator=g, dtype=torch.int32)
+    pitch, phase = 0.05 + 0.4 * torch.rand((n, 1, feat), generator=g), 2 * math.pi * torch.rand((n, 1, feat), generator=g)
+    all_of = torch.sin(torch.arange(longest)[None, :, None] * pitch + phase)
+    frames = torch.cat([all_of[i, :m] for i, m in enumerate(lengths.tolist())])
+    return frames.to(dtype).to(device), lengths.to(device)
+
+
+def train(steps: int = 60, n: int = 200, t_blk: int = 256, feat: int = 64, dtype: torch.dtype = torch.bfloat16, rate: float = 3e-3):
+    """Losses of the steps, and the served answers beside the layer's own."""
+    device = torch.device("cuda")
+    frames, lengths = recordings(n, t_blk, feat, dtype, device)
+    layer = Layer(feat, 4, 2, 32, dtype, device)
+    master = [w.detach().float().requires_grad_() for w in layer.weights]        # in 32 bits, as the update is small
+    adam = torch.optim.Adam(master, lr=rate)
+    losses = []
+    for step in range(steps):
+        b = Batch(frames, lengths, t_blk, seed=step)                             # another order of the blocks every time
+        said, _ = layer.forward(b)
+        goes_on = (b.valid[:, 1:] == 1) & (b.reset[:, 1:] == 0)
+        off = (said[:, :-1].float() - b.x[:, 1:].float())[goes_on]
+        loss = off.square().mean()
+        for w in layer.weights:
+            w.grad = None
+        loss.backward()
+        with torch.no_grad():
+            for m, w in zip(master, layer.weights):
+                m.grad = w.grad.float()
+        adam.step()
+        with torch.no_grad():
+            for m, w in zip(master, layer.weights):
+                w.copy_(m)
+        losses.append(loss.detach())
+    with torch.no_grad():
+        said, (k, v, h) = layer.forward(b)
+        at = last_slots(b)
+        states = h.flatten(0, 1)[(at - 1).clamp(min=0)].float()
+        return [float(x) for x in losses], layer.last_frames(b, k, v, states), said.flatten(0, 1)[at]
+
+
+if __name__ == "__main__":
+    losses, served, packed = train(int(sys.argv[1]) if len(sys.argv) > 1 else 60)
+    for i in range(0, len(losses), 10):
+        print(f"step {i:4d}  loss {losses[i]:.4f}")
+    print(f"step {len(losses) - 1:4d}  loss {losses[-1]:.4f}")
+    print(f"last frames, served against packed: off by {float((served.float() - packed.float()).abs().max()):.4f} "
+          f"of {float(packed.float().abs().max()):.4f}")
