@@ -23,13 +23,13 @@ __device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 {
     const int D = a.D, kv = head / a.G;
     const Score score(a, head);
-    float q[2], acc[2] = {0.0f, 0.0f}, m = -INFINITY, l = 0.0f;
+    float q[2], acc[2] = {0.0f, 0.0f}, m = -INFINITY, l = 0.0f, keep;
     load_row2(att_at<T>(a.q, b, i, head), D, q);
     for (int j = span.lo; j < span.hi; ++j) {
         float k[2], v[2];
         load_row2(att_at<T>(a.k, b, j, kv), D, k);
         load_row2(att_at<T>(a.v, b, j, kv), D, v);
-        const float s = score.of<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, nullptr);
+        const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
         const float up = fmaxf(m, s), base = up == -INFINITY ? 0.0f : up;
         const float f = exp2_fast(m - base), p = exp2_fast(s - base);
         m = up;
@@ -46,7 +46,7 @@ __device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 // A workgroup takes 128 queries of one head, a wavefront 32 of them (they stay in its registers, as does O^T);
 // tiles of keys and values go through LDS, two tiles deep, the next one on its way from memory
 // while the present one is multiplied.
-template <typename T, int DP, bool MOD, bool ODD>
+template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs 
     }
     arrived(q);
     const Score score(a, head);
-    const float c = MOD ? 1.0f : a.scale * kLog2e;
+    const float c = MOD != kPlain ? 1.0f : a.scale * kLog2e;
 
     f32x16 o[kParts];
 #pragma unroll
@@ -120,20 +120,19 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs 
         ahead<kHalves * kSteps, kAhead>([&](int n) { return L::row_frag(ks[buf], by_row, 32 * (n / kSteps), n % kSteps); },
                                   [&](int n, frag8<T> f) { x[n / kSteps] = mma(f, q[n % kSteps], x[n / kSteps]); });
         const int key0 = k0 + 4 * (lane >> 5);
-        if constexpr (MOD) {
+        if constexpr (MOD != kPlain) {
+            const float away = (float)(row - key0);
+            float keep;
 #pragma unroll
             for (int t = 0; t < kHalves; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[t][i] = score.of<T>(x[t][i], row - (key0 + 32 * t + 8 * (i / 4) + i % 4), nullptr);
+                for (int i = 0; i < 16; ++i) x[t][i] = score.of<T, MOD>(x[t][i], away - (32 * t + result_row(i)), keep);
         }
         if (!range.full(k0, kKeys)) {
 #pragma unroll
             for (int t = 0; t < kHalves; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = key0 + 32 * t + 8 * (i / 4) + i % 4;
-                    x[t][i] = key >= span.lo && key < span.hi ? x[t][i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) x[t][i] = span.has(key0 + 32 * t + result_row(i)) ? x[t][i] : -INFINITY;
         }
         float top = x[0][0];
 #pragma unroll

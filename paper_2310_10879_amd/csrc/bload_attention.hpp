@@ -335,35 +335,40 @@ __device__ __forceinline__ frag8<T> pack8(const f32x16& x, int from)
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh: for 16-bit types 1 - 2 / (1 + e^2x), whose absolute error of some 1e-7 is far below what the
-// rounded inputs leave of a score; for float the library's.
-template <typename T>
-__device__ __forceinline__ float cap_tanh(float x)
-{
-    if constexpr (sizeof(T) == 2) return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + exp2_fast(2.0f * kLog2e * x));
-    else return tanhf(x);
-}
+// What a kernel does to the products of queries and keys, compiled in: the bias by distance costs two instructions a score, the cap
+// six and two transcendental ones, and a branch on either in the loop would keep the compiler from laying scores among products.
+enum { kPlain = 0, kBias = 1, kCap = 2 };                  // kCap: with the bias, of slope 0 where there is none
 
 // A raw product q.k as a score in units of ln 2: cap tanh(scale q.k / cap) - slope |i - j|.
 struct Score {
-    float scale, cap, inv_cap, slope;
+    float scale, inner, outer, slope;                      // all but `inner` in units of ln 2; outer: 0 without a cap
     __device__ __forceinline__ Score(const AttArgs& a, int head)
-        : scale(a.scale), cap(a.cap), inv_cap(a.cap > 0.0f ? a.scale / a.cap : 0.0f), slope(a.slopes ? a.slopes[head] : 0.0f) {}
-    // `keep` (may be null): the derivative of the capped score by the scaled one
-    template <typename T>
-    __device__ __forceinline__ float of(float qk, int distance, float* keep) const
+        : scale(a.scale * kLog2e), inner(a.cap > 0.0f ? a.scale / a.cap : 0.0f), outer(a.cap * kLog2e),
+          slope(a.slopes ? a.slopes[head] * kLog2e : 0.0f) {}
+    // `keep`: the derivative of the capped score by the scaled one.  tanh: for 16-bit types 1 - 2 / (1 + e^2x), whose absolute error of
+    // some 1e-7 is far below what the rounded inputs leave of a score; for float the library's.
+    template <typename T, int MOD>
+    __device__ __forceinline__ float of(float qk, float distance, float& keep) const
     {
-        float s = qk * scale;
-        if (cap > 0.0f) {
-            const float t = cap_tanh<T>(qk * inv_cap);
-            s = cap * t;
-            if (keep) *keep = 1.0f - t * t;
-        } else if (keep) {
-            *keep = 1.0f;
-        }
-        return (s - slope * fabsf((float)distance)) * kLog2e;
+        keep = 1.0f;
+        if constexpr (MOD == kPlain) return qk * scale;
+        if constexpr (MOD == kBias) return fmaf(-slope, fabsf(distance), qk * scale);
+        float t;
+        if constexpr (sizeof(T) == 2) t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + exp2_fast(qk * (inner * (2.0f * kLog2e))));
+        else t = tanhf(qk * inner);
+        keep = 1.0f - t * t;
+        return fmaf(-slope, fabsf(distance), outer * t);
+    }
+    // as the arguments say
+    template <typename T>
+    __device__ __forceinline__ float any(float qk, int distance, float& keep) const
+    {
+        return outer > 0.0f ? of<T, kCap>(qk, (float)distance, keep) : of<T, kBias>(qk, (float)distance, keep);
     }
 };
+
+// Row n (0 .. 15) of a result, beside the lane's first.
+__device__ __forceinline__ constexpr int result_row(int n) { return 8 * (n / 4) + n % 4; }
 
 // Sum and maximum over a lane and lane ^ 32: one instruction hands each half of the wavefront the other's.
 struct Halves {
@@ -427,6 +432,7 @@ __device__ __forceinline__ int wave_max(int x)
 // What one lane's row may look at, inside [0, T); an empty interval is [0, 0).
 struct Span {
     int lo, hi;
+    __device__ __forceinline__ bool has(int at) const { return (uint32_t)(at - lo) < (uint32_t)(hi - lo); }
 };
 __device__ __forceinline__ Span clamp_span(int lo, int hi, int T)
 {

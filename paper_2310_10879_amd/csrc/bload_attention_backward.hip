@@ -31,7 +31,7 @@ __device__ void dq_row(const AttArgs& a, int b, int head, int i, Span span)
         float k[2], v[2], keep;
         load_row2(att_at<T>(a.k, b, j, kv), D, k);
         load_row2(att_at<T>(a.v, b, j, kv), D, v);
-        const float s = score.of<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, &keep);
+        const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
         const float ds = exp2_fast(s - lse) * (wave_sum(g[0] * v[0] + g[1] * v[1]) - delta) * keep;
         acc[0] += ds * k[0];
         acc[1] += ds * k[1];
@@ -42,7 +42,7 @@ __device__ void dq_row(const AttArgs& a, int b, int head, int i, Span span)
 // A workgroup takes 128 queries of one head, a wavefront 32: q and do stay in registers as B fragments, dq^T as
 // the result; keys and values stream through LDS as in the forward kernel, the keys read by rows
 // (for the scores) and by columns (for dq).
-template <typename T, int DP, bool MOD, bool ODD>
+template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
@@ -136,24 +136,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                                           else y = mma(f, go[n - kSteps], y);
                                       });
             const int key0 = k0 + 32 * t + 4 * (lane >> 5);
-            if (!MOD && !range.full(k0 + 32 * t, 32)) {    // what is hidden gets probability 0
+            if (MOD == kPlain && !range.full(k0 + 32 * t, 32)) {       // what is hidden gets probability 0
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = key0 + 8 * (i / 4) + i % 4;
-                    x[i] = key >= span.lo && key < span.hi ? x[i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) x[i] = span.has(key0 + result_row(i)) ? x[i] : -INFINITY;
             }
+            const float away = (float)(row - key0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float keep = 1.0f;
-                if constexpr (MOD) {                       // (a cap makes a finite score of -infinity: hidden here)
-                    const int key = key0 + 8 * (i / 4) + i % 4;
-                    const float s = score.of<T>(x[i], row - key, &keep);
-                    x[i] = key >= span.lo && key < span.hi ? exp2_fast(s - lse) : 0.0f;
+                y[i] -= delta;
+                if constexpr (MOD != kPlain) {                 // (a cap makes a finite score of -infinity: hidden here, in any tile)
+                    float keep;
+                    const float s = score.of<T, MOD>(x[i], away - result_row(i), keep) - lse;
+                    x[i] = exp2_fast(span.has(key0 + result_row(i)) ? s : -INFINITY);
+                    if constexpr (MOD == kCap) y[i] *= keep;
                 } else {
                     x[i] = exp2_fast(fmaf(x[i], c, -lse));
                 }
-                x[i] *= (y[i] - delta) * keep;
+                x[i] *= y[i];
             }
             ahead<2 * kParts, kAhead>([&](int n) { return L::col_frag(ks[buf], by_col, 32 * t + 16 * (n / kParts), 32 * (n % kParts)); },
                                       [&](int n, frag8<T> f) { o[n % kParts] = mma(f, pack8<T>(x, 8 * (n / kParts)), o[n % kParts]); });

@@ -34,7 +34,7 @@ __device__ __forceinline__ int decode_length(const DecodeArgs& p, int64_t seq, i
 }
 
 // One share of one sequence for up to 32 heads of queries.
-template <typename T, int DP, bool MOD, bool ODD>
+template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p)
 {
     using L = Tile<T, DP>;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     }
     arrived(q);
     const Score score(a, head);
-    const float c = MOD ? 1.0f : a.scale * kLog2e;
+    const float c = MOD != kPlain ? 1.0f : a.scale * kLog2e;
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
@@ -108,8 +108,9 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int key = k0 + 4 * (lane >> 5) + 8 * (i / 4) + i % 4;
-            if constexpr (MOD) x[i] = score.of<T>(x[i], n - 1 - key, nullptr);
+            const int key = k0 + 4 * (lane >> 5) + result_row(i);
+            float keep;
+            if constexpr (MOD != kPlain) x[i] = score.of<T, MOD>(x[i], (float)(n - 1 - key), keep);
             x[i] = key < hi ? x[i] : -INFINITY;
             top = fmaxf(top, x[i]);
         }

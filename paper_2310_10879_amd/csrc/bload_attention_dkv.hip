@@ -21,7 +21,7 @@ __device__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
             float q[2], go[2], keep;
             load_row2(att_at<T>(a.q, b, i, head), D, q);
             load_row2(att_at<T>(a.dout, b, i, head), D, go);
-            const float s = score.of<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, &keep);
+            const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
             const float p = exp2_fast(s - a.lse[at + i] * kLog2e);
             const float ds = p * (wave_sum(go[0] * v[0] + go[1] * v[1]) - a.delta[at + i]) * keep;
             for (int n = 0; n < 2; ++n) {
@@ -38,7 +38,7 @@ __device__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
 // dv^T as results; tiles of 64 queries (float: 32) with their do stream through LDS, head after head of those that
 // share the keys, and are read by rows for the scores and by columns for dk and dv.  128 sums, 64 registers of operands and
 // the scores leave room for one wave a SIMD, which has to overlap its own work: the order of its instructions is written out.
-template <typename T, int DP, bool MOD, bool ODD>
+template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attention_dkv_kernel(AttArgs a)
 {
     using L = Tile<T, DP>;
@@ -165,12 +165,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
                 __builtin_memcpy(&lse[i], &sums[buf][0][32 * t + 8 * i + 4 * (lane >> 5)], 16);
                 __builtin_memcpy(&delta[i], &sums[buf][1][32 * t + 8 * i + 4 * (lane >> 5)], 16);
             }
-            if (!MOD && !range.full(q32, 32)) {        // what does not see the key gets probability 0
+            const int query0 = q32 + 4 * (lane >> 5);
+            if (MOD == kPlain && !range.full(q32, 32)) {       // what does not see the key gets probability 0
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int query = q32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                    x[i] = query >= span.lo && query < span.hi ? x[i] : -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i) x[i] = span.has(query0 + result_row(i)) ? x[i] : -INFINITY;
             }
             in_order();
             frag8<T> cq[2][kParts], cg[2][kParts];
@@ -179,17 +177,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
                 else cq[u][d - kParts] = L::col_frag(tq, by_col, 16 * u, 32 * (d - kParts));
             };
             float keep[16];
+            const float away = (float)(query0 - row);
             auto probability = [&](int i) {
-                keep[i] = 1.0f;
-                if constexpr (MOD) {                           // (a cap makes a finite score of -infinity: hidden here)
-                    const int query = q32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                    const float s = score.of<T>(x[i], query - row, &keep[i]);
-                    x[i] = query >= span.lo && query < span.hi ? exp2_fast(s - lse[i / 4][i % 4]) : 0.0f;
+                if constexpr (MOD != kPlain) {                 // (a cap makes a finite score of -infinity: hidden here, in any tile)
+                    const float s = score.of<T, MOD>(x[i], away + result_row(i), keep[i]) - lse[i / 4][i % 4];
+                    x[i] = exp2_fast(span.has(query0 + result_row(i)) ? s : -INFINITY);
                 } else {
                     x[i] = exp2_fast(fmaf(x[i], c, -lse[i / 4][i % 4]));
                 }
             };
-            auto slope = [&](int i) { y[i] = x[i] * (y[i] - delta[i / 4][i % 4]) * keep[i]; };      // ds / scale
+            auto slope = [&](int i) {                          // ds / scale
+                y[i] = x[i] * (y[i] - delta[i / 4][i % 4]);
+                if constexpr (MOD == kCap) y[i] *= keep[i];
+            };
 #pragma unroll
             for (int n = 0; n < kSteps; ++n) {
                 y = mma(f[(n + kSteps) % kAhead], v[n], y);

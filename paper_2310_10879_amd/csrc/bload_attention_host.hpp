@@ -69,14 +69,23 @@ inline void att_dispatch(bload_dtype dtype, int32_t D, F f)
     else att_dispatch_dim<float>(D, f);
 }
 
-// A kernel's variant: with the cap and the slopes compiled in, and for heads that are no whole number of 16 bytes (which come
-// with cap and slopes only, to be looked at as the kernel runs: fewer instances of what loads slowly anyway).
+// A kernel's variant: what it does to scores, and for heads that are no whole number of 16 bytes (which come with a bias at least,
+// of slope 0 if need be: fewer instances of what loads slowly anyway).
 template <typename T, typename F>
 inline void att_variant(const AttArgs& a, F f)
 {
-    if (a.D % (16 / (int)sizeof(T))) f(std::true_type(), std::true_type());
-    else if (a.cap > 0.0f || a.slopes) f(std::true_type(), std::false_type());
-    else f(std::false_type(), std::false_type());
+    using bias = std::integral_constant<int, kBias>;
+    using cap = std::integral_constant<int, kCap>;
+    if (a.D % (16 / (int)sizeof(T))) {
+        if (a.cap > 0.0f) f(cap(), std::true_type());
+        else f(bias(), std::true_type());
+    } else if (a.cap > 0.0f) {
+        f(cap(), std::false_type());
+    } else if (a.slopes) {
+        f(bias(), std::false_type());
+    } else {
+        f(std::integral_constant<int, kPlain>(), std::false_type());
+    }
 }
 
 }  // namespace bload
