@@ -461,21 +461,25 @@ def bload_pack_tile_bytes(n_seq: int, num_blocks: int, t_blk: int, frame_bytes: 
 
 
 def _heads(t: torch.Tensor, shape, dtype, name: str) -> Heads:
-    """A tensor [B, T, heads, D] of any strides with the elements of a head side by side."""
+    """A tensor [B, T, heads, D] (or [n, heads, D]) of any strides with the elements of a head side by side."""
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a device tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    sb, st, sh, sd = t.stride()
-    if sd != 1 and shape[3] > 1:
+    stride = t.stride()
+    if stride[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the elements of a head have to lie side by side")
-    return Heads(t.data_ptr(), sb, st, sh)
+    return Heads(t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0, stride[-2])
 
 
 def _sized(t: torch.Tensor | None, numel: int, dtype, name: str) -> int:
-    if t is not None and t.numel() != numel:
+    if t is None:
+        return 0
+    if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()                        # (the checks below at half their price: small calls are all host time)
+    if t.numel() != numel:
         raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
     return _ptr(t, dtype)
 
@@ -526,11 +530,10 @@ def bload_segment_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, m
     shape = (B, T, Hkv, D)
     hq, hk, hv = _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v")
     if out is None:
-        out = torch.empty((B, T, Hq, D), dtype=dtype, device=q.device)
+        out = q.new_empty((B, T, Hq, D))
     saved = hr = None
     if training:
-        saved = Saved(torch.empty((B, Hq, T), dtype=torch.float32, device=q.device),
-                      None if dtype == torch.float32 else torch.empty((B, T, Hq, D), dtype=dtype, device=q.device))
+        saved = Saved(q.new_empty((B, Hq, T), dtype=torch.float32), None if dtype == torch.float32 else q.new_empty((B, T, Hq, D)))
         hr = None if saved.rest is None else _heads(saved.rest, q.shape, dtype, "rest")
     _check(_lib.bload_segment_attention(hq, hk, hv, _sized(mask, B * T * 4, torch.int32, "mask"), B, T, Hq, Hkv, D, code,
                                         D ** -0.5 if scale is None else scale, cap, _sized(slopes, Hq, torch.float32, "slopes"),
@@ -552,7 +555,7 @@ def bload_segment_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: tor
     code = _type_code(q)
     shape = (B, T, Hkv, D)
     if grads is None:
-        grads = tuple(torch.empty((B, T, h, D), dtype=dtype, device=q.device) for h in (Hq, Hkv, Hkv))
+        grads = q.new_empty((B, T, Hq, D)), q.new_empty((B, T, Hkv, D)), q.new_empty((B, T, Hkv, D))
     dq, dk, dv = grads
     if workspace is None:
         workspace = torch.empty(max(16, bload_segment_attention_backward_workspace_bytes(B, T, Hq)), dtype=torch.uint8, device=q.device)
@@ -582,16 +585,16 @@ def bload_segment_attention_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Te
     dtype = q.dtype
     code = _type_code(q)
     if out is None:
-        out = torch.empty((n, Hq, D), dtype=dtype, device=q.device)
+        out = q.new_empty((n, Hq, D))
     if workspace is None:
         need = bload_segment_attention_decode_workspace_bytes(n, T, Hq, Hkv, D)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    shape, flat = (B, T, Hkv, D), (n, 1, Hq, D)
+    shape = (B, T, Hkv, D)
     _check(_lib.bload_segment_attention_decode(
-        _heads(q.unsqueeze(1), flat, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
+        _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
         _sized(block_of_seq, n, torch.int32, "block_of_seq"), _sized(offset_of_seq, n, torch.int32, "offset_of_seq"),
         _sized(lengths, n, torch.int32, "lengths"), n, B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
-        _sized(slopes, Hq, torch.float32, "slopes"), _heads(out.unsqueeze(1), flat, dtype, "out"), _ptr(workspace), _room(workspace),
+        _sized(slopes, Hq, torch.float32, "slopes"), _heads(out, q.shape, dtype, "out"), _ptr(workspace), _room(workspace),
         _stream()))
     return out
 
@@ -615,9 +618,9 @@ def bload_gated_scan(gate: torch.Tensor, x: torch.Tensor, reset: torch.Tensor, v
     B, T, D = x.shape
     dtype, code, n = x.dtype, _type_code(x), x.numel()
     if out is None:
-        out = torch.empty((B, T, D), dtype=dtype, device=x.device)
+        out = x.new_empty((B, T, D))
     if state is None:
-        state = torch.empty((B, D), dtype=torch.float32, device=x.device)
+        state = x.new_empty((B, D), dtype=torch.float32)
     workspace = _gated_workspace(workspace, B, T, D, code, x.device)
     _check(_lib.bload_gated_scan(_sized(gate, n, dtype, "gate"), _ptr(x), _sized(reset, B * T, torch.uint8, "reset"),
                                  _sized(valid, B * T, torch.uint8, "valid"), B, T, D, code, _sized(h0, B * D, torch.float32, "h0"),
@@ -634,8 +637,7 @@ def bload_gated_scan_backward(dout: torch.Tensor, gate: torch.Tensor, out: torch
     B, T, D = dout.shape
     dtype, code, n = dout.dtype, _type_code(dout), dout.numel()
     if grads is None:
-        grads = (torch.empty((B, T, D), dtype=dtype, device=dout.device), torch.empty((B, T, D), dtype=dtype, device=dout.device),
-                 torch.empty((B, D), dtype=torch.float32, device=dout.device))
+        grads = dout.new_empty((B, T, D)), dout.new_empty((B, T, D)), dout.new_empty((B, D), dtype=torch.float32)
     dgate, dx, dh0 = grads
     workspace = _gated_workspace(workspace, B, T, D, code, dout.device)
     _check(_lib.bload_gated_scan_backward(_ptr(dout), _sized(gate, n, dtype, "gate"), _sized(out, n, dtype, "out"),
@@ -664,7 +666,7 @@ def bload_rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Te
     B, T, H, D = x.shape
     code = _type_code(x)
     if out is None:
-        out = torch.empty((B, T, H, D), dtype=x.dtype, device=x.device)
+        out = x.new_empty((B, T, H, D))
     _check(_lib.bload_rotary(_heads(x, x.shape, x.dtype, "x"), _sized(positions, B * T, torch.int32, "positions"), B, T, H, D, code,
                              _ptr(frequencies, torch.float32), 2 * frequencies.shape[0], ROTARY_LAYOUTS[layout], scale, int(inverse),
                              _heads(out, x.shape, x.dtype, "out"), _stream()))
