@@ -496,7 +496,8 @@ bload_status bload_gated_scan(const void* d_gate, const void* d_x, const uint8_t
 /* Gradients of sum(out * dout) + sum(state_out * dstate_out) by gate, x and state_in.
  * d_out, d_state_in  in   of the forward pass;  d_dstate_out  in  float32[B, feat_dim] or NULL
  * d_dgate, d_dx      out  [B, t_blk, feat_dim] of `dtype`, every element written, overlapping no input
- * d_dstate_in        out  float32[B, feat_dim] or NULL (0 where the first slot does not go on) */
+ * d_dstate_in        out  float32[B, feat_dim] or NULL (0 where the first slot does not go on); may be
+ *                         d_dstate_out where t_blk <= 8 */
 bload_status bload_gated_scan_backward(const void* d_dout, const void* d_gate, const void* d_out, const uint8_t* d_reset,
                                        const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk, int64_t feat_dim,
                                        bload_dtype dtype, const float* d_state_in, const float* d_dstate_out, void* d_dgate,

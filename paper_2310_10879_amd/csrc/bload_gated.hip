@@ -49,7 +49,7 @@ __device__ __forceinline__ int slot_code(const GatedArgs& a, const uint8_t* rese
 }
 
 // V elements side by side, as they lie in memory; any alignment.  A lane whose V elements would pass the end of a row takes the
-// row's last V instead (some of them are its neighbour's too, which computes and stores the same).
+// row's last V instead.  Some of them are its neighbour's too, which in gated_kernel computes and stores the same.
 template <typename T, int V>
 struct Piece {
     static constexpr int kWords = V * sizeof(T) >= 4 ? V * (int)sizeof(T) / 4 : 1;
@@ -76,11 +76,23 @@ __device__ __forceinline__ void store_piece(void* base, int64_t row, int D, int 
     __builtin_memcpy(reinterpret_cast<T*>(base) + row * D + d, &t, sizeof(t));
 }
 
+// Elements from `skip` on alone; the others are 0, or are not stored.
 template <int V>
-__device__ __forceinline__ void load_state(const float* base, int64_t b, int D, int d, float (&x)[V])
+__device__ __forceinline__ void load_state(const float* base, int64_t b, int D, int d, float (&x)[V], int skip = 0)
 {
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = base ? base[b * D + d + v] : 0.0f;
+    for (int v = 0; v < V; ++v) x[v] = base && v >= skip ? base[b * D + d + v] : 0.0f;
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_behind(void* base, int64_t row, int D, int d, const float (&x)[V], int skip)
+{
+    if (skip == 0) {
+        store_piece<T, V>(base, row, D, d, x);
+    } else {
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (v >= skip) reinterpret_cast<T*>(base)[row * D + d + v] = (T)x[v];
+    }
 }
 
 // K slots of one lane in the order of the recurrence: slot i is row first + i forward, first - i backward, and the chunk's last
@@ -341,8 +353,9 @@ __global__ __launch_bounds__(kThreads) void gated_kernel(GatedArgs a)
     }
 }
 
-// Blocks of a few slots (one, when streams are served): a lane takes 16 bytes of a block from its first slot
-// to its last.
+// Blocks of a few slots (one, when streams are served): a lane takes V elements of a block from its first slot
+// to its last.  The state may be advanced in place, and nothing orders one wavefront's loads and another's stores: every element
+// has one lane that reads its state and stores its results.  The last lane of a row leaves `skip` elements to its neighbour.
 constexpr int kShort = 8;
 
 template <typename T, int V, bool BACK>
@@ -351,12 +364,12 @@ __global__ __launch_bounds__(kThreads) void gated_short_kernel(GatedArgs a, int6
     const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (n >= lanes) return;
     const int64_t b = n / a.slices;
-    const int d = min((int)(n - b * a.slices) * V, a.D - V);
+    const int d0 = (int)(n - b * a.slices) * V, d = min(d0, a.D - V), skip = d0 - d;
     const bool has_state = (BACK ? a.h0 : a.in) != nullptr;
     const uint8_t* reset = a.reset + b * a.T;
     const uint8_t* valid = a.valid + b * a.T;
     float at[V];
-    load_state<V>(a.in, b, a.D, d, at);
+    load_state<V>(a.in, b, a.D, d, at, skip);
     for (int i = 0; i < a.T; ++i) {
         const int t = BACK ? a.T - 1 - i : i;
         const int64_t row = b * a.T + t;
@@ -370,14 +383,14 @@ __global__ __launch_bounds__(kThreads) void gated_short_kernel(GatedArgs a, int6
         if constexpr (!BACK) {
 #pragma unroll
             for (int v = 0; v < V; ++v) at[v] = what == 2 ? fmaf(g[v], at[v], x[v]) : (what == 1 ? x[v] : 0.0f);
-            store_piece<T, V>(a.y, row, a.D, d, at);
+            store_behind<T, V>(a.y, row, a.D, d, at, skip);
         } else {
             float h[V], dg[V];
             if (t > 0) {
                 piece.load(a.h, row - 1, a.D, d);
                 piece.widen(h);
             } else {
-                load_state<V>(a.h0, b, a.D, d, h);
+                load_state<V>(a.h0, b, a.D, d, h, skip);
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -385,13 +398,14 @@ __global__ __launch_bounds__(kThreads) void gated_short_kernel(GatedArgs a, int6
                 dg[v] = what == 2 ? x[v] * h[v] : 0.0f;
                 at[v] = what == 2 ? g[v] * x[v] : 0.0f;
             }
-            store_piece<T, V>(a.y, row, a.D, d, x);
-            store_piece<T, V>(a.dgate, row, a.D, d, dg);
+            store_behind<T, V>(a.y, row, a.D, d, x, skip);
+            store_behind<T, V>(a.dgate, row, a.D, d, dg, skip);
         }
     }
     if (a.last)
 #pragma unroll
-        for (int v = 0; v < V; ++v) a.last[b * a.D + d + v] = at[v];
+        for (int v = 0; v < V; ++v)
+            if (v >= skip) a.last[b * a.D + d + v] = at[v];
 }
 
 struct GatedPlan {
