@@ -480,7 +480,8 @@ bload_status bload_segment_attention_decode(const bload_heads* q, const bload_he
  * d_state_in   in   float32[B, feat_dim] or NULL (no state: the first slot starts a sequence)
  * d_out        out  [B, t_blk, feat_dim] of `dtype`: h; every element is written
  * d_state_out  out  float32[B, feat_dim] or NULL: h of the last slot, unrounded; may be
- *                   d_state_in where t_blk <= 8
+ *                   d_state_in where t_blk <= 8, and is refused (BLOAD_EINVAL) where it meets
+ *                   d_state_in in any other way
  * d_workspace       device scratch of >= bload_gated_scan_workspace_bytes(...) bytes, 16-byte
  *                   aligned (may be NULL when that is 0); one answer for both passes
  * States are held in 32 bits.  What is cut off by a start or by padding has no part in a
@@ -497,7 +498,7 @@ bload_status bload_gated_scan(const void* d_gate, const void* d_x, const uint8_t
  * d_out, d_state_in  in   of the forward pass;  d_dstate_out  in  float32[B, feat_dim] or NULL
  * d_dgate, d_dx      out  [B, t_blk, feat_dim] of `dtype`, every element written, overlapping no input
  * d_dstate_in        out  float32[B, feat_dim] or NULL (0 where the first slot does not go on); may be
- *                         d_dstate_out where t_blk <= 8 */
+ *                         d_dstate_out or d_state_in where t_blk <= 8, else refused where it meets one */
 bload_status bload_gated_scan_backward(const void* d_dout, const void* d_gate, const void* d_out, const uint8_t* d_reset,
                                        const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk, int64_t feat_dim,
                                        bload_dtype dtype, const float* d_state_in, const float* d_dstate_out, void* d_dgate,

@@ -450,6 +450,15 @@ inline bload_status gated_check(int64_t num_blocks, int32_t t_blk, int64_t feat_
     return BLOAD_OK;
 }
 
+// A state may be handed in and out in one buffer where every element has one lane (gated_short_kernel); elsewhere a workgroup
+// could read what another one has advanced already.
+inline bool states_apart(const float* in, const float* out, int64_t num_blocks, int32_t t_blk, int64_t feat_dim)
+{
+    if (!in || !out || (in == out && t_blk <= kShort)) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(in), q = reinterpret_cast<uintptr_t>(out);
+    return (p < q ? q - p : p - q) >= (uintptr_t)num_blocks * (uintptr_t)feat_dim * sizeof(float);
+}
+
 template <typename T, int V, bool BACK>
 void gated_launch(const GatedArgs& a, const GatedPlan& p, hipStream_t stream)
 {
@@ -519,6 +528,7 @@ extern "C" bload_status bload_gated_scan(const void* d_gate, const void* d_x, co
     const size_t e = att_elem_bytes(dtype);
     if (!aligned_to(d_gate, e) || !aligned_to(d_x, e) || !aligned_to(d_out, e) || !aligned_to(d_state_in, 4) || !aligned_to(d_state_out, 4))
         return BLOAD_EALIGN;
+    if (!states_apart(d_state_in, d_state_out, num_blocks, t_blk, feat_dim)) return BLOAD_EINVAL;
     GatedArgs a = {};
     a.gate = d_gate;
     a.x = d_x;
@@ -545,6 +555,8 @@ extern "C" bload_status bload_gated_scan_backward(const void* d_dout, const void
     if (!aligned_to(d_dout, e) || !aligned_to(d_gate, e) || !aligned_to(d_out, e) || !aligned_to(d_dgate, e) || !aligned_to(d_dx, e) ||
         !aligned_to(d_state_in, 4) || !aligned_to(d_dstate_out, 4) || !aligned_to(d_dstate_in, 4))
         return BLOAD_EALIGN;
+    if (!states_apart(d_dstate_out, d_dstate_in, num_blocks, t_blk, feat_dim) || !states_apart(d_state_in, d_dstate_in, num_blocks, t_blk, feat_dim))
+        return BLOAD_EINVAL;
     GatedArgs a = {};
     a.gate = d_gate;
     a.x = d_dout;
