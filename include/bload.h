@@ -414,7 +414,7 @@ bload_status bload_segment_mask(const uint8_t* d_reset, const uint8_t* d_valid, 
  * part in a result, infinite or NaN as it may be.
  *
  * dtype      F16, BF16 or F32 (of q, k, v and out); head_dim 1 .. BLOAD_ATTENTION_MAX_HEAD_DIM
- * scale      > 0;  cap >= 0 (0: none);  d_slopes  in  float32[heads_q] or NULL
+ * scale      > 0;  cap >= 0 (0: none; from 2^100 on all alike);  d_slopes  in  float32[heads_q] or NULL
  * d_mask     from bload_segment_mask.  Any other intervals do as well; they are cut to
  *            [0, t_blk), and the backward pass needs the two of each slot to agree.
  * d_lse      out  float32[num_blocks, heads_q, t_blk] or NULL: ln sum e^s, for the

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                     float keep;
                     const float s = score.of<T, MOD>(x[i], away - result_row(i), keep) - lse;
                     x[i] = exp2_fast(span.has(key0 + result_row(i)) ? s : -INFINITY);
-                    if constexpr (MOD == kCap) y[i] *= keep;
+                    if constexpr (MOD >= kCap) y[i] *= keep;
                 } else {
                     x[i] = exp2_fast(fmaf(x[i], c, -lse));
                 }

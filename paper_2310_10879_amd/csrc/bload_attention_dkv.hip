@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
             };
             auto slope = [&](int i) {                          // ds / scale
                 y[i] = x[i] * (y[i] - delta[i / 4][i % 4]);
-                if constexpr (MOD == kCap) y[i] *= keep[i];
+                if constexpr (MOD >= kCap) y[i] *= keep[i];
             };
 #pragma unroll
             for (int n = 0; n < kSteps; ++n) {

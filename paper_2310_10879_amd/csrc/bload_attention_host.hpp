@@ -33,7 +33,7 @@ inline bload_status att_args(AttArgs& a, int64_t num_blocks, int32_t t_blk, int3
     a.mask = reinterpret_cast<const int4*>(d_mask);
     a.slopes = d_slopes;
     a.scale = scale;
-    a.cap = cap;
+    a.cap = std::fmin(cap, 0x1p100f);      // what float32 keeps of scores that such a cap moves (2^88 and more) has steps of 2^64
     a.B = (int32_t)num_blocks;
     a.T = t_blk;
     a.Hq = heads_q;
@@ -76,9 +76,13 @@ inline void att_variant(const AttArgs& a, F f)
 {
     using bias = std::integral_constant<int, kBias>;
     using cap = std::integral_constant<int, kCap>;
+    using cap_far = std::integral_constant<int, sizeof(T) == 2 ? kCapFar : kCap>;
     if (a.D % (16 / (int)sizeof(T))) {
-        if (a.cap > 0.0f) f(cap(), std::true_type());
+        if (a.cap > kNearCap) f(cap_far(), std::true_type());
+        else if (a.cap > 0.0f) f(cap(), std::true_type());
         else f(bias(), std::true_type());
+    } else if (a.cap > kNearCap) {
+        f(cap_far(), std::false_type());
     } else if (a.cap > 0.0f) {
         f(cap(), std::false_type());
     } else if (a.slopes) {
