@@ -432,8 +432,11 @@ bload_status bload_segment_attention(const bload_heads* q, const bload_heads* k,
 /* Gradients of sum(out * dout) by q, k and v (dk and dv summed over the heads that share
  * them; no gradient of scale, cap and slopes).  out, d_lse and, where it was written,
  * out_rest are those of the forward call with the same arguments; the outputs must not
- * overlap any input.  d_workspace: >= bload_segment_attention_backward_workspace_bytes()
- * bytes, 16-byte aligned.  Asynchronous on `hip_stream`; bit-identical like the forward pass. */
+ * overlap any input.  For 16-bit types probabilities and the gradients of scores are rounded to
+ * the type's precision before they meet dout, q and k; for F16 scaled by powers of two, so that
+ * they keep it however small or large dout is.
+ * d_workspace: >= bload_segment_attention_backward_workspace_bytes() bytes, 16-byte aligned.
+ * Asynchronous on `hip_stream`; bit-identical like the forward pass. */
 size_t bload_segment_attention_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t heads_q);
 
 bload_status bload_segment_attention_backward(const bload_heads* dout, const bload_heads* q, const bload_heads* k,

@@ -322,8 +322,9 @@ __device__ __forceinline__ void arrived(F (&x)[N])
     for (int s = 0; s < N; ++s) asm volatile("" : "+v"(x[s]));
 }
 
-// Eight scores in 32 bits to a B fragment.  16-bit types: rounded to nearest, which is the one rounding between
-// the inputs and the output (half a step of the type on each probability; sums and states stay in 32 bits).
+// Eight probabilities, or gradients of scores, in 32 bits to a B fragment.  16-bit types: rounded to nearest, half a step of the type
+// on each, because the matrix instructions take no wider operand beside 16-bit keys and values.  These are the roundings between the
+// inputs and the output: one forward, two on the way to dq and dk; sums and states stay in 32 bits.
 template <typename T>
 __device__ __forceinline__ frag8<T> pack8(const f32x16& x, int from)
 {
@@ -418,6 +419,30 @@ struct Maximum {
         f = up == -INFINITY ? 1.0f : exp2_fast(m - up);
         m = up;
         return true;
+    }
+};
+
+// Gradients of scores, p (dp - delta), may lie anywhere in the range of dout, and far below it where a row sees many: float16 would
+// lose them among its subnormals, or overflow.  They are packed as a multiple `by` of themselves, a power of two for each row of results:
+// the row's first one that is not 0 brings the largest of its tile between 2^12 and 2^13, and one that passes 2^15 does so again; the
+// row's sums shrink along.  Measured: 16 blocks of 3000 short recordings, 16 heads of 128: dq 413 -> 419 us, dk and dv 535 -> 569.
+struct Reach {
+    enum { kNone = 0, kFirst, kSums };
+    float by = 1.0f, limit = 0.0f;
+    // `top`: the largest of the new ones, times `by`.  Whether some lane's multiple changed, and that of sums which are not all 0; then
+    // `f` is what each lane's change by.
+    __device__ __forceinline__ int moves(float top, float& f)
+    {
+        if (!__any(top > limit)) return kNone;
+        f = 1.0f;
+        bool held = false;
+        if (top > limit) {
+            held = limit > 0.0f;
+            f = ldexpf(1.0f, min(13 - __builtin_amdgcn_frexp_expf(top), 64));     // (times any dp, below 2^41: far inside float32)
+            by *= f;
+            limit = 0x1p15f;
+        }
+        return __any(held) ? kSums : kFirst;
     }
 };
 

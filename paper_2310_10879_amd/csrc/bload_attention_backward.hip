@@ -116,6 +116,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     f32x16 o[kParts];
 #pragma unroll
     for (int d = 0; d < kParts; ++d) o[d] = f32x16{};
+    constexpr bool kHalf = std::is_same<T, att_half>::value;
+    Reach reach;
     typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
@@ -144,9 +146,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                 for (int i = 0; i < 16; ++i) x[i] = span.has(key0 + result_row(i)) ? x[i] : -INFINITY;
             }
             const float away = (float)(row - key0);
+            const float less = kHalf ? delta * reach.by : delta;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                y[i] -= delta;
+                y[i] = kHalf ? fmaf(y[i], reach.by, -less) : y[i] - less;
                 if constexpr (MOD != kPlain) {                 // (a cap makes a finite score of -infinity: hidden here, in any tile)
                     float keep;
                     const float s = score.of<T, MOD>(x[i], away - result_row(i), keep) - lse;
@@ -157,6 +160,19 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                 }
                 x[i] *= y[i];
             }
+            if constexpr (kHalf) {
+                in_order();                                    // (with what follows among it some instances need more registers than there are)
+                float top = 0.0f, f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+                if (const int moved = reach.moves(halves_max(top), f)) {
+                    x *= f;
+                    if (moved == Reach::kSums) {
+#pragma unroll
+                        for (int d = 0; d < kParts; ++d) o[d] *= f;
+                    }
+                }
+            }
             ahead<2 * kParts, kAhead>([&](int n) { return L::col_frag(ks[buf], by_col, 32 * t + 16 * (n / kParts), 32 * (n % kParts)); },
                                       [&](int n, frag8<T> f) { o[n % kParts] = mma(f, pack8<T>(x, 8 * (n / kParts)), o[n % kParts]); });
         }
@@ -164,7 +180,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     bool bad = false;
 #pragma unroll
     for (int d = 0; d < kParts; ++d) {
-        o[d] *= a.scale;
+        o[d] *= kHalf ? a.scale / reach.by : a.scale;
 #pragma unroll
         for (int i = 0; i < 16; ++i) bad |= not_finite(o[d][i]);
         if (span.hi <= span.lo) o[d] = f32x16{};

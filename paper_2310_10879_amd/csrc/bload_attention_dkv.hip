@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
     using L = Tile<T, DP>;
     constexpr int kSteps = DP / 16, kParts = DP / 32, kQueries = sizeof(T) == 2 ? 64 : 32;
     __shared__ T tiles[2][2][kQueries * DP];               // of queries and of do: one array, so that one address serves both
-    __shared__ float sums[2][2][kQueries];                 // lse (in units of ln 2) and delta of the tile's queries
+    __shared__ float sums[2][2][kQueries];                 // lse (in units of ln 2, less what probabilities carry) and delta of the tile's queries
     __shared__ int hull[2][kThreads / kWave];
     const int lane = lane_id(), wave = wave_id(), tid = (int)threadIdx.x;
 
@@ -108,6 +108,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
         next_at += kQueries;
     };
     const float c = a.scale * kLog2e;
+    // float16: probabilities carry 2^12, so that those of long sequences stay above its subnormals
+    constexpr bool kHalf = std::is_same<T, att_half>::value;
+    constexpr int kMore = kHalf ? 12 : 0;
+    constexpr bool kAccumulators = !(sizeof(T) == 2 && DP <= 64);
+    Reach reach;
 
     int left = lo < hi ? a.G : 0, q0 = lo;                 // heads
     if (left > 0) {
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
     arrived(k);
     arrived(v);
     for (int buf = 0; left > 0; buf ^= 1) {
-        if constexpr (!(sizeof(T) == 2 && DP <= 64)) {
+        if constexpr (kAccumulators) {
             keep_sums(dk);
             keep_sums(dv);
         }
@@ -126,7 +131,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
         if (tid < 2 * kQueries) {
             // (a query that sees nothing has lse -infinity: no part of it may get a probability)
             float z = next_sum;
-            if (tid < kQueries) z = z == -INFINITY ? INFINITY : z * kLog2e;
+            if (tid < kQueries) z = z == -INFINITY ? INFINITY : z * kLog2e - kMore;
             sums[buf][tid / kQueries][tid & (kQueries - 1)] = z;
         }
         __syncthreads();
@@ -206,24 +211,65 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
             }
 #pragma unroll
             for (int d = kAhead; d < 2 * kParts; ++d) column(0, d);
-            frag8<T> p = pack8<T>(x, 0);
+            frag8<T> p = pack8<T>(x, 0), ds;
+            if constexpr (kHalf) {
+                // (both halves' products with p first, beside the search for the largest ds, on which the multiple depends)
+                float top = 0.0f, f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) slope(i);
-            in_order();
-            frag8<T> ds = pack8<T>(y, 0);
+                for (int d = 0; d < kParts; ++d) {
+                    dv[d] = mma(cg[0][d], p, dv[d]);
+                    column(1, d);
 #pragma unroll
-            for (int d = 0; d < 2 * kParts; ++d) {
-                if (d < kParts) dv[d] = mma(cg[0][d], p, dv[d]);
-                else dk[d - kParts] = mma(cq[0][d - kParts], ds, dk[d - kParts]);
-                column(1, d);
+                    for (int i = 16 * d / kParts; i < 16 * (d + 1) / kParts; ++i) {
+                        slope(i);
+                        top = fmaxf(top, fabsf(y[i]));
+                    }
+                    in_order();
+                }
+                if (reach.moves(halves_max(top) * reach.by, f) == Reach::kSums) {
+                    if constexpr (kAccumulators) keep_sums(dk);        // (they leave their registers here, not at every step)
 #pragma unroll
-                for (int i = 8 + 4 * d / kParts; i < 8 + 4 * (d + 1) / kParts; ++i) slope(i);
+                    for (int d = 0; d < kParts; ++d) dk[d] *= f;
+                    if constexpr (kAccumulators) keep_sums(dk);
+                }
+                p = pack8<T>(x, 8);
                 in_order();
-            }
-            p = pack8<T>(x, 8);
-            ds = pack8<T>(y, 8);
 #pragma unroll
-            for (int d = 0; d < kParts; ++d) dv[d] = mma(cg[1][d], p, dv[d]);
+                for (int d = 0; d < kParts; ++d) {
+                    dv[d] = mma(cg[1][d], p, dv[d]);
+#pragma unroll
+                    for (int i = 8 * d / kParts; i < 8 * (d + 1) / kParts; ++i) y[i] *= reach.by;
+                    in_order();
+                }
+                ds = pack8<T>(y, 0);
+#pragma unroll
+                for (int d = 0; d < kParts; ++d) {
+                    dk[d] = mma(cq[0][d], ds, dk[d]);
+                    column(1, kParts + d);
+#pragma unroll
+                    for (int i = 8 + 8 * d / kParts; i < 8 + 8 * (d + 1) / kParts; ++i) y[i] *= reach.by;
+                    in_order();
+                }
+                ds = pack8<T>(y, 8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) slope(i);
+                in_order();
+                ds = pack8<T>(y, 0);
+#pragma unroll
+                for (int d = 0; d < 2 * kParts; ++d) {
+                    if (d < kParts) dv[d] = mma(cg[0][d], p, dv[d]);
+                    else dk[d - kParts] = mma(cq[0][d - kParts], ds, dk[d - kParts]);
+                    column(1, d);
+#pragma unroll
+                    for (int i = 8 + 4 * d / kParts; i < 8 + 4 * (d + 1) / kParts; ++i) slope(i);
+                    in_order();
+                }
+                p = pack8<T>(x, 8);
+                ds = pack8<T>(y, 8);
+#pragma unroll
+                for (int d = 0; d < kParts; ++d) dv[d] = mma(cg[1][d], p, dv[d]);
+            }
 #pragma unroll
             for (int d = 0; d < kParts; ++d) dk[d] = mma(cq[1][d], ds, dk[d]);
         }
@@ -231,7 +277,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
     bool bad = false;
 #pragma unroll
     for (int d = 0; d < kParts; ++d) {
-        dk[d] *= a.scale;
+        dk[d] *= kHalf ? a.scale / (reach.by * (1 << kMore)) : a.scale;
+        if constexpr (kHalf) dv[d] *= 1.0f / (1 << kMore);
 #pragma unroll
         for (int i = 0; i < 16; ++i) bad |= not_finite(dk[d][i]) || not_finite(dv[d][i]);
         if (span.hi <= span.lo) dk[d] = dv[d] = f32x16{};

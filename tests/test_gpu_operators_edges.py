@@ -91,3 +91,95 @@ def test_large_and_small_caps(cap, size, dtype):
     """A cap far above the scores leaves them as they are; one far below leaves all alike."""
     print(f"cap {cap} scores of {size} {dtype}", flush=True)
     capped(dtype, cap, size)
+
+
+def gradients(T, dtype, starts, causal, q, k, v, g, where=None):
+    """dq, dk and dv of one block of sequences that begin at `starts`, with one head of keys and a scale of 1, against 64 bits, with bounds that hold over the whole range of a type: a gradient of a
+    score, p (dp - delta), keeps half a step of the type however small dout is, down to 2^-37 of the row's largest dp - delta (float16 packs it
+    as a multiple: 2^-25 is half of its smallest number, the row's largest lies above 2^12), a probability down to 2^-37.  where: the slots to compare."""
+    bl = binding()
+    H, D, scale = q.shape[2], q.shape[3], 1.0
+    at = np.arange(T)
+    seq = np.searchsorted(starts, at, side="right")
+    see = (seq[:, None] == seq) & ((at[:, None] >= at) | (not causal))
+    Q, K, V, G = (np.moveaxis(ref.wide(t), 2, 1)[0] for t in (q, k, v, g))
+    u, z = ref.half_step(dtype), ref.tiny(dtype)
+    z_ds = 2.0 ** -37 if dtype == "f16" else 0.0
+    s = scale * Q @ K.swapaxes(1, 2)
+    off = (D + 4) * ref.U32 * scale * (np.abs(Q) @ np.abs(K).swapaxes(1, 2)) + 4 * ref.U32 * (np.abs(s) + 1)
+    m = np.where(see, s, -np.inf).max(2, keepdims=True)
+    p = np.where(see, np.exp(s - m), 0)
+    total = p.sum(2, keepdims=True)
+    p /= total
+    lse = np.log(total) + m
+    d = 2.5 * np.where(see, off + 4 * ref.U32 * np.abs(s - m), 0).max(2, keepdims=True) + (T + 8) * ref.U32
+    out = p @ V
+    out_off = (d + u) * (p @ np.abs(V)) + z * (see @ np.abs(V))
+    d = 2 * d + 12 * ref.U32 * (np.abs(lse) + 1)             # the backward pass takes p from the stored lse
+    dp, dp_off = G @ V.swapaxes(1, 2), (D + 2) * ref.U32 * (np.abs(G) @ np.abs(V).swapaxes(1, 2))
+    delta = (G * out).sum(2, keepdims=True)
+    delta_off = (np.abs(G) * (out_off + (2 * u * u + D * ref.U32) * np.abs(out) + z)).sum(2, keepdims=True)
+    ds = p * (dp - delta)
+    ds_off = (d + u) * np.abs(ds) + p * (dp_off + delta_off)
+    size = np.where(see, np.abs(dp - delta) + dp_off + delta_off, 0)
+    dq = scale * ds @ K
+    dq_off = scale * (ds_off + 2 * T * ref.U32 * np.abs(ds) + z_ds * see * size.max(2, keepdims=True)) @ np.abs(K)
+    t = lambda x: x.swapaxes(1, 2)
+    dk = (scale * t(ds) @ Q).sum(0)
+    dk_off = (scale * t(ds_off + 2 * H * T * ref.U32 * np.abs(ds) + z_ds * see * size.max((0, 1))) @ np.abs(Q)).sum(0)
+    dv = (t(p) @ G).sum(0)
+    dv_off = (t((d + u + 2 * H * T * ref.U32) * p + z_ds * see) @ np.abs(G)).sum(0)
+    want = [(x, x_off + u * np.abs(x) + z) for x, x_off in ((dq, dq_off), (dk, dk_off), (dv, dv_off))]
+    dq, dk, dv, dg = (x.cuda() for x in (q, k, v, g))
+    reset = to_dev(np.isin(at, starts).astype(np.uint8)[None])
+    mask = bl.bload_segment_mask(reset, torch.ones_like(reset), causal=causal)
+    y, saved = bl.bload_segment_attention(dq, dk, dv, mask, scale=scale, training=True)
+    got = bl.bload_segment_attention_backward(dg, dq, dk, dv, y, saved, mask, scale=scale)
+    live = np.ones(T, bool) if where is None else where
+    for name, x, (value, bound) in zip(("dq", "dk", "dv"), got, want):
+        x = np.moveaxis(ref.wide(x), 2, 1)[0]
+        value, bound = (y if y.ndim == 3 else y[None] for y in (value, bound))
+        # a value that the type cannot hold is infinite in it
+        x = np.where((np.abs(value) + bound > torch.finfo(ref.TORCH[dtype]).max) & (x == np.copysign(np.inf, value)), value, x)
+        ref.assert_close(x[:, live], value[:, live], bound[:, live], f"{name} T={T} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("gain", [1e-6, 1e-5, 1e-3, 1.0, 1e4])
+@pytest.mark.parametrize("causal,D", [(False, 64), (True, 40), (False, 128)])
+def test_gradients_of_small_and_large_dout(causal, D, gain, dtype):
+    """One long sequence whose values are its keys, so that dq is dout times their spread, at any size of dout."""
+    print(f"gradients D={D} {dtype} causal {causal} dout of {gain}", flush=True)
+    T, H = 1500, 2
+    rng = np.random.default_rng([T, D])
+    q, k, g = (ref.draw(rng, (1, T, h, D), "f32") for h in (H, 1, H))
+    q, k, g = (x.to(ref.TORCH[dtype]) for x in (q / D, k, g * gain))
+    gradients(T, dtype, [0], causal, q, k, k, g)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("rise", [6.0, -6.0])
+def test_gradients_of_sizes_that_change(rise, causal, dtype):
+    """dout, or values, that grow or shrink by a factor of 10^6 along a sequence."""
+    T, H, D = 700, 2, 64
+    rng = np.random.default_rng(T)
+    q, k, v, g = (ref.draw(rng, (1, T, h, D), "f32") for h in (H, 1, 1, H))
+    slope = torch.from_numpy(10.0 ** (rise * (np.arange(T) / T - 0.5))).float()[None, :, None, None]
+    half = slope.abs() ** 0.5
+    for x, y in ((v, g * slope), (v * half, g), (v * half, g * half.flip(1))):
+        gradients(T, dtype, [0], causal, *(t.to(ref.TORCH[dtype]) for t in (q / 8, k, x, y)))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients_beside_a_sequence_of_large_ones(causal, dtype):
+    """The largest gradients of a neighbour in the block leave small ones as they are."""
+    T, H, D = 300, 2, 64
+    rng = np.random.default_rng(T)
+    q, k, g = (ref.draw(rng, (1, T, h, D), "f32") for h in (H, 1, H))
+    starts = [0, 45, 90, 200]
+    loud = (np.arange(T) >= 45) & (np.arange(T) < 90)
+    g = g * torch.from_numpy(np.where(loud, 1e4, 1e-6)).float()[None, :, None, None]
+    q, k, g = (x.to(ref.TORCH[dtype]) for x in (q / 8, k, g))
+    gradients(T, dtype, starts, causal, q, k, k, g, ~loud)
