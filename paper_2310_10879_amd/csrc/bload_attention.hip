@@ -15,31 +15,17 @@ namespace {
 // waits at its barrier or forms probabilities.
 template <typename T> constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
 
-// One query again, key by key in plain 32-bit arithmetic.  The matrix product adds 0 * v for what the
-// mask hides, which is NaN where a hidden v is infinite or NaN; rows that come out not finite are
-// computed here, from visible keys alone.
+// One query again.  The matrix product adds 0 * v for what the mask hides, which is NaN where a hidden v is infinite or NaN,
+// and its sums are not divided on the way; rows that come out not finite are computed here, from visible keys alone.
 template <typename T>
 __device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 {
     const int D = a.D, kv = head / a.G;
-    const Score score(a, head);
-    float q[2], acc[2] = {0.0f, 0.0f}, m = -INFINITY, l = 0.0f, keep;
-    load_row2(att_at<T>(a.q, b, i, head), D, q);
-    for (int j = span.lo; j < span.hi; ++j) {
-        float k[2], v[2];
-        load_row2(att_at<T>(a.k, b, j, kv), D, k);
-        load_row2(att_at<T>(a.v, b, j, kv), D, v);
-        const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
-        const float up = fmaxf(m, s), base = up == -INFINITY ? 0.0f : up;
-        const float f = exp2_fast(m - base), p = exp2_fast(s - base);
-        m = up;
-        l = l * f + p;
-        acc[0] = acc[0] * f + p * v[0];
-        acc[1] = acc[1] * f + p * v[1];
-    }
-    const float inv = 1.0f / l, o0 = acc[0] * inv, o1 = acc[1] * inv;
-    store_row2(att_at<T>(a.out, b, i, head), D, o0, o1);
-    if (a.rest.p) store_row2(att_at<T>(a.rest, b, i, head), D, o0 - (float)(T)o0, o1 - (float)(T)o1);
+    float o[2], m, l;
+    plain_row<T>(att_at<T>(a.q, b, i, head), att_at<T>(a.k, b, 0, kv), att_at<T>(a.v, b, 0, kv), a.k.st, a.v.st, D, Score(a, head), i, span.lo,
+                 span.hi, o, m, l);
+    store_row2(att_at<T>(a.out, b, i, head), D, o[0], o[1]);
+    if (a.rest.p) store_row2(att_at<T>(a.rest, b, i, head), D, o[0] - (float)(T)o[0], o[1] - (float)(T)o[1]);
     if (a.lse && lane_id() == 0) a.lse[((int64_t)b * a.Hq + head) * a.T + i] = (m + log2f(l)) * kLn2;
 }
 

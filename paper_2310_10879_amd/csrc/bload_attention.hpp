@@ -509,4 +509,58 @@ __device__ __forceinline__ void store_row2(T* row, int D, float x0, float x1)
 
 __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
+// One query, at slot `at` of its block, over the keys [lo, hi), in plain 32-bit arithmetic, by one wavefront: lanes take a key each for the
+// scores, then two elements of the values each.  The result is a mean all along (a sum could leave float32 where the mean does
+// not), NaN where no key has a probability.  m and l as in the kernels: the maximum in units of ln 2, the sum of 2^(s - m).
+template <typename T>
+__device__ void plain_row(const T* q, const T* k, const T* v, int64_t k_stride, int64_t v_stride, int D, const Score& score, int at, int lo, int hi,
+                          float (&o)[2], float& m, float& l)
+{
+    constexpr int N = 16 / (int)sizeof(T);
+    o[0] = o[1] = l = 0.0f;
+    m = -INFINITY;
+    for (int j0 = lo; j0 < hi; j0 += kWave) {
+        const int j = j0 + lane_id();
+        float s = -INFINITY;
+        if (j < hi) {
+            const T* row = k + j * k_stride;
+            float dot = 0.0f, keep;
+            for (int d = 0; d < D; d += N) {
+                const vec16 a = load_chunk<T, true>(q, d, D), b = load_chunk<T, true>(row, d, D);
+                T x[N], y[N];
+                __builtin_memcpy(&x, &a, 16);
+                __builtin_memcpy(&y, &b, 16);
+#pragma unroll
+                for (int n = 0; n < N; ++n) dot = fmaf((float)x[n], (float)y[n], dot);
+            }
+            s = score.any<T>(dot, at - j, keep);
+        }
+        float top = s;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float up = fmaxf(m, top), base = up == -INFINITY ? 0.0f : up;
+        const float p = exp2_fast(s - base), part = l * exp2_fast(m - base);
+        m = up;
+        l = part + wave_sum(p);
+        if (l != l) break;                                 // a score that is no number: nor is anything else
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f, w = p * inv;
+        o[0] *= part * inv;
+        o[1] *= part * inv;
+        const int count = min(hi - j0, kWave);
+        for (int n0 = 0; n0 < count; n0 += 4) {
+            float x[4][2];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) load_row2(v + (j0 + min(n0 + n, count - 1)) * v_stride, D, x[n]);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float weight = __shfl(w, n0 + n);
+                if (n0 + n >= count) break;
+                o[0] = fmaf(weight, x[n][0], o[0]);
+                o[1] = fmaf(weight, x[n][1], o[1]);
+            }
+        }
+    }
+    if (!(l > 0.0f)) o[0] = o[1] = NAN;
+}
+
 }  // namespace bload

@@ -33,6 +33,18 @@ __device__ __forceinline__ int decode_length(const DecodeArgs& p, int64_t seq, i
     return block >= 0 && block < p.blocks && offset >= 0 && n > 0 && n <= p.a.T - offset ? n : 0;
 }
 
+// One sequence and head again, where the result is not finite: a value that is seen and infinite meets the zeros of a tile's missing
+// keys, and sums of values near the largest float leave float32 (see plain_row).
+template <typename T>
+__device__ void decode_row(const AttArgs& a, int64_t seq, int head, int64_t b, int offset, int n)
+{
+    const int kv = head / a.G;
+    float o[2], m, l;
+    plain_row<T>(att_at<T>(a.q, seq, 0, head), att_at<T>(a.k, b, offset, kv), att_at<T>(a.v, b, offset, kv), a.k.st, a.v.st, a.D, Score(a, head), n - 1,
+                 0, n, o, m, l);
+    store_row2(att_at<T>(a.out, seq, 0, head), a.D, o[0], o[1]);
+}
+
 // One share of one sequence for up to 32 heads of queries.  Measured: 32 blocks of 32768 slots, 8 heads of 128 bfloat16 read by 32: 0.58 ms,
 // 5.6 TB/s of keys and values (a copy of 2 GiB: 4.9 read and written).
 template <typename T, int DP, int MOD, bool ODD>
@@ -44,6 +56,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     // tiles of keys and values, later the wavefronts' results
     __shared__ __attribute__((aligned(16))) char raw[std::max<size_t>(2 * kWaves * kTile * sizeof(T), kWaves * 32 * DP * sizeof(float))];
     __shared__ float tops[kWaves][32], sums[kWaves][32];
+    __shared__ int again[32], any_again;                   // heads whose result is not finite
     const AttArgs& a = p.a;
     const int lane = lane_id(), wave = wave_id(), D = a.D;
     T* ks = reinterpret_cast<T*>(raw) + wave * 2 * kTile;
@@ -149,6 +162,7 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
     if (lane < 32) {
         tops[wave][lane] = max.m;
         sums[wave][lane] = l;
+        if (wave == 0) again[lane] = any_again = 0;
     }
     __syncthreads();
     const int columns = min(a.G - cg * 32, 32);
@@ -166,7 +180,9 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
             z += f * sums[w][col];
         }
         if (p.splits == 1) {
-            att_at<T>(a.out, seq, 0, h)[d] = (T)(n > 0 ? y / z : 0.0f);
+            const float r = n > 0 ? y / z : 0.0f;
+            att_at<T>(a.out, seq, 0, h)[d] = (T)r;
+            if (not_finite(r)) again[col] = any_again = 1;
         } else {
             float* to = p.part + ((seq * a.Hq + h) * p.splits + split) * (D + 2);
             to[2 + d] = y;
@@ -176,6 +192,11 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
             }
         }
     }
+    if (p.splits > 1) return;
+    __syncthreads();
+    if (!any_again) return;
+    for (int col = wave; col < columns; col += kWaves)
+        if (again[col]) decode_row<T>(a, seq, kv * a.G + cg * 32 + col, b, off, n);
 }
 
 // The shares of one sequence and head to one: a wavefront each.
@@ -206,7 +227,10 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(DecodeArgs p)
     }
     const float inv = n > 0 ? 1.0f / z : 0.0f;
     if (n == 0) y[0] = y[1] = 0.0f;
-    store_row2(att_at<T>(a.out, seq, 0, head), D, y[0] * inv, y[1] * inv);
+    y[0] *= inv;
+    y[1] *= inv;
+    if (__any(not_finite(y[0]) || not_finite(y[1]))) decode_row<T>(a, seq, head, b, off, n);
+    else store_row2(att_at<T>(a.out, seq, 0, head), D, y[0], y[1]);
 }
 
 // Shares: as many as make eight workgroups for each CU, of at least 256 keys of the longest sequence that a block can hold.

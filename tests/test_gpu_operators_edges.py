@@ -183,3 +183,52 @@ def test_gradients_beside_a_sequence_of_large_ones(causal, dtype):
     g = g * torch.from_numpy(np.where(loud, 1e4, 1e-6)).float()[None, :, None, None]
     q, k, g = (x.to(ref.TORCH[dtype]) for x in (q / 8, k, g))
     gradients(T, dtype, starts, causal, q, k, k, g, ~loud)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (40, 1, 37), (2, 2, 128)])
+@pytest.mark.parametrize("T,n", [(200, 1), (200, 31), (200, 32), (200, 33), (200, 130), (2000, 33), (2000, 1999)])
+def test_single_query_with_an_infinite_value(T, n, Hq, Hkv, D, dtype):
+    """A value that is seen and infinite: infinite in the result, where it lies, whatever tile or share it ends (T decides on the shares)."""
+    print(f"single query T={T} n={n} Hq={Hq} Hkv={Hkv} D={D} {dtype}", flush=True)
+    bl = binding()
+    rng = np.random.default_rng([T, n, Hq, D])
+    q, k, v = (ref.draw(rng, (1, t, h, D), dtype).cuda() for t, h in ((1, Hq), (T, Hkv), (T, Hkv)))
+    table = [to_dev(np.array([x], np.int32)) for x in (0, T - n, n)]
+    one = torch.ones((1, n), dtype=torch.uint8, device="cuda")
+    mask = bl.bload_segment_mask(torch.zeros_like(one), one, causal=False)
+    clean = bl.bload_segment_attention_decode(q[0], k, v, *table)
+    assert torch.isfinite(clean).all()
+    for at, value in ((T - 1, float("inf")), (T - n, float("-inf")), (T - 1 - n // 2, float("nan"))):
+        v2 = v.clone()
+        v2[0, at, :, D // 2] = value
+        got = bl.bload_segment_attention_decode(q[0], k, v2, *table)
+        wide = torch.cat([torch.zeros((1, n - 1, Hq, D), dtype=q.dtype, device="cuda"), q], 1)
+        whole = bl.bload_segment_attention(wide, k[:, T - n:], v2[:, T - n:], mask)[0, -1:]
+        want = torch.full((1, Hq), value, dtype=q.dtype, device="cuda")
+        for x in (got, whole):
+            assert torch.equal(x[:, :, D // 2].nan_to_num(nan=5.0), want.nan_to_num(nan=5.0)), f"value {value} at {at}"
+        rest = torch.arange(D, device="cuda") != D // 2
+        # (the same sums in another order, and probabilities that are not rounded: a few steps of the type)
+        assert ((got - clean)[:, :, rest].float().abs() <= 8 * ref.half_step(dtype) * (clean[:, :, rest].float().abs() + 1)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,n", [(200, 7), (200, 150), (2000, 1999)])
+def test_values_near_the_largest(T, n, dtype):
+    """Sums of them leave float32, their mean does not."""
+    bl = binding()
+    rng = np.random.default_rng([T, n])
+    big = 0.9 * float(torch.finfo(ref.TORCH[dtype]).max)
+    q, k = (ref.draw(rng, (1, t, 2, 32), dtype).cuda() for t in (1, T))
+    v = torch.full((1, T, 2, 32), big, dtype=ref.TORCH[dtype], device="cuda")
+    v[..., 1::2] *= -1
+    table = [to_dev(np.array([x], np.int32)) for x in (0, T - n, n)]
+    got = bl.bload_segment_attention_decode(q[0], k, v, *table)
+    one = torch.ones((1, n), dtype=torch.uint8, device="cuda")
+    mask = bl.bload_segment_mask(torch.zeros_like(one), one, causal=False)
+    whole = bl.bload_segment_attention(k[:, T - n:], k[:, T - n:], v[:, T - n:], mask)
+    # a mean of equal values: the weights' sum is off by n + 8 roundings, the result by one of the type
+    off = (n + 8) * ref.U32 + 2 * ref.half_step(dtype)
+    for x, y in ((got, v[0, :1]), (whole, v[:, :n])):
+        assert torch.isfinite(x).all() and ((x.double() / y.double() - 1).abs() <= off).all()
