@@ -15,10 +15,9 @@ namespace {
 // waits at its barrier or forms probabilities.
 template <typename T> constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
 
-// One query again.  The matrix product adds 0 * v for what the mask hides, which is NaN where a hidden v is infinite or NaN,
-// and its sums are not divided on the way; rows that come out not finite are computed here, from visible keys alone.
+// One query again, from visible keys alone.
 template <typename T>
-__device__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
+__device__ __forceinline__ void forward_row(const AttArgs& a, int b, int head, int i, Span span)
 {
     const int D = a.D, kv = head / a.G;
     float o[2], m, l;
@@ -97,8 +96,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs 
     typename L::Reader by_row = L::rows(), by_col = L::columns();
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
-        next_k.store(ks[buf]);
-        next_v.store(vs[buf]);
+        next_k.store(ks[buf], hi - k0);
+        next_v.store(vs[buf], hi - k0);
         __syncthreads();
         if (k0 + kKeys < hi) {
             next_k.load(k0 + kKeys, hi);
@@ -187,12 +186,19 @@ __global__ __launch_bounds__(kThreads, 2) void attention_forward_kernel(AttArgs 
         if (a.lse && lane < 32)
             a.lse[((int64_t)b * a.Hq + head) * T_ + row] = span.hi > span.lo ? (max.m + log2f(l)) * kLn2 : -INFINITY;
     }
-    uint64_t again = __ballot(bad && span.hi > span.lo);
+    if (!__any(bad && span.hi > span.lo)) return;
+    const AttArgs late = args_again();
+    // spoiled by what is hidden; or by sums that left float32, which those of halfs cannot: then nothing seen is at fault
+    Met met;
+    auto keys = [&](int r) { return row_not_finite(att_at<T>(late.k, b, r, kv), late.D) || row_not_finite(att_at<T>(late.v, b, r, kv), late.D); };
+    constexpr bool kHalf = std::is_same<T, att_half>::value;
+    met.look_around(span, late.T, !kHalf, keys);
+    uint64_t again = __ballot(bad && span.hi > span.lo && (met.hidden || (!kHalf && !met.seen)));
     again = (again | (again >> 32)) & 0xffffffffu;
     while (again) {
         const int r = __ffsll((unsigned long long)again) - 1;
         again &= again - 1;
-        forward_row<T>(a, b, head, tile * 128 + wave * 32 + r, {__shfl(span.lo, r), __shfl(span.hi, r)});
+        forward_row<T>(late, b, head, __builtin_amdgcn_readlane(row, r), {__builtin_amdgcn_readlane(span.lo, r), __builtin_amdgcn_readlane(span.hi, r)});
     }
 }
 

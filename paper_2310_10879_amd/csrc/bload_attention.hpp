@@ -236,7 +236,7 @@ struct Stage {
         return r;
     }
     // the R rows from row0 on, where begin() or the last load() left off; in the place of rows from `limit` on, the last one in
-    // front of it (what they give is masked)
+    // front of it
     __device__ __forceinline__ void load(int row0, int limit)
     {
         if (row0 + R <= limit) {
@@ -269,11 +269,15 @@ struct Stage {
         return v;
     }
     __device__ __forceinline__ void put(T* tile, int i, vec16 y) const { __builtin_memcpy(tile + L::at(row + i * kRows, place), &y, 16); }
-    __device__ __forceinline__ void store(T* tile) const
+    // `left`: rows in front of the limit; zeros behind them, as 0 times what they hold has to be 0
+    __device__ __forceinline__ void store(T* tile, int left) const
     {
         if (kWide != L::kChunks && place >= L::kChunks) return;
         if (kRows > R && (int)threadIdx.x % THREADS / kWide >= R) return;
-        if (D == DP) {
+        if (left < R) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) put(tile, i, row + i * kRows < left ? whole(x[i]) : vec16{0, 0, 0, 0});
+        } else if (D == DP) {
             asm volatile("");                              // (a branch: by selection instead it costs every 16 bytes four of them)
 #pragma unroll
             for (int i = 0; i < kEach; ++i) put(tile, i, x[i]);
@@ -509,31 +513,145 @@ __device__ __forceinline__ void store_row2(T* row, int D, float x0, float x1)
 
 __device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) <= 3.402823466e38f); }
 
-// One query, at slot `at` of its block, over the keys [lo, hi), in plain 32-bit arithmetic, by one wavefront: lanes take a key each for the
-// scores, then two elements of the values each.  The result is a mean all along (a sum could leave float32 where the mean does
-// not), NaN where no key has a probability.  m and l as in the kernels: the maximum in units of ln 2, the sum of 2^(s - m).
+// ---- rows that come out not finite ---------------------------------------------------
+//
+// What the mask hides has probability 0 in a matrix product, and 0 times an infinite or NaN element is NaN.  Such rows are computed
+// again by their wavefront, in plain 32-bit arithmetic and from what they see alone, but only where something hidden is not finite:
+// a row that sees such an element itself is what the matrix product made of it.
+
+// The kernel's arguments read anew, so that those which only the rows below use are not held in registers up to there.
+__device__ __forceinline__ AttArgs args_again()
+{
+    auto p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    AttArgs a;
+    __builtin_memcpy(&a, (const void*)p, sizeof(a));
+    return a;
+}
+
 template <typename T>
-__device__ void plain_row(const T* q, const T* k, const T* v, int64_t k_stride, int64_t v_stride, int D, const Score& score, int at, int lo, int hi,
-                          float (&o)[2], float& m, float& l)
+__device__ __forceinline__ bool row_not_finite(const T* row, int D)
 {
     constexpr int N = 16 / (int)sizeof(T);
+    bool bad = false;
+    for (int d = 0; d < D; d += 4 * N) {
+        vec16 c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = load_chunk<T, true>(row, d + i * N, D);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            T x[N];
+            __builtin_memcpy(&x, &c[i], 16);
+#pragma unroll
+            for (int n = 0; n < N; ++n) bad |= not_finite((float)x[n]);
+        }
+    }
+    return bad;
+}
+
+// Rows of operands that are not finite, as each lane's row meets them: hidden from it, or seen.
+struct Met {
+    bool hidden = false, seen = false;
+    // bad(r): row r of the operands has an element that is not finite; lanes ask for 64 rows at a time
+    template <typename Bad>
+    __device__ __forceinline__ void look(Span span, int lo, int hi, Bad bad)
+    {
+        for (int r0 = lo; r0 < hi; r0 += kWave) {
+            const int r = r0 + lane_id();
+            for (uint64_t rows = __ballot(r < hi && bad(r)); rows; rows &= rows - 1) {
+                const bool has = span.has(r0 + __ffsll((unsigned long long)rows) - 1);
+                hidden |= !has;
+                seen |= has;
+            }
+        }
+    }
+    // of the rows that its wavefront's tiles can have held: those that some lane does not see, or all
+    template <typename Bad>
+    __device__ __forceinline__ void look_around(Span span, int T, bool all, Bad bad)
+    {
+        const bool any = span.hi > span.lo;
+        const int from = max(0, wave_min(any ? span.lo : T) - 64), to = min(T, wave_max(span.hi) + 64);
+        const int in_lo = wave_max(any ? span.lo : 0), in_hi = wave_min(any ? span.hi : T);
+        if (all || in_lo >= in_hi) return look(span, from, to, bad);
+        look(span, from, in_lo, bad);
+        look(span, in_hi, to, bad);
+    }
+};
+
+// x.y over N pairs of rows of a lane's own; elements beyond D count as 0
+template <typename T, int N>
+__device__ __forceinline__ void row_dots(const T* const (&x)[N], const T* const (&y)[N], int D, float (&dot)[N])
+{
+    constexpr int kElems = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int n = 0; n < N; ++n) dot[n] = 0.0f;
+    for (int d = 0; d < D; d += 4 * kElems) {
+        vec16 a[N][4], b[N][4];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[n][i] = load_chunk<T, true>(x[n], d + i * kElems, D);
+                b[n][i] = load_chunk<T, true>(y[n], d + i * kElems, D);
+            }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                T u[kElems], w[kElems];
+                __builtin_memcpy(&u, &a[n][i], 16);
+                __builtin_memcpy(&w, &b[n][i], 16);
+#pragma unroll
+                for (int e = 0; e < kElems; ++e) dot[n] = fmaf((float)u[e], (float)w[e], dot[n]);
+            }
+    }
+}
+
+// acc += the sum over n < count of lane n's `weight` times row n, two elements of the rows to a lane (as load_row2 has them)
+template <typename T>
+__device__ __forceinline__ void add_rows(const T* rows, int64_t stride, int count, int D, float weight, float (&acc)[2])
+{
+    constexpr int kRows = sizeof(T) == 2 ? 16 : 8;         // on their way at a time
+    const int d0 = min(lane_id(), D - 1), d1 = min(lane_id() + 64, D - 1);     // (what is beyond a row is stored nowhere)
+    for (int n0 = 0; n0 < count; n0 += kRows) {
+        T x[kRows][2];
+#pragma unroll
+        for (int n = 0; n < kRows; ++n) {
+            const T* row = rows + min(n0 + n, count - 1) * stride;
+            x[n][0] = row[d0];
+            x[n][1] = row[d1];
+        }
+#pragma unroll
+        for (int n = 0; n < kRows; ++n) {
+            if (n0 + n >= count) break;
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), n0 + n));
+            acc[0] = fmaf(w, (float)x[n][0], acc[0]);
+            acc[1] = fmaf(w, (float)x[n][1], acc[1]);
+        }
+    }
+}
+
+// Whether any element of a row that lies in the lanes as load_row2 has it is finite.
+__device__ __forceinline__ bool any_finite(const float (&x)[2], int D)
+{
+    return __any((lane_id() < D && !not_finite(x[0])) || (lane_id() + 64 < D && !not_finite(x[1])));
+}
+
+// One query, at slot `at` of its block, over the keys [lo, hi), by one wavefront: lanes take a key each for the scores, then two
+// elements of the values each.  The result is a mean all along (a sum could leave float32 where the mean does not), NaN where no
+// key has a probability.  m and l as in the kernels: the maximum in units of ln 2, the sum of 2^(s - m).
+template <typename T>
+__device__ __forceinline__ void plain_row(const T* q, const T* k, const T* v, int64_t k_stride, int64_t v_stride, int D, const Score& score, int at, int lo, int hi,
+                          float (&o)[2], float& m, float& l)
+{
     o[0] = o[1] = l = 0.0f;
     m = -INFINITY;
     for (int j0 = lo; j0 < hi; j0 += kWave) {
         const int j = j0 + lane_id();
-        float s = -INFINITY;
+        float s = -INFINITY, keep, qk[1];
         if (j < hi) {
-            const T* row = k + j * k_stride;
-            float dot = 0.0f, keep;
-            for (int d = 0; d < D; d += N) {
-                const vec16 a = load_chunk<T, true>(q, d, D), b = load_chunk<T, true>(row, d, D);
-                T x[N], y[N];
-                __builtin_memcpy(&x, &a, 16);
-                __builtin_memcpy(&y, &b, 16);
-#pragma unroll
-                for (int n = 0; n < N; ++n) dot = fmaf((float)x[n], (float)y[n], dot);
-            }
-            s = score.any<T>(dot, at - j, keep);
+            row_dots<T, 1>({q}, {k + j * k_stride}, D, qk);
+            s = score.any<T>(qk[0], at - j, keep);
         }
         float top = s;
 #pragma unroll
@@ -543,22 +661,10 @@ __device__ void plain_row(const T* q, const T* k, const T* v, int64_t k_stride, 
         m = up;
         l = part + wave_sum(p);
         if (l != l) break;                                 // a score that is no number: nor is anything else
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f, w = p * inv;
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         o[0] *= part * inv;
         o[1] *= part * inv;
-        const int count = min(hi - j0, kWave);
-        for (int n0 = 0; n0 < count; n0 += 4) {
-            float x[4][2];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) load_row2(v + (j0 + min(n0 + n, count - 1)) * v_stride, D, x[n]);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float weight = __shfl(w, n0 + n);
-                if (n0 + n >= count) break;
-                o[0] = fmaf(weight, x[n][0], o[0]);
-                o[1] = fmaf(weight, x[n][1], o[1]);
-            }
-        }
+        if (any_finite(o, D)) add_rows(v + j0 * v_stride, v_stride, min(hi - j0, kWave), D, p * inv, o);
     }
     if (!(l > 0.0f)) o[0] = o[1] = NAN;
 }

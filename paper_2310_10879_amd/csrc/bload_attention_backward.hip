@@ -15,26 +15,30 @@ namespace {
 
 constexpr int kKeys = 64;
 
-// One row of dq from visible keys alone (see forward_row in bload_attention.hip): for rows that come
-// out not finite from the matrix products.
+// One row of dq again, from visible keys alone.
 template <typename T>
-__device__ void dq_row(const AttArgs& a, int b, int head, int i, Span span)
+__device__ __forceinline__ void dq_row(const AttArgs& a, int b, int head, int i, Span span)
 {
     const int D = a.D, kv = head / a.G;
     const Score score(a, head);
     const int64_t at = ((int64_t)b * a.Hq + head) * a.T + i;
     const float lse = a.lse[at] * kLog2e, delta = a.delta[at];
-    float q[2], g[2], acc[2] = {0.0f, 0.0f};
-    load_row2(att_at<T>(a.q, b, i, head), D, q);
-    load_row2(att_at<T>(a.dout, b, i, head), D, g);
-    for (int j = span.lo; j < span.hi; ++j) {
-        float k[2], v[2], keep;
-        load_row2(att_at<T>(a.k, b, j, kv), D, k);
-        load_row2(att_at<T>(a.v, b, j, kv), D, v);
-        const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
-        const float ds = exp2_fast(s - lse) * (wave_sum(g[0] * v[0] + g[1] * v[1]) - delta) * keep;
-        acc[0] += ds * k[0];
-        acc[1] += ds * k[1];
+    const T *q = att_at<T>(a.q, b, i, head), *g = att_at<T>(a.dout, b, i, head);
+    const T *k = att_at<T>(a.k, b, 0, kv), *v = att_at<T>(a.v, b, 0, kv);
+    float acc[2] = {0.0f, 0.0f};
+    for (int j0 = span.lo; j0 < span.hi; j0 += kWave) {
+        const int j = j0 + lane_id();
+        float ds = 0.0f, keep, dot[2];
+        if (j < span.hi) {
+            row_dots<T, 2>({q, g}, {k + j * a.k.st, v + j * a.v.st}, D, dot);
+            const float s = score.any<T>(dot[0], i - j, keep);
+            ds = exp2_fast(s - lse) * (dot[1] - delta) * keep;
+        }
+        if (__any(ds != ds)) {                             // no element of the row is a number
+            acc[0] = acc[1] = NAN;
+            break;
+        }
+        add_rows(k + j0 * a.k.st, a.k.st, min(span.hi - j0, kWave), D, ds, acc);
     }
     store_row2(att_at<T>(a.dq, b, i, head), D, acc[0] * a.scale, acc[1] * a.scale);
 }
@@ -122,8 +126,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
     int buf = 0;
     for (int k0 = lo; k0 < hi; k0 += kKeys, buf ^= 1) {
         if constexpr (sizeof(T) == 4) keep_sums(o);
-        next_k.store(ks[buf]);
-        next_v.store(vs[buf]);
+        next_k.store(ks[buf], hi - k0);
+        next_v.store(vs[buf], hi - k0);
         __syncthreads();
         if (k0 + kKeys < hi) {
             next_k.load(k0 + kKeys, hi);
@@ -195,12 +199,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void attention_dq
                 store4(p, 32 * d + 8 * i + 4 * (lane >> 5), D, y);
             }
     }
-    uint64_t again = __ballot(bad && span.hi > span.lo);
+    if (!__any(bad && span.hi > span.lo)) return;
+    const AttArgs late = args_again();
+    Met met;
+    met.look_around(span, late.T, false, [&](int r) { return row_not_finite(att_at<T>(late.k, b, r, kv), late.D) || row_not_finite(att_at<T>(late.v, b, r, kv), late.D); });
+    uint64_t again = __ballot(bad && span.hi > span.lo && met.hidden);
     again = (again | (again >> 32)) & 0xffffffffu;
     while (again) {
         const int r = __ffsll((unsigned long long)again) - 1;
         again &= again - 1;
-        dq_row<T>(a, b, head, tile * 128 + wave * 32 + r, {__shfl(span.lo, r), __shfl(span.hi, r)});
+        dq_row<T>(late, b, head, __builtin_amdgcn_readlane(row, r), {__builtin_amdgcn_readlane(span.lo, r), __builtin_amdgcn_readlane(span.hi, r)});
     }
 }
 

@@ -36,7 +36,7 @@ __device__ __forceinline__ int decode_length(const DecodeArgs& p, int64_t seq, i
 // One sequence and head again, where the result is not finite: a value that is seen and infinite meets the zeros of a tile's missing
 // keys, and sums of values near the largest float leave float32 (see plain_row).
 template <typename T>
-__device__ void decode_row(const AttArgs& a, int64_t seq, int head, int64_t b, int offset, int n)
+__device__ __forceinline__ void decode_row(const AttArgs& a, int64_t seq, int head, int64_t b, int offset, int n)
 {
     const int kv = head / a.G;
     float o[2], m, l;
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p
         next_v.load(k0, hi);
     }
     for (; k0 < hi; k0 += kWaves * kTileKeys) {
-        next_k.store(ks);
-        next_v.store(vs);
+        next_k.store(ks, kTileKeys);                       // (rows beyond hi as they are: decode_row takes care of what they spoil)
+        next_v.store(vs, kTileKeys);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");

@@ -5,31 +5,38 @@
 namespace bload {
 namespace {
 
-// One row of dk and dv from the queries that see it alone.
+// One row of dk and dv again, from the queries that see it alone.
 template <typename T>
-__device__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
+__device__ __forceinline__ void dkv_row(const AttArgs& a, int b, int kv, int j, Span span)
 {
     const int D = a.D;
-    float k[2], v[2], dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
-    load_row2(att_at<T>(a.k, b, j, kv), D, k);
-    load_row2(att_at<T>(a.v, b, j, kv), D, v);
-    for (int g = 0; g < a.G; ++g) {
+    float dk[2] = {0.0f, 0.0f}, dv[2] = {0.0f, 0.0f};
+    const T *k = att_at<T>(a.k, b, j, kv), *v = att_at<T>(a.v, b, j, kv);
+    // a probability that is no number: no element of the rows is one; a gradient of a score: none of dk
+    bool lost = false, lost_dk = false;
+    for (int g = 0; g < a.G && !lost; ++g) {
         const int head = kv * a.G + g;
         const Score score(a, head);
         const int64_t at = ((int64_t)b * a.Hq + head) * a.T;
-        for (int i = span.lo; i < span.hi; ++i) {
-            float q[2], go[2], keep;
-            load_row2(att_at<T>(a.q, b, i, head), D, q);
-            load_row2(att_at<T>(a.dout, b, i, head), D, go);
-            const float s = score.any<T>(wave_sum(q[0] * k[0] + q[1] * k[1]), i - j, keep);
-            const float p = exp2_fast(s - a.lse[at + i] * kLog2e);
-            const float ds = p * (wave_sum(go[0] * v[0] + go[1] * v[1]) - a.delta[at + i]) * keep;
-            for (int n = 0; n < 2; ++n) {
-                dv[n] += p * go[n];
-                dk[n] += ds * q[n];
+        const T *q = att_at<T>(a.q, b, 0, head), *go = att_at<T>(a.dout, b, 0, head);
+        for (int i0 = span.lo; i0 < span.hi && !lost; i0 += kWave) {
+            const int i = i0 + lane_id();
+            float p = 0.0f, ds = 0.0f, keep, dot[2];
+            if (i < span.hi) {
+                row_dots<T, 2>({k, v}, {q + i * a.q.st, go + i * a.dout.st}, D, dot);
+                p = exp2_fast(score.any<T>(dot[0], i - j, keep) - a.lse[at + i] * kLog2e);
+                ds = p * (dot[1] - a.delta[at + i]) * keep;
             }
+            lost = __any(p != p);
+            lost_dk |= __any(ds != ds);
+            const int count = min(span.hi - i0, kWave);
+            add_rows(go + i0 * a.dout.st, a.dout.st, count, D, p, dv);
+            if (!lost_dk) add_rows(q + i0 * a.q.st, a.q.st, count, D, ds, dk);
+            else if (!any_finite(dv, D)) break;            // (what is lost stays lost)
         }
     }
+    if (lost) dv[0] = dv[1] = NAN;
+    if (lost || lost_dk) dk[0] = dk[1] = NAN;
     store_row2(att_at<T>(a.dk, b, j, kv), D, dk[0] * a.scale, dk[1] * a.scale);
     store_row2(att_at<T>(a.dv, b, j, kv), D, dv[0], dv[1]);
 }
@@ -126,8 +133,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
             keep_sums(dk);
             keep_sums(dv);
         }
-        next_q.store(tiles[buf][0]);
-        next_g.store(tiles[buf][1]);
+        next_q.store(tiles[buf][0], hi - q0);
+        next_g.store(tiles[buf][1], hi - q0);
         if (tid < 2 * kQueries) {
             // (a query that sees nothing has lse -infinity: no part of it may get a probability)
             float z = next_sum;
@@ -297,12 +304,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void 
                 store4(pv, at, D, z);
             }
     }
-    uint64_t again = __ballot(bad && span.hi > span.lo);
+    if (!__any(bad && span.hi > span.lo)) return;
+    const AttArgs late = args_again();
+    Met met;
+    for (int g = 0; g < late.G; ++g) {
+        const int head = kv * late.G + g;
+        const int64_t at = ((int64_t)b * late.Hq + head) * late.T;
+        met.look_around(span, late.T, false, [&](int r) {
+            return not_finite(late.delta[at + r]) || !(late.lse[at + r] < INFINITY) || row_not_finite(att_at<T>(late.q, b, r, head), late.D) ||
+                   row_not_finite(att_at<T>(late.dout, b, r, head), late.D);
+        });
+    }
+    uint64_t again = __ballot(bad && span.hi > span.lo && met.hidden);
     again = (again | (again >> 32)) & 0xffffffffu;
     while (again) {
         const int r = __ffsll((unsigned long long)again) - 1;
         again &= again - 1;
-        dkv_row<T>(a, b, kv, tile * 128 + wave * 32 + r, {__shfl(span.lo, r), __shfl(span.hi, r)});
+        dkv_row<T>(late, b, kv, __builtin_amdgcn_readlane(row, r), {__builtin_amdgcn_readlane(span.lo, r), __builtin_amdgcn_readlane(span.hi, r)});
     }
 }
 

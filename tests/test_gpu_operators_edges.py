@@ -232,3 +232,55 @@ def test_values_near_the_largest(T, n, dtype):
     off = (n + 8) * ref.U32 + 2 * ref.half_step(dtype)
     for x, y in ((got, v[0, :1]), (whole, v[:, :n])):
         assert torch.isfinite(x).all() and ((x.double() / y.double() - 1).abs() <= off).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 90, 128])
+@pytest.mark.parametrize("at", [0, 63, 200, 389])
+def test_one_element_that_is_not_finite(at, D, dtype):
+    """Causally, in one of two sequences: in v or dout it reaches its own element of what depends on it, in q or k all of it, and
+    nothing else changes but for the rounding of what is computed another way."""
+    print(f"one element at {at} D={D} {dtype}", flush=True)
+    bl = binding()
+    T, Hq, Hkv, d = 400, 4, 2, D // 3
+    rng = np.random.default_rng([at, D])
+    q, k, v, g = (ref.draw(rng, (1, T, h, D), dtype).cuda() for h in (Hq, Hkv, Hkv, Hq))
+    reset = torch.zeros((1, T), dtype=torch.uint8, device="cuda")
+    reset[0, 390] = 1
+    mask = bl.bload_segment_mask(reset, torch.ones_like(reset))
+
+    def both(q, k, v, g):
+        out, saved = bl.bload_segment_attention(q, k, v, mask, training=True)
+        return [t[0] for t in (out, *bl.bload_segment_attention_backward(g, q, k, v, out, saved, mask))]
+    clean = both(q, k, v, g)
+    own = torch.arange(T, device="cuda")
+    behind, front, here = (own >= at) & (own < 390), own <= at, own == at
+    heads = {Hq: slice(0, Hq // Hkv), Hkv: slice(0, 1)}                 # those of the first head of keys
+
+    def check(tensors, lost):
+        """lost: which elements of out, dq, dk, dv (rows, elements) of the first head of keys are not finite"""
+        for i, (got, want) in enumerate(zip(both(*tensors), clean)):
+            gone = torch.zeros_like(got, dtype=torch.bool)
+            if lost[i] is not None:
+                rows, elements = lost[i]
+                part = gone[:, heads[got.shape[1]] if lost[4] is None else lost[4] if got.shape[1] == Hq else slice(0, 1)]
+                part[rows] = elements
+            name = f"{('out', 'dq', 'dk', 'dv')[i]}"
+            assert not torch.isfinite(got[gone]).any(), name
+            assert torch.isfinite(got[~gone]).all(), name
+            # either way is within the bound of the other tests; a few steps of the type of sums of some 400 terms
+            off = 32 * ref.half_step(dtype) * (want.float().abs() + 1)
+            assert ((got.float() - want.float()).abs() <= off)[~gone].all(), name
+    every = torch.ones(D, dtype=torch.bool, device="cuda")
+    one = torch.arange(D, device="cuda") == d
+    for value in (float("inf"), float("nan")):
+        x = v.clone()
+        x[0, at, 0, d] = value
+        # (a query that sees it has no delta, so it has no dq, and the keys that it sees have no dk)
+        check((q, k, x, g), ((behind, one), (behind, every), (own < 390, every), None, None))
+        x = g.clone()
+        x[0, at, 0, d] = value
+        check((q, k, v, x), (None, (here, every), (front, every), (front, one), slice(0, 1)))
+    x = q.clone()
+    x[0, at, 0, d] = float("nan")
+    check((x, k, v, g), ((here, every), (here, every), (front, every), (front, every), slice(0, 1)))
