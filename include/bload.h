@@ -62,7 +62,8 @@ typedef enum {
     BLOAD_EALIGN = 4,      /* a payload / workspace base is not 16-byte aligned (32-byte for
                               bload_pack's workspace), or an int32 / int64 table is not
                               naturally aligned */
-    BLOAD_EOVERFLOW = 5,   /* n_seq or num_blocks * t_blk beyond the supported range */
+    BLOAD_EOVERFLOW = 5,   /* n_seq or num_blocks * t_blk beyond the supported range, or more
+                              work than one launch holds (2^24 - 1 workgroups) */
     BLOAD_EHIP = 6         /* a HIP runtime call failed (bload_last_hip_error() says which) */
 } bload_status;
 

@@ -283,7 +283,8 @@ extern "C" bload_status bload_segment_attention_decode(const bload_heads* q, con
     if (!aligned_to(d_block_of_seq, 4) || !aligned_to(d_offset_of_seq, 4) || !aligned_to(d_lengths, 4)) return BLOAD_EALIGN;
     p.column_groups = (int32_t)ceil_div(p.a.G, 32);
     p.splits = decode_splits(n_seq, t_blk, heads_kv, p.column_groups);
-    if (n_seq > (int64_t)0x7fffffff / heads_kv / p.splits / p.column_groups || n_seq > (int64_t)0x7fffffff / heads_q) return BLOAD_EOVERFLOW;
+    if (n_seq > kMaxGroups / heads_kv / p.splits / p.column_groups || (p.splits > 1 && ceil_div(n_seq * heads_q, kThreads / kWave) > kMaxGroups))
+        return BLOAD_EOVERFLOW;
     const size_t need = bload_segment_attention_decode_workspace_bytes(n_seq, t_blk, heads_q, heads_kv, head_dim);
     if (need) {
         if (!d_workspace) return BLOAD_EINVAL;

@@ -27,7 +27,7 @@ inline bload_status att_args(AttArgs& a, int64_t num_blocks, int32_t t_blk, int3
     if (t_blk > (1 << 30) || num_blocks >= ((int64_t)1 << 40) / t_blk) return BLOAD_EOVERFLOW;
     const int64_t tiles = ceil_div(t_blk, rows);
     // one workgroup per tile and head (by division: heads * blocks alone may not fit)
-    if (num_blocks > 0 && tiles > (int64_t)0x7fffffff / heads_q / num_blocks) return BLOAD_EOVERFLOW;
+    if (num_blocks > 0 && tiles > kMaxGroups / heads_q / num_blocks) return BLOAD_EOVERFLOW;
     if (num_blocks > 0 && !d_mask) return BLOAD_EINVAL;
     if (!aligned_to(d_mask, 16) || !aligned_to(d_slopes, 4)) return BLOAD_EALIGN;
     a.mask = reinterpret_cast<const int4*>(d_mask);

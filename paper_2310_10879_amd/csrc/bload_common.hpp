@@ -52,6 +52,10 @@ inline bool aligned_to(const void* p, size_t a)
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0;
 }
 
+// Workgroups of one launch: its threads are counted in 32 bits.  With one more the runtime refuses the launch, and with some
+// numbers beyond it launches what is left of them modulo 2^24 without a word.
+constexpr int64_t kMaxGroups = 0xffffffffLL / kThreads;
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline size_t round_up(size_t a, size_t b) { return (a + b - 1) / b * b; }

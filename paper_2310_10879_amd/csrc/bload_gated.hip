@@ -474,14 +474,14 @@ bload_status gated_run(GatedArgs a, int64_t B, void* workspace, size_t room, hip
         const int V = a.D < kPiece ? 1 : kPiece;
         a.slices = (int32_t)ceil_div(a.D, V);
         const int64_t lanes = B * a.slices, groups = ceil_div(lanes, kThreads);
-        if (groups > 0x7fffffff) return BLOAD_EOVERFLOW;
+        if (groups > kMaxGroups) return BLOAD_EOVERFLOW;
         const dim3 grid((unsigned)groups), block(kThreads);
         if (V == 1) gated_short_kernel<T, 1, BACK><<<grid, block, 0, stream>>>(a, lanes);
         else gated_short_kernel<T, kPiece, BACK><<<grid, block, 0, stream>>>(a, lanes);
         return launch_status();
     }
     const GatedPlan p = gated_plan(B, a.T, a.D);
-    if (p.groups > 0x7fffffff) return BLOAD_EOVERFLOW;
+    if (p.groups > kMaxGroups) return BLOAD_EOVERFLOW;
     if (p.bytes) {
         if (!workspace) return BLOAD_EINVAL;
         if (!aligned_to(workspace, 16)) return BLOAD_EALIGN;

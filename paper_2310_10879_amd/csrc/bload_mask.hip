@@ -147,7 +147,7 @@ extern "C" bload_status bload_segment_mask(const uint8_t* d_reset, const uint8_t
     if (!d_reset || !d_valid || !d_mask) return BLOAD_EINVAL;
     if (!aligned_to(d_mask, 16) || !aligned_to(d_seq_id, 4) || !aligned_to(d_prefix, 4)) return BLOAD_EALIGN;
     const int64_t tiles = ceil_div(t_blk, kMaskTile), groups = num_blocks * tiles;
-    if (groups > 0x7fffffff) return BLOAD_EOVERFLOW;
+    if (groups > kMaxGroups) return BLOAD_EOVERFLOW;
     const MaskArgs a = {d_reset, d_valid, d_seq_id, d_prefix, reinterpret_cast<int4*>(d_mask), n_seq, t_blk, (int32_t)tiles, causal};
     segment_mask_kernel<<<dim3((unsigned)groups), dim3(kThreads), 0, (hipStream_t)hip_stream>>>(a);
     return launch_status();

@@ -181,7 +181,7 @@ extern "C" bload_status bload_rotary(const bload_heads* x, const int32_t* d_posi
     a.by_heads = magic(heads_each);
     a.by_pairs = magic(rot_dim / 2);
     const int64_t groups = ceil_div(a.slots, each), parts = ceil_div(heads, heads_each);
-    if (groups > 0x7fffffff || parts > 65535) return BLOAD_EOVERFLOW;
+    if (groups > kMaxGroups || parts > 65535) return BLOAD_EOVERFLOW;
     const dim3 grid((unsigned)groups, (unsigned)parts);
     if (dtype == BLOAD_F16) rotary_launch<att_half>(a, grid, half, (hipStream_t)hip_stream);
     else if (dtype == BLOAD_BF16) rotary_launch<att_bf16>(a, grid, half, (hipStream_t)hip_stream);

@@ -1,7 +1,7 @@
 """Further refusals of the model's operators, answered on the host before anything is launched (no GPU)."""
 import torch
 
-from test_operators_refuse import EINVAL, EWORKSPACE, F16, P, bl  # noqa: F401
+from test_operators_refuse import EINVAL, EOVERFLOW, EWORKSPACE, F16, P, bl, heads  # noqa: F401
 
 BIG = 1 << 40
 
@@ -27,3 +27,21 @@ def test_gated_states_that_meet(bl):
         for t in (1, 8):
             assert f(BIG, BIG + 4, t) == f(BIG + size - 4, BIG, t) == EINVAL
         assert f(BIG, BIG + size, 5000) == f(BIG + size, BIG, 5000) == f(BIG, None, 5000) == EWORKSPACE
+
+
+def test_more_workgroups_than_a_launch_holds(bl):
+    """2^24 workgroups of 256 threads and more, which is beyond the 32 bits of a launch's grid: with a few numbers beyond them only
+    the rest modulo 2^24 would run, and the call would say that all is well."""
+    lib, h, most = bl._lib, heads(bl), 1 << 24
+    for more in (0, 5, most):
+        n = most + more
+        assert lib.bload_segment_mask(P, P, None, n, 1, 1, None, 0, P, None) == EOVERFLOW
+        assert lib.bload_segment_mask(P, P, None, (n + 1) // 2, 1025, 1, None, 0, P, None) == EOVERFLOW
+        for B, T, H in ((n, 100, 1), ((n + 15) // 16, 100, 16), ((n + 31) // 32, 129, 16)):
+            assert lib.bload_segment_attention(h, h, h, P, B, T, H, 1, 64, F16, 0.1, 0.0, None, h, None, None, None) == EOVERFLOW
+            assert lib.bload_segment_attention_backward(h, h, h, h, h, P, None, P, B, T, H, 1, 64, F16, 0.1, 0.0, None, h, h, h, P, BIG, None) == EOVERFLOW
+        assert lib.bload_segment_attention_decode(h, h, h, P, P, P, (n + 7) // 8, 4, 100, 8, 8, 64, F16, 0.1, 0.0, None, h, P, BIG, None) == EOVERFLOW
+        assert lib.bload_gated_scan(P, P, P, P, n, 1, 1024, F16, None, P, None, None, 0, None) == EOVERFLOW
+        assert lib.bload_gated_scan(P, P, P, P, n, 9, 4, F16, None, P, None, None, 0, None) == EOVERFLOW
+        assert lib.bload_gated_scan_backward(P, P, P, P, P, n, 1, 1024, F16, None, None, P, P, None, None, 0, None) == EOVERFLOW
+        assert lib.bload_rotary(h, P, n, 1, 40, 128, F16, P, 128, 0, 1.0, 0, h, None) == EOVERFLOW
