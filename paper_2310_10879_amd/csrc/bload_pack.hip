@@ -1215,6 +1215,7 @@ bload_status pack_enqueue(const PackLayout& l, const void* d_src, const int64_t*
     const int64_t wanted = once ? 1 : ceil_div(frame_bytes < 64 ? 1024 : 4096, l.tiles);
     const int32_t parts = (int32_t)(frame_bytes == 4 && aligned_to(d_src, 4) ? 1 : wanted < vectors ? wanted : vectors);
     const bool two_passes = frame_bytes == 4 && aligned_to(d_src, 4) && a.total_slots >= kTablePassFromSlots;
+    if ((two_passes && !l.wide ? ceil_div(l.tiles, kPassGroup) : l.tiles) > kMaxGroups) return BLOAD_EOVERFLOW;
 
     const PlanTables t{d_src_offsets, d_lengths, d_order, d_block_of_seq, d_offset_of_seq, d_block_first};
     if (l.wide && l.tiles <= kDirectTiles) {

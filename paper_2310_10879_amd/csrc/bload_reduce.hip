@@ -1983,6 +1983,13 @@ static void launch_flat(const ReducePlan& p, const ReduceArgs& a, hipStream_t st
     hipLaunchKernelGGL((reduce_flat_kernel<ElemT, STREAM>), dim3((uint32_t)p.total_chunks), dim3(kThreads), lds, stream, a);
 }
 
+// Chunks that a workgroup of the stitch takes, and its workgroups.
+static int32_t stitch_chunks(int64_t feat_dim) { return feat_dim >= kThreads ? 1 : (int32_t)(kThreads / feat_dim); }
+static int64_t stitch_groups(const ReducePlan& p, int64_t feat_dim)
+{
+    return stitch_chunks(feat_dim) > 1 ? ceil_div(p.total_chunks, stitch_chunks(feat_dim)) : p.total_chunks * ceil_div(feat_dim, kThreads);
+}
+
 template <typename ElemT>
 static void launch_reduce(const ReducePlan& p, const ReduceArgs& a, hipStream_t stream)
 {
@@ -2013,10 +2020,8 @@ static void launch_reduce(const ReducePlan& p, const ReduceArgs& a, hipStream_t 
     }
     if (p.partials) {
         const int32_t feat_tiles = (int32_t)ceil_div(a.feat_dim, kThreads);
-        const int32_t chunks_per_wg = a.feat_dim >= kThreads ? 1 : kThreads / a.feat_dim;
-        const int64_t groups = chunks_per_wg > 1 ? ceil_div(p.total_chunks, chunks_per_wg)
-                                                 : p.total_chunks * feat_tiles;
-        const dim3 grid((uint32_t)groups), block(kThreads);
+        const int32_t chunks_per_wg = stitch_chunks(a.feat_dim);
+        const dim3 grid((uint32_t)stitch_groups(p, a.feat_dim)), block(kThreads);
         if (p.pair_parts)
             hipLaunchKernelGGL((reduce_stitch_kernel<Acc, typename WideSum<Acc>::T>), grid, block, 0, stream, a, feat_tiles, chunks_per_wg);
         else
@@ -2073,6 +2078,10 @@ extern "C" bload_status bload_segment_reduce(const void* d_packed, const int32_t
     if (p.total_chunks * ceil_div(feat_dim, kThreads) > INT32_MAX) return BLOAD_EOVERFLOW;
     if (p.wide && ceil_div(p.total_chunks, (kThreads >> p.row_lanes_log2) >> p.split) *
                       ceil_div(p.n_vec, 1 << p.row_lanes_log2) > INT32_MAX)
+        return BLOAD_EOVERFLOW;
+    const int64_t feat_tiles = ceil_div(p.n_vec, (int64_t)1 << p.row_lanes_log2);
+    if ((p.wide ? ceil_div(p.total_chunks, (kThreads >> p.row_lanes_log2) >> p.split) * feat_tiles : p.total_chunks) > kMaxGroups ||
+        (p.partials && stitch_groups(p, feat_dim) > kMaxGroups))
         return BLOAD_EOVERFLOW;
     if (p.partials) {
         if (!d_workspace) return BLOAD_EINVAL;

@@ -890,7 +890,7 @@ extern "C" bload_status bload_segment_scan(const void* d_packed, const uint8_t* 
         }
         p = scan_plan(num_blocks, t_blk, feat_dim, scan_elem_bytes(dtype), true);
     }
-    if (p.grid > 0x7fffffffLL) return BLOAD_EOVERFLOW;
+    if (p.grid > kMaxGroups) return BLOAD_EOVERFLOW;
 
     ScanArgs a{};
     a.packed = static_cast<const uint8_t*>(d_packed);

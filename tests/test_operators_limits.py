@@ -1,7 +1,8 @@
-"""Further refusals of the model's operators, answered on the host before anything is launched (no GPU)."""
+"""Further refusals, answered on the host before anything is launched (no GPU): of the model's operators, and of more work than a
+launch holds by all entry points."""
 import torch
 
-from test_operators_refuse import EINVAL, EOVERFLOW, EWORKSPACE, F16, P, bl, heads  # noqa: F401
+from test_operators_refuse import EINVAL, EOVERFLOW, EWORKSPACE, F16, F32, P, bl, heads  # noqa: F401
 
 BIG = 1 << 40
 
@@ -45,3 +46,16 @@ def test_more_workgroups_than_a_launch_holds(bl):
         assert lib.bload_gated_scan(P, P, P, P, n, 9, 4, F16, None, P, None, None, 0, None) == EOVERFLOW
         assert lib.bload_gated_scan_backward(P, P, P, P, P, n, 1, 1024, F16, None, None, P, P, None, None, 0, None) == EOVERFLOW
         assert lib.bload_rotary(h, P, n, 1, 40, 128, F16, P, 128, 0, 1.0, 0, h, None) == EOVERFLOW
+
+
+def test_more_workgroups_than_a_launch_holds_on_the_packing_path(bl):
+    """The packed tensor in 4 KiB tiles is 64 GiB from there on; reductions and scans of more than 2^24 chunks."""
+    lib, room = bl._lib, 1 << 50
+    for n in (1 << 20, (1 << 20) + 1, 1 << 21):
+        assert lib.bload_pack(P, P, P, P, P, P, P, n, n, 16, 4096, P, P, P, P, P, P, room, None) == EOVERFLOW
+        assert lib.bload_pack_noalloc(P, P, P, P, P, P, P, n, n, 16, 4096, P, P, P, P, P, None) == EOVERFLOW
+    B = 1 << 24
+    for dtype in (0, F16, F32):
+        assert lib.bload_segment_scan(P, P, P, B, 2048, 64, dtype, 0.5, P, P, room, None) == EOVERFLOW
+        for T, F in ((2048, 64), (16, 16384)):
+            assert lib.bload_segment_reduce(P, P, P, P, B, T, F, dtype, 0, 1000, P, P, room, None) == EOVERFLOW
