@@ -8,6 +8,9 @@ There is no fallback: importing this module without the built library raises.
 from __future__ import annotations
 
 import ctypes
+import itertools
+import math
+import operator
 import os
 from dataclasses import dataclass
 
@@ -474,13 +477,21 @@ def _heads(t: torch.Tensor, shape, dtype, name: str) -> Heads:
     return Heads(t.data_ptr(), stride[0], stride[1] if len(stride) == 4 else 0, stride[-2])
 
 
-def _sized(t: torch.Tensor | None, numel: int, dtype, name: str) -> int:
+def _merges(got, shape) -> bool:
+    """Whether `got` is `shape` with neighbouring dimensions taken together, or with some of 1 more or less: the same elements
+    in the same order, other than a transposed tensor of as many."""
+    ends = set(itertools.accumulate(reversed(shape), operator.mul, initial=1))
+    return math.prod(got) == math.prod(shape) and ends.issuperset(itertools.accumulate(reversed(got), operator.mul))
+
+
+def _sized(t: torch.Tensor | None, shape, dtype, name: str) -> int:
+    """A contiguous tensor of this shape, dimensions taken together or not; None: no pointer."""
     if t is None:
         return 0
-    if t.dtype is dtype and t.numel() == numel and t.is_cuda and t.is_contiguous():
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
         return t.data_ptr()                        # (the checks below at half their price: small calls are all host time)
-    if t.numel() != numel:
-        raise ValueError(f"{name}: expected {numel} elements, got {t.numel()}")
+    if not _merges(t.shape, shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     return _ptr(t, dtype)
 
 
@@ -505,7 +516,7 @@ def bload_segment_mask(reset: torch.Tensor, valid: torch.Tensor, causal: bool = 
     n = 0 if prefix is None else prefix.shape[0]
     _check(_lib.bload_segment_mask(_ptr(reset, torch.uint8), _ptr(valid, torch.uint8),
                                    0 if prefix is None else _ptr(seq_id, torch.int32), B, T, int(causal), _ptr(prefix, torch.int32),
-                                   n, _sized(out, B * T * 4, torch.int32, "out"), _stream()))
+                                   n, _sized(out, (B, T, 4), torch.int32, "out"), _stream()))
     return out
 
 
@@ -535,8 +546,8 @@ def bload_segment_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, m
     if training:
         saved = Saved(q.new_empty((B, Hq, T), dtype=torch.float32), None if dtype == torch.float32 else q.new_empty((B, T, Hq, D)))
         hr = None if saved.rest is None else _heads(saved.rest, q.shape, dtype, "rest")
-    _check(_lib.bload_segment_attention(hq, hk, hv, _sized(mask, B * T * 4, torch.int32, "mask"), B, T, Hq, Hkv, D, code,
-                                        D ** -0.5 if scale is None else scale, cap, _sized(slopes, Hq, torch.float32, "slopes"),
+    _check(_lib.bload_segment_attention(hq, hk, hv, _sized(mask, (B, T, 4), torch.int32, "mask"), B, T, Hq, Hkv, D, code,
+                                        D ** -0.5 if scale is None else scale, cap, _sized(slopes, (Hq,), torch.float32, "slopes"),
                                         _heads(out, q.shape, dtype, "out"), saved.lse.data_ptr() if training else 0, hr, _stream()))
     return (out, saved) if training else out
 
@@ -562,9 +573,9 @@ def bload_segment_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: tor
     hr = None if saved.rest is None else _heads(saved.rest, q.shape, dtype, "rest")
     _check(_lib.bload_segment_attention_backward(
         _heads(dout, q.shape, dtype, "dout"), _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
-        _heads(out, q.shape, dtype, "out"), _sized(saved.lse, B * Hq * T, torch.float32, "lse"), hr,
-        _sized(mask, B * T * 4, torch.int32, "mask"), B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
-        _sized(slopes, Hq, torch.float32, "slopes"), _heads(dq, q.shape, dtype, "dq"), _heads(dk, shape, dtype, "dk"),
+        _heads(out, q.shape, dtype, "out"), _sized(saved.lse, (B, Hq, T), torch.float32, "lse"), hr,
+        _sized(mask, (B, T, 4), torch.int32, "mask"), B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
+        _sized(slopes, (Hq,), torch.float32, "slopes"), _heads(dq, q.shape, dtype, "dq"), _heads(dk, shape, dtype, "dk"),
         _heads(dv, shape, dtype, "dv"), _ptr(workspace), _room(workspace), _stream()))
     return dq, dk, dv
 
@@ -592,9 +603,9 @@ def bload_segment_attention_decode(q: torch.Tensor, k: torch.Tensor, v: torch.Te
     shape = (B, T, Hkv, D)
     _check(_lib.bload_segment_attention_decode(
         _heads(q, q.shape, dtype, "q"), _heads(k, shape, dtype, "k"), _heads(v, shape, dtype, "v"),
-        _sized(block_of_seq, n, torch.int32, "block_of_seq"), _sized(offset_of_seq, n, torch.int32, "offset_of_seq"),
-        _sized(lengths, n, torch.int32, "lengths"), n, B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
-        _sized(slopes, Hq, torch.float32, "slopes"), _heads(out, q.shape, dtype, "out"), _ptr(workspace), _room(workspace),
+        _sized(block_of_seq, (n,), torch.int32, "block_of_seq"), _sized(offset_of_seq, (n,), torch.int32, "offset_of_seq"),
+        _sized(lengths, (n,), torch.int32, "lengths"), n, B, T, Hq, Hkv, D, code, D ** -0.5 if scale is None else scale, cap,
+        _sized(slopes, (Hq,), torch.float32, "slopes"), _heads(out, q.shape, dtype, "out"), _ptr(workspace), _room(workspace),
         _stream()))
     return out
 
@@ -616,15 +627,15 @@ def bload_gated_scan(gate: torch.Tensor, x: torch.Tensor, reset: torch.Tensor, v
     [B, T, D] of float16, bfloat16 or float32; h0 (float32[B, D]): the state in front of the blocks.  Returns h and
     the state behind the last slots (float32[B, D]).  Asynchronous on the current stream."""
     B, T, D = x.shape
-    dtype, code, n = x.dtype, _type_code(x), x.numel()
+    dtype, code, shape = x.dtype, _type_code(x), x.shape
     if out is None:
         out = x.new_empty((B, T, D))
     if state is None:
         state = x.new_empty((B, D), dtype=torch.float32)
     workspace = _gated_workspace(workspace, B, T, D, code, x.device)
-    _check(_lib.bload_gated_scan(_sized(gate, n, dtype, "gate"), _ptr(x), _sized(reset, B * T, torch.uint8, "reset"),
-                                 _sized(valid, B * T, torch.uint8, "valid"), B, T, D, code, _sized(h0, B * D, torch.float32, "h0"),
-                                 _sized(out, n, dtype, "out"), _sized(state, B * D, torch.float32, "state"), _ptr(workspace),
+    _check(_lib.bload_gated_scan(_sized(gate, shape, dtype, "gate"), _ptr(x), _sized(reset, (B, T), torch.uint8, "reset"),
+                                 _sized(valid, (B, T), torch.uint8, "valid"), B, T, D, code, _sized(h0, (B, D), torch.float32, "h0"),
+                                 _sized(out, shape, dtype, "out"), _sized(state, (B, D), torch.float32, "state"), _ptr(workspace),
                                  _room(workspace), _stream()))
     return out, state
 
@@ -635,16 +646,16 @@ def bload_gated_scan_backward(dout: torch.Tensor, gate: torch.Tensor, out: torch
     """Gradients (dgate, dx, dh0) of sum(out * dout) + sum(state * dstate); out is the forward call's result.
     grads: three tensors to write into.  Asynchronous on the current stream."""
     B, T, D = dout.shape
-    dtype, code, n = dout.dtype, _type_code(dout), dout.numel()
+    dtype, code, shape = dout.dtype, _type_code(dout), dout.shape
     if grads is None:
         grads = dout.new_empty((B, T, D)), dout.new_empty((B, T, D)), dout.new_empty((B, D), dtype=torch.float32)
     dgate, dx, dh0 = grads
     workspace = _gated_workspace(workspace, B, T, D, code, dout.device)
-    _check(_lib.bload_gated_scan_backward(_ptr(dout), _sized(gate, n, dtype, "gate"), _sized(out, n, dtype, "out"),
-                                          _sized(reset, B * T, torch.uint8, "reset"), _sized(valid, B * T, torch.uint8, "valid"),
-                                          B, T, D, code, _sized(h0, B * D, torch.float32, "h0"),
-                                          _sized(dstate, B * D, torch.float32, "dstate"), _sized(dgate, n, dtype, "dgate"),
-                                          _sized(dx, n, dtype, "dx"), _sized(dh0, B * D, torch.float32, "dh0"), _ptr(workspace),
+    _check(_lib.bload_gated_scan_backward(_ptr(dout), _sized(gate, shape, dtype, "gate"), _sized(out, shape, dtype, "out"),
+                                          _sized(reset, (B, T), torch.uint8, "reset"), _sized(valid, (B, T), torch.uint8, "valid"),
+                                          B, T, D, code, _sized(h0, (B, D), torch.float32, "h0"),
+                                          _sized(dstate, (B, D), torch.float32, "dstate"), _sized(dgate, shape, dtype, "dgate"),
+                                          _sized(dx, shape, dtype, "dx"), _sized(dh0, (B, D), torch.float32, "dh0"), _ptr(workspace),
                                           _room(workspace), _stream()))
     return dgate, dx, dh0
 
@@ -667,7 +678,7 @@ def bload_rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Te
     code = _type_code(x)
     if out is None:
         out = x.new_empty((B, T, H, D))
-    _check(_lib.bload_rotary(_heads(x, x.shape, x.dtype, "x"), _sized(positions, B * T, torch.int32, "positions"), B, T, H, D, code,
+    _check(_lib.bload_rotary(_heads(x, x.shape, x.dtype, "x"), _sized(positions, (B, T), torch.int32, "positions"), B, T, H, D, code,
                              _ptr(frequencies, torch.float32), 2 * frequencies.shape[0], ROTARY_LAYOUTS[layout], scale, int(inverse),
                              _heads(out, x.shape, x.dtype, "out"), _stream()))
     return out

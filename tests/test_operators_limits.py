@@ -1,5 +1,6 @@
 """Further refusals, answered on the host before anything is launched (no GPU): of the model's operators, and of more work than a
 launch holds by all entry points."""
+import pytest
 import torch
 
 from test_operators_refuse import EINVAL, EOVERFLOW, EWORKSPACE, F16, F32, P, bl, heads  # noqa: F401
@@ -59,3 +60,32 @@ def test_more_workgroups_than_a_launch_holds_on_the_packing_path(bl):
         assert lib.bload_segment_scan(P, P, P, B, 2048, 64, dtype, 0.5, P, P, room, None) == EOVERFLOW
         for T, F in ((2048, 64), (16, 16384)):
             assert lib.bload_segment_reduce(P, P, P, P, B, T, F, dtype, 0, 1000, P, P, room, None) == EOVERFLOW
+
+
+def test_binding_takes_no_other_order_of_dimensions(bl):
+    """A tensor of as many elements in another order is refused before it is looked at; dimensions may be taken together."""
+    B, T, D = 3, 10, 16
+    byte = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    word = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    real = lambda *shape: torch.zeros(shape)
+
+    def refused(t, shape, dtype):
+        with pytest.raises(ValueError, match="expected shape"):
+            bl._sized(t, shape, dtype, "it")
+
+    def taken(t, shape, dtype):                              # (as far as the check of the device: these lie on the host)
+        with pytest.raises(ValueError, match="expected a device tensor"):
+            bl._sized(t, shape, dtype, "it")
+    for t in (word(T, B, 4), word(B, 4, T), word(4, B, T), word(B, T, 3), word(B, T), word(T, B * 4)):
+        refused(t, (B, T, 4), torch.int32)
+    for t in (word(B, T, 4), word(B * T, 4), word(B, T * 4), word(B * T * 4), word(1, B, T, 1, 4)):
+        taken(t, (B, T, 4), torch.int32)
+    for t in (real(B, D, T), real(T, B, D), real(D, B * T)):
+        refused(t, (B, T, D), torch.float32)
+    for t in (real(B, T, D), real(B * T, D), real(B, 1, T, D)):
+        taken(t, (B, T, D), torch.float32)
+    refused(byte(T, B), (B, T), torch.uint8)
+    taken(byte(B, T), (B, T), torch.uint8)
+    refused(real(D, B), (B, D), torch.float32)
+    taken(real(B, 1, D), (B, D), torch.float32)
+    assert bl._sized(None, (B, T), torch.uint8, "it") == 0
