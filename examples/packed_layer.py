@@ -19,6 +19,11 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2310_10879_amd import bload  # noqa: E402
 
 
+def side_by_side(dout):
+    """A gradient as the operators take it: the elements of a head next to each other.  (That of a sum is one element everywhere.)"""
+    return dout if dout.stride(-1) == 1 else dout.contiguous()
+
+
 class Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, positions, frequencies):
@@ -27,7 +32,7 @@ class Rotary(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dout):
-        return bload.bload_rotary(dout, *ctx.saved_tensors, inverse=True), None, None
+        return bload.bload_rotary(side_by_side(dout), *ctx.saved_tensors, inverse=True), None, None
 
 
 class SegmentAttention(torch.autograd.Function):
@@ -40,7 +45,7 @@ class SegmentAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, mask = ctx.saved_tensors
-        return (*bload.bload_segment_attention_backward(dout, q, k, v, out, ctx.kept, mask), None)
+        return (*bload.bload_segment_attention_backward(side_by_side(dout), q, k, v, out, ctx.kept, mask), None)
 
 
 class GatedScan(torch.autograd.Function):

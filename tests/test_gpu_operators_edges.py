@@ -1,4 +1,7 @@
 """The model's operators at the edges of what their callers may do, on the GPU."""
+import os
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -7,6 +10,8 @@ import operators_reference as ref
 from gpu_util import binding, to_dev
 
 pytestmark = pytest.mark.gpu
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
 
 
 # rows that are no whole number of a lane's elements: their last lane and its neighbour meet at the borders of wavefronts and workgroups
@@ -284,3 +289,24 @@ def test_one_element_that_is_not_finite(at, D, dtype):
     x = q.clone()
     x[0, at, 0, d] = float("nan")
     check((x, k, v, g), ((here, every), (here, every), (front, every), (front, every), slice(0, 1)))
+
+
+def test_example_takes_the_gradient_of_a_sum():
+    """It is one element with strides of 0; the gradients are those of ones."""
+    import packed_layer
+    bl = binding()
+    B, T, H, D = 2, 40, 2, 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    one = torch.ones((B, T), dtype=torch.uint8, device="cuda")
+    mask, reset = bl.bload_segment_mask(torch.zeros_like(one), one), torch.zeros_like(one)
+    at = torch.arange(B * T, dtype=torch.int32, device="cuda").view(B, T)
+    freq = bl.bload_rotary_frequencies(D).cuda()
+    new = lambda *shape: torch.rand(shape, device="cuda", generator=g).requires_grad_()
+    x, q, k, v, gate, y = new(B, T, H, D), new(B, T, H, D), new(B, T, H, D), new(B, T, H, D), new(B, T, D), new(B, T, D)
+    for f, leaves in ((lambda: packed_layer.Rotary.apply(x, at, freq), (x,)),
+                      (lambda: packed_layer.SegmentAttention.apply(q, k, v, mask), (q, k, v)),
+                      (lambda: packed_layer.GatedScan.apply(gate, y, reset, one), (gate, y))):
+        out = f()
+        want = torch.autograd.grad(out, leaves, torch.ones_like(out), retain_graph=True)
+        got = torch.autograd.grad(out.sum(), leaves)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
