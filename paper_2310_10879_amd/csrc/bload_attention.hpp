@@ -428,8 +428,9 @@ struct Maximum {
 
 // Gradients of scores, p (dp - delta), may lie anywhere in the range of dout, and far below it where a row sees many: float16 would
 // lose them among its subnormals, or overflow.  They are packed as a multiple `by` of themselves, a power of two for each row of results:
-// the row's first one that is not 0 brings the largest of its tile between 2^12 and 2^13, and one that passes 2^15 does so again; the
-// row's sums shrink along.  Measured: 16 blocks of 3000 short recordings, 16 heads of 128: dq 413 -> 419 us, dk and dv 535 -> 569.
+// the first ones that are not 0 bring the largest of its tile between 2^6 and 2^7, and one that passes 2^15 does so again; the
+// row's sums shrink along.  Measured: 16 blocks of 3000 short recordings, 16 heads of 128: dq 413 -> 416 us, dk and dv 535 -> 552 (569
+// from 2^12 on: more rows whose sums have to shrink).
 struct Reach {
     enum { kNone = 0, kFirst, kSums };
     float by = 1.0f, limit = 0.0f;
@@ -442,7 +443,7 @@ struct Reach {
         bool held = false;
         if (top > limit) {
             held = limit > 0.0f;
-            f = ldexpf(1.0f, min(13 - __builtin_amdgcn_frexp_expf(top), 64));     // (times any dp, below 2^41: far inside float32)
+            f = ldexpf(1.0f, min(7 - __builtin_amdgcn_frexp_expf(top), 64));     // (times any dp, below 2^41: far inside float32)
             by *= f;
             limit = 0x1p15f;
         }

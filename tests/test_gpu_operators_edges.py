@@ -99,9 +99,11 @@ def test_large_and_small_caps(cap, size, dtype):
 
 
 def gradients(T, dtype, starts, causal, q, k, v, g, where=None):
-    """dq, dk and dv of one block of sequences that begin at `starts`, with one head of keys and a scale of 1, against 64 bits, with bounds that hold over the whole range of a type: a gradient of a
-    score, p (dp - delta), keeps half a step of the type however small dout is, down to 2^-37 of the row's largest dp - delta (float16 packs it
-    as a multiple: 2^-25 is half of its smallest number, the row's largest lies above 2^12), a probability down to 2^-37.  where: the slots to compare."""
+    """dq, dk and dv of one block of sequences that begin at `starts`, with one head of keys and a scale of 1, against 64 bits, with
+    bounds that hold over the whole range of a type: a gradient of a score, p (dp - delta), keeps half a step of the type however small dout is.
+    (float16 packs it as a multiple, the row's largest above 2^6 and float16's smallest normal number 2^-14: the step holds down to 2^-20 of
+    the row's largest, where these inputs lie; the bound's 2^-37 of the largest dp - delta is stricter than what holds below.)
+    A probability keeps it down to 2^-37.  where: the slots to compare."""
     bl = binding()
     H, D, scale = q.shape[2], q.shape[3], 1.0
     at = np.arange(T)
