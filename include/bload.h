@@ -13,6 +13,10 @@
  *                         write the per-slot form of the start table
  *   bload_segment_reduce  per-sequence sum / mean over the packed blocks, using
  *                         only the packed tensor and that per-slot table
+ * for the model that trains on the blocks and serves from them,
+ *   bload_segment_mask, bload_segment_attention (_backward, _decode)
+ *   bload_rotary, bload_rotary_frequencies
+ *   bload_gated_scan (_backward)
  * and, around that path,
  *   bload_plan_random_fit   the plan built with the sampler of the paper's pseudocode
  *   bload_plan_shard        one data-parallel worker's share of a plan
@@ -30,8 +34,8 @@
  *   - A frame is an opaque record of `frame_bytes` bytes (H*W*C*sizeof(elem));
  *     H and W are the same for all sequences of one call.
  *   - `hip_stream` is a hipStream_t passed as void* (NULL = the null stream).
- *     bload_pack, bload_segment_reduce and bload_segment_scan only enqueue work
- *     on it (no synchronisation, no allocation: they can be recorded into a HIP
+ *     bload_pack, bload_segment_reduce, bload_segment_scan and the model's operators only
+ *     enqueue work on it (no synchronisation, no allocation: they can be recorded into a HIP
  *     graph); the planners and bload_strategy_counts enqueue, then wait for the
  *     stream, because they return counts to the host.
  *   - Every function returns a bload_status; nothing is thrown.  On any
@@ -412,7 +416,10 @@ bload_status bload_segment_mask(const uint8_t* d_reset, const uint8_t* d_valid, 
  *     s = scale q_i.k_j;   with cap > 0: s = cap tanh(s / cap);   s = s - slope |i - j|
  *     out_i = sum_j softmax_j(s) v_j over the keys that the mask lets i see
  * A row that sees nothing (padding) is 0 and its lse -infinity.  What is not seen has no
- * part in a result, infinite or NaN as it may be.
+ * part in a result, infinite or NaN as it may be.  (That takes time: rows whose neighbours in
+ * the block, up to 127 slots from what they see, are not finite are computed again one by one;
+ * 127 of them that see 2048 slots each take some 60 ms.)  A value that is seen and infinite makes
+ * its element of the result infinite, or NaN where its probability is 0 in the type.
  *
  * dtype      F16, BF16 or F32 (of q, k, v and out); head_dim 1 .. BLOAD_ATTENTION_MAX_HEAD_DIM
  * scale      > 0;  cap >= 0 (0: none; from 2^100 on all alike);  d_slopes  in  float32[heads_q] or NULL
@@ -482,7 +489,7 @@ bload_status bload_segment_attention_decode(const bload_heads* q, const bload_he
  * d_gate, d_x  in   [B, t_blk, feat_dim] of `dtype` (F16, BF16 or F32), aligned to an element
  * d_reset, d_valid  in  uint8[B, t_blk]
  * d_state_in   in   float32[B, feat_dim] or NULL (no state: the first slot starts a sequence)
- * d_out        out  [B, t_blk, feat_dim] of `dtype`: h; every element is written
+ * d_out        out  [B, t_blk, feat_dim] of `dtype`: h; every element is written; overlaps no input
  * d_state_out  out  float32[B, feat_dim] or NULL: h of the last slot, unrounded; may be
  *                   d_state_in where t_blk <= 8, and is refused (BLOAD_EINVAL) where it meets
  *                   d_state_in in any other way
@@ -499,7 +506,8 @@ bload_status bload_gated_scan(const void* d_gate, const void* d_x, const uint8_t
                               void* d_out, float* d_state_out, void* d_workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradients of sum(out * dout) + sum(state_out * dstate_out) by gate, x and state_in.
- * d_out, d_state_in  in   of the forward pass;  d_dstate_out  in  float32[B, feat_dim] or NULL
+ * d_out, d_state_in  in   of the forward pass; dgate is formed with the rounded states of d_out
+ * d_dstate_out       in   float32[B, feat_dim] or NULL
  * d_dgate, d_dx      out  [B, t_blk, feat_dim] of `dtype`, every element written, overlapping no input
  * d_dstate_in        out  float32[B, feat_dim] or NULL (0 where the first slot does not go on); may be
  *                         d_dstate_out or d_state_in where t_blk <= 8, else refused where it meets one */

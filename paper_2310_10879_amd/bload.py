@@ -461,6 +461,9 @@ def bload_pack_tile_bytes(n_seq: int, num_blocks: int, t_blk: int, frame_bytes: 
 
 
 # ---- operators on packed blocks whose element type is the tensors' own -------------------------
+#
+# Their results carry no gradient, whatever requires one: a backward pass is a call of its own (examples/packed_layer.py wraps each
+# pair in a torch.autograd.Function).
 
 
 def _heads(t: torch.Tensor, shape, dtype, name: str) -> Heads:

@@ -31,8 +31,8 @@ __device__ __forceinline__ void forward_row(const AttArgs& a, int b, int head, i
 // A workgroup takes 128 queries of one head, a wavefront 32 of them (they stay in its registers, as does O^T);
 // tiles of keys and values go through LDS, two tiles deep, the next one on its way from memory
 // while the present one is multiplied.
-// Measured: 8 blocks of 4096 bfloat16, 32 heads of 128 over 8, causal: 1.42 ms, 790 TFLOP/s (a product of 8192 x 8192 matrices reaches
-// 1204 on that card).  Matrix units are busy for 41 % of the cycles, vector units for 49 (exponentials), LDS for 41, at 1.9 GHz: the
+// Measured: 8 blocks of 4096 bfloat16, 32 heads of 128 over 8, causal: 1.45 ms, 760 TFLOP/s (a product of 8192 x 8192 matrices reaches
+// 1200 on that card).  Matrix units are busy for 41 % of the cycles, vector units for 45 (exponentials), LDS for 31, at 1.8 GHz: the
 // two kinds of work of the two waves of a SIMD hardly overlap.  Units of 32 keys whose exponentials stood between the products of
 // their neighbours took 1.53 ms, a higher priority around products changed nothing.  16 blocks of 3000, 16 heads of 128, some 65 keys to
 // a query: 0.32 ms, 3.0 TB/s, bound by the latencies of few tiles.

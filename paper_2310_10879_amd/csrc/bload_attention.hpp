@@ -1,8 +1,8 @@
 // What the attention kernels share: element types, tiles in LDS, fragments of the matrix
 // instructions, scores.
 //
-// Every product goes through v_mfma_f32_32x32x16: a wavefront multiplies A (32 rows x 16) with
-// B (16 x 32 columns); lane l holds 8 elements of A's row l % 32 and 8 of B's column l % 32, at the
+// Every product goes through v_mfma_f32_32x32x16 (float: eight v_mfma_f32_32x32x2 in its place): a wavefront multiplies
+// A (32 rows x 16) with B (16 x 32 columns); lane l holds 8 elements of A's row l % 32 and 8 of B's column l % 32, at the
 // places 8 (l / 32) + j of the 16; of the result it holds column l % 32 and rows
 // 8 (i / 4) + 4 (l / 32) + i % 4, i = 0..15.  The order of the 16 is free as long as A and B agree.
 //
@@ -429,8 +429,8 @@ struct Maximum {
 // Gradients of scores, p (dp - delta), may lie anywhere in the range of dout, and far below it where a row sees many: float16 would
 // lose them among its subnormals, or overflow.  They are packed as a multiple `by` of themselves, a power of two for each row of results:
 // the first ones that are not 0 bring the largest of its tile between 2^6 and 2^7, and one that passes 2^15 does so again; the
-// row's sums shrink along.  Measured: 16 blocks of 3000 short recordings, 16 heads of 128: dq 413 -> 416 us, dk and dv 535 -> 552 (569
-// from 2^12 on: more rows whose sums have to shrink).
+// row's sums shrink along.  Measured: 16 blocks of 3000 short recordings, 16 heads of 128: dq 411 -> 424 us, dk and dv 533 -> 562 (20
+// more from 2^12 on: more rows whose sums have to shrink).
 struct Reach {
     enum { kNone = 0, kFirst, kSums };
     float by = 1.0f, limit = 0.0f;

@@ -45,8 +45,8 @@ __device__ __forceinline__ void decode_row(const AttArgs& a, int64_t seq, int he
     store_row2(att_at<T>(a.out, seq, 0, head), a.D, o[0], o[1]);
 }
 
-// One share of one sequence for up to 32 heads of queries.  Measured: 32 blocks of 32768 slots, 8 heads of 128 bfloat16 read by 32: 0.58 ms,
-// 5.6 TB/s of keys and values (a copy of 2 GiB: 4.9 read and written).
+// One share of one sequence for up to 32 heads of queries.  Measured: 32 blocks of 32768 slots, 8 heads of 128 bfloat16 read by 32: 0.57 ms,
+// 5.7 TB/s of keys and values (tiles are read at 6.8 where nothing else is done).
 template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads) void attention_decode_kernel(DecodeArgs p)
 {
@@ -233,7 +233,9 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(DecodeArgs p)
     else store_row2(att_at<T>(a.out, seq, 0, head), D, y[0], y[1]);
 }
 
-// Shares: as many as make eight workgroups for each CU, of at least 256 keys of the longest sequence that a block can hold.
+// Shares: as many as make 2048 workgroups, of at least 256 keys of the longest sequence that a block can hold; eight rounds of them on the
+// card for heads of 128, of which one workgroup is resident a CU, fewer for smaller ones.  The lengths are on the device, so the
+// number goes by the blocks' size: many sequences (2048 with all their heads of keys) get one share however long one of them is.
 inline int decode_splits(int64_t n_seq, int32_t t_blk, int32_t heads_kv, int32_t groups)
 {
     const int64_t alone = n_seq * heads_kv * groups;

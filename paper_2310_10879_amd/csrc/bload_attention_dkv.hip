@@ -45,9 +45,9 @@ __device__ __forceinline__ void dkv_row(const AttArgs& a, int b, int kv, int j, 
 // dv^T as results; tiles of 64 queries (float: 32) with their do stream through LDS, head after head of those that
 // share the keys, and are read by rows for the scores and by columns for dk and dv.  128 sums, 64 registers of operands and
 // the scores leave room for one wave a SIMD, which has to overlap its own work: the order of its instructions is written out.
-// Measured: 8 blocks of 4096 bfloat16, 32 heads of 128 over 8, causal: 2.92 ms, 750 TFLOP/s over its four products; LDS reads take as
-// many cycles as the matrix units (39 % of all).  16 blocks of 3000 short recordings, 16 heads: 0.55 ms, 2.1 TB/s: one workgroup a CU waits out
-// each latency of its few tiles.
+// Measured: 8 blocks of 4096 bfloat16, 32 heads of 128 over 8, causal: 2.92 ms, 750 TFLOP/s over its four products; matrix units are
+// busy for 39 % of the cycles, vector units for 31, LDS for 30: the one wave waits for each in turn where the order leaves a gap.  16 blocks of
+// 3000 short recordings, 16 heads, float16: 0.56 ms, 2.0 TB/s: one workgroup a CU waits out each latency of its few tiles.
 template <typename T, int DP, int MOD, bool ODD>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DP <= 64 ? 2 : 1) void attention_dkv_kernel(AttArgs a)
 {

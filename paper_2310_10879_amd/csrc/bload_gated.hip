@@ -9,15 +9,18 @@
 //
 // A stretch of slots is an affine map of what enters it: out = A in + H, A the product of its gates, or
 // out = H where some slot of it does not go on (by selection: A in may be NaN then).  Two stretches
-// make one: (A2 A1, A2 H1 + H2).  A workgroup takes F lanes across features, 16 bytes each, and
+// make one: (A2 A1, A2 H1 + H2).  A workgroup takes F lanes across features, four elements each, and
 // 256 / F stretches of K slots: every lane keeps its K slots in registers, forms the map, the maps are
 // scanned across lanes and waves, and the slots are gone through again from what really enters.  So the data is read
 // once and written once; HBM bound.  Blocks are walked from end to end by one workgroup, or where that
 // leaves the card empty, cut into chunks: a first launch forms the maps of all chunks, the second starts each
 // chunk from the maps in front of it (the data is read twice, which matters little: it is
 // small, or it would not leave the card empty).  No workgroup waits for another one.
-// All of h, g, A, H and u is in 32 bits; only results are rounded to the type.
-// Measured: 48 blocks of 3000 x 2048 half: forward 0.41 to 0.45 ms, backward 0.61 ms (4.1 and 4.8 TB/s; a copy of 2 GiB: 4.9).
+// All of h, g, A, H and u is in 32 bits; only results are rounded to the type.  Backward, h_prev is the forward pass's rounded
+// result: dgate is off by half a step of the type from that, beside its own rounding, where x would have to be read for
+// more.
+// Measured: 48 blocks of 3000 x 2048 half: forward 0.46 ms for 1.77 GB, 3.8 TB/s, backward 0.61 ms for 2.95 GB, 4.8 TB/s (a copy in tiles:
+// 6.4).  Forward, a step loads, exchanges, and stores with nothing on its way meanwhile: latency more than HBM.
 #include <algorithm>
 
 #include "bload_attention_host.hpp"
