@@ -628,7 +628,8 @@ def bload_gated_scan(gate: torch.Tensor, x: torch.Tensor, reset: torch.Tensor, v
                      out: torch.Tensor | None = None, state: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """h = gate * h_prev + x inside the sequences of packed blocks, x at their starts, 0 on padding.  gate, x: contiguous
     [B, T, D] of float16, bfloat16 or float32; h0 (float32[B, D]): the state in front of the blocks.  Returns h and
-    the state behind the last slots (float32[B, D]).  Asynchronous on the current stream."""
+    the state behind the last slots (float32[B, D]), written to `state`, which may be h0 where T <= 8 and is refused where
+    it meets h0 in any other way.  Asynchronous on the current stream."""
     B, T, D = x.shape
     dtype, code, shape = x.dtype, _type_code(x), x.shape
     if out is None:
@@ -647,7 +648,7 @@ def bload_gated_scan_backward(dout: torch.Tensor, gate: torch.Tensor, out: torch
                               h0: torch.Tensor | None = None, dstate: torch.Tensor | None = None, grads=None,
                               workspace: torch.Tensor | None = None):
     """Gradients (dgate, dx, dh0) of sum(out * dout) + sum(state * dstate); out is the forward call's result.
-    grads: three tensors to write into.  Asynchronous on the current stream."""
+    grads: three tensors to write into (dh0 may be dstate or h0 where T <= 8).  Asynchronous on the current stream."""
     B, T, D = dout.shape
     dtype, code, shape = dout.dtype, _type_code(dout), dout.shape
     if grads is None:
