@@ -17,6 +17,7 @@
  *   bload_segment_mask, bload_segment_attention (_backward, _decode)
  *   bload_rotary, bload_rotary_frequencies
  *   bload_gated_scan (_backward)
+ *   bload_layer_norm, bload_segment_conv, bload_selective_scan (each with _backward)
  * and, around that path,
  *   bload_plan_random_fit   the plan built with the sampler of the paper's pseudocode
  *   bload_plan_shard        one data-parallel worker's share of a plan
@@ -72,7 +73,7 @@ typedef enum {
 } bload_status;
 
 typedef enum { BLOAD_U8 = 0, BLOAD_F16 = 1, BLOAD_F32 = 2, BLOAD_I32 = 3,
-               BLOAD_BF16 = 4 /* bload_segment_attention*, bload_gated_scan*, bload_rotary */ } bload_dtype;
+               BLOAD_BF16 = 4 /* the model's operators */ } bload_dtype;
 typedef enum { BLOAD_SUM = 0, BLOAD_MEAN = 1 } bload_op;
 
 /* Human-readable name of a status (static storage, never NULL). */
@@ -540,6 +541,129 @@ bload_status bload_rotary(const bload_heads* x, const int32_t* d_positions, int6
  * and the ones between mixed in proportion (slow < fast).  Host only. */
 bload_status bload_rotary_frequencies(int32_t rot_dim, double base, double factor, int64_t trained, double slow, double fast,
                                       float* h_freq);
+
+/* ------------------------------------------------------------ layer norm --
+ * Rows of features brought to one size: with s = x, or x + residual rounded to the type,
+ *     m = mean(s) (center = 1) or 0 (center = 0: root mean square norm)
+ *     out = (s - m) / sqrt(mean((s - m)^2) + eps) * weight + bias
+ * over the `dim` elements of each head of each slot: heads = 1 for a slot's features as a whole, the heads of queries and keys
+ * for a norm of each.
+ *
+ * x, residual, out, sum   [num_blocks, t_blk, heads, dim] of F16, BF16 or F32; residual may be NULL.  out may be x, and sum
+ *                 residual, with the same strides; else outputs overlap no input
+ * d_valid         in   uint8[num_blocks, t_blk] or NULL (all valid): rows of padding are not read, and become 0
+ * eps             >= 0
+ * d_weight, d_bias in  float32[dim], or NULL for ones and zeros
+ * sum             out  s, or NULL
+ * d_stats         out  float32[num_blocks, t_blk, heads, 2], 8-byte aligned, or NULL: mean and 1 / deviation, for the backward pass
+ * The mean, the mean square and everything per element are in 32 bits.  num_blocks * t_blk * heads < 2^31.
+ * Asynchronous on `hip_stream`, no workspace; same inputs give bit-identical outputs. */
+bload_status bload_layer_norm(const bload_heads* x, const bload_heads* residual, const uint8_t* d_valid, int64_t num_blocks,
+                              int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype, int32_t center, float eps,
+                              const float* d_weight, const float* d_bias, const bload_heads* out, const bload_heads* sum,
+                              float* d_stats, void* hip_stream);
+
+/* Gradients of sum(out * dout) + sum(sum * dsum) by s (which is that by x and by residual), weight and bias.
+ * x               in   what was normalised: the forward call's x, or its sum where it had a residual
+ * d_stats         in   of the forward call;  dsum  in  like x, or NULL
+ * dx              out  like x, 0 on padding; may be dout or dsum with the same strides
+ * d_dweight, d_dbias out float32[dim], or NULL; written also where there are no rows
+ * d_workspace     >= bload_layer_norm_backward_workspace_bytes() bytes, 16-byte aligned (may be NULL without d_dweight and d_dbias)
+ * Asynchronous on `hip_stream`; bit-identical like the forward pass. */
+size_t bload_layer_norm_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype);
+
+bload_status bload_layer_norm_backward(const bload_heads* dout, const bload_heads* x, const float* d_stats, const uint8_t* d_valid,
+                                       int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype, int32_t center,
+                                       const float* d_weight, const bload_heads* dsum, const bload_heads* dx, float* d_dweight,
+                                       float* d_dbias, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* -------------------------------------------------------- segment conv --
+ * A short causal convolution of every feature by itself inside the sequences: per slot t of a block
+ *     p = bias + sum_j weight[d][taps - 1 - j] x[t - j]
+ * over the taps j that reach no further back than t's sequence, and out = p, or with silu = 1 p / (1 + e^-p); 0 on padding.  A
+ * slot goes on from the one in front of it as in bload_gated_scan, and the first slot of a block from the state, where that is
+ * given and the slot carries no start flag.  Blocks of one slot with a state in and out are the form for single tokens.
+ *
+ * x, out       [num_blocks, t_blk, feat_dim] of F16, BF16 or F32 (bload_heads whose head_stride is not used); out overlaps no input
+ * d_weight     in   float32[feat_dim, taps], taps 1 .. BLOAD_CONV_MAX_TAPS;  d_bias  in  float32[feat_dim] or NULL
+ * d_reset, d_valid  in  uint8[num_blocks, t_blk]
+ * d_state_in   in   [num_blocks, taps - 1, feat_dim] of `dtype` or NULL: the inputs in front of the first slot, the oldest first
+ * d_state_out  out  the same behind the last slot, 0 where its sequence (or padding) does not reach, or NULL; may be d_state_in
+ *                   where t_blk <= 8, and is refused (BLOAD_EINVAL) where it meets d_state_in in any other way
+ * Sums are in 32 bits.  What lies in another sequence has no part in a result, infinite or NaN as it may be.
+ * Asynchronous on `hip_stream`, no workspace; same inputs give bit-identical outputs. */
+#define BLOAD_CONV_MAX_TAPS 8
+
+bload_status bload_segment_conv(const bload_heads* x, const float* d_weight, const float* d_bias, const uint8_t* d_reset,
+                                const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t taps,
+                                bload_dtype dtype, int32_t silu, const void* d_state_in, const bload_heads* out, void* d_state_out,
+                                void* hip_stream);
+
+/* Gradients of sum(out * dout) + sum(state_out * dstate_out) by x, weight, bias and state_in.
+ * d_dstate_out  in   like the state, or NULL
+ * dx            out  like x, every element written (0 on padding), overlapping no input
+ * d_dweight, d_dbias  out  float32[feat_dim, taps] and [feat_dim], or NULL; written also where there are no blocks
+ * d_dstate_in   out  like the state, or NULL; overlaps neither state nor d_dstate_out (BLOAD_EINVAL)
+ * d_workspace   >= bload_segment_conv_backward_workspace_bytes() bytes, 16-byte aligned (may be NULL without d_dweight and d_dbias) */
+size_t bload_segment_conv_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t taps, bload_dtype dtype);
+
+bload_status bload_segment_conv_backward(const bload_heads* dout, const bload_heads* x, const float* d_weight, const float* d_bias,
+                                         const uint8_t* d_reset, const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk,
+                                         int32_t feat_dim, int32_t taps, bload_dtype dtype, int32_t silu, const void* d_state_in,
+                                         const void* d_dstate_out, const bload_heads* dx, float* d_dweight, float* d_dbias,
+                                         void* d_dstate_in, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------ selective scan --
+ * A state space whose steps, inputs and outputs go by the frame: every channel d keeps `states` states h_n, and per slot
+ *     step = dt + dt_bias[d], or with softplus = 1 ln(1 + e^(dt + dt_bias[d]))
+ *     h_n = e^(step rate[d][n]) h_n + step b_n x   where the slot goes on (as in bload_gated_scan),
+ *     h_n = step b_n x                             where it starts a sequence, and 0 on padding
+ *     y = sum_n c_n h_n + skip[d] x;   out = y z / (1 + e^-z), or y without z; 0 on padding
+ * b and c are shared by the feat_dim / groups consecutive channels of a group.  Blocks of one slot with a state in and out are
+ * the form for single tokens. */
+#define BLOAD_SELECTIVE_MAX_STATES 64
+
+typedef struct {
+    bload_heads x, dt, z;            /* [num_blocks, t_blk, feat_dim] of `dtype` (head_stride is not used); z.d_data may be NULL */
+    bload_heads b, c;                /* [num_blocks, t_blk, groups, states] of `dtype` */
+    const float* d_rate;             /* float32[feat_dim, states]: negative where states fade */
+    const float* d_skip;             /* float32[feat_dim] or NULL */
+    const float* d_dt_bias;          /* float32[feat_dim] or NULL */
+    const uint8_t *d_reset, *d_valid;        /* uint8[num_blocks, t_blk] */
+    const float* d_state_in;         /* float32[num_blocks, feat_dim, states] or NULL (no state: the first slot starts a sequence) */
+    int64_t num_blocks;
+    int32_t t_blk, feat_dim, states, groups; /* states 1 .. BLOAD_SELECTIVE_MAX_STATES; groups divides feat_dim */
+    bload_dtype dtype;               /* F16, BF16 or F32 */
+    int32_t softplus;
+} bload_selective;
+
+/* out          out  like x, every element written; overlaps no input
+ * d_state_out  out  like the state, or NULL: the state of the last slot; may be d_state_in where t_blk <= 8, and is refused
+ *                   (BLOAD_EINVAL) where it meets d_state_in in any other way
+ * d_saved      out  bload_selective_scan_saved_bytes() bytes, for the backward pass, or NULL: the state in front of every 16th slot
+ * d_workspace  >= bload_selective_scan_workspace_bytes() bytes, 16-byte aligned (may be NULL when that is 0)
+ * States, steps and sums are in 32 bits.  What lies in another sequence or in padding has no part in a result, infinite or NaN as
+ * it may be.  Asynchronous on `hip_stream`; same inputs give bit-identical outputs. */
+size_t bload_selective_scan_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t states, int32_t groups);
+size_t bload_selective_scan_saved_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t states, int32_t groups);
+
+bload_status bload_selective_scan(const bload_selective* s, const bload_heads* out, float* d_state_out, float* d_saved,
+                                  void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of sum(out * dout) + sum(state_out * dstate_out) by x, dt, rate, b, c, skip, z, dt_bias and state_in.
+ * s, d_saved     in   the forward call's
+ * d_dstate_out   in   float32[num_blocks, feat_dim, states] or NULL
+ * dx, ddt, db, dc, dz  out  like their inputs, every element written (0 on padding), overlapping no input; dz is not used without z
+ * d_drate, d_dskip, d_ddt_bias  out  float32 like their inputs, or NULL; written also where there are no blocks
+ * d_dstate_in    out  like the state, or NULL (0 where the first slot does not go on); meets neither state nor d_dstate_out (BLOAD_EINVAL)
+ * d_workspace    >= bload_selective_scan_backward_workspace_bytes() bytes, 16-byte aligned */
+size_t bload_selective_scan_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t states, int32_t groups);
+
+bload_status bload_selective_scan_backward(const bload_selective* s, const bload_heads* dout, const float* d_saved,
+                                           const float* d_dstate_out, const bload_heads* dx, const bload_heads* ddt, float* d_drate,
+                                           const bload_heads* db, const bload_heads* dc, float* d_dskip, const bload_heads* dz,
+                                           float* d_ddt_bias, float* d_dstate_in, void* d_workspace, size_t workspace_bytes,
+                                           void* hip_stream);
 
 /* -------------------------------------------------------- strategy counts --
  * Problem Statement and Table 1 (rows "padding amount" and "# frames deleted"):

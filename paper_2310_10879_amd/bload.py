@@ -130,6 +130,38 @@ _lib.bload_rotary.restype = _int
 _lib.bload_rotary.argtypes = [_hp, _vp, _i64, _i32, _i32, _i32, _int, _vp, _i32, _int, _f32, _i32, _hp, _vp]
 _lib.bload_rotary_frequencies.restype = _int
 _lib.bload_rotary_frequencies.argtypes = [_i32, ctypes.c_double, ctypes.c_double, _i64, ctypes.c_double, ctypes.c_double, _vp]
+_lib.bload_layer_norm.restype = _int
+_lib.bload_layer_norm.argtypes = [_hp, _hp, _vp, _i64, _i32, _i32, _i32, _int, _i32, _f32, _vp, _vp, _hp, _hp, _vp, _vp]
+_lib.bload_layer_norm_backward_workspace_bytes.restype = _sz
+_lib.bload_layer_norm_backward_workspace_bytes.argtypes = [_i64, _i32, _i32, _i32, _int]
+_lib.bload_layer_norm_backward.restype = _int
+_lib.bload_layer_norm_backward.argtypes = [_hp, _hp, _vp, _vp, _i64, _i32, _i32, _i32, _int, _i32, _vp, _hp, _hp, _vp, _vp, _vp, _sz, _vp]
+_lib.bload_segment_conv.restype = _int
+_lib.bload_segment_conv.argtypes = [_hp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _int, _i32, _vp, _hp, _vp, _vp]
+_lib.bload_segment_conv_backward_workspace_bytes.restype = _sz
+_lib.bload_segment_conv_backward_workspace_bytes.argtypes = [_i64, _i32, _i32, _i32, _int]
+_lib.bload_segment_conv_backward.restype = _int
+_lib.bload_segment_conv_backward.argtypes = [_hp, _hp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _int, _i32, _vp, _vp, _hp, _vp, _vp, _vp,
+                                             _vp, _sz, _vp]
+
+
+class Selective(ctypes.Structure):
+    """bload_selective"""
+    _fields_ = [("x", Heads), ("dt", Heads), ("z", Heads), ("b", Heads), ("c", Heads), ("d_rate", _vp), ("d_skip", _vp),
+                ("d_dt_bias", _vp), ("d_reset", _vp), ("d_valid", _vp), ("d_state_in", _vp), ("num_blocks", _i64), ("t_blk", _i32),
+                ("feat_dim", _i32), ("states", _i32), ("groups", _i32), ("dtype", _int), ("softplus", _i32)]
+
+
+_sp = ctypes.POINTER(Selective)
+SELECTIVE_MAX_STATES = 64
+CONV_MAX_TAPS = 8
+for _name in ("workspace", "saved", "backward_workspace"):
+    _f = getattr(_lib, f"bload_selective_scan_{_name}_bytes")
+    _f.restype, _f.argtypes = _sz, [_i64, _i32, _i32, _i32, _i32]
+_lib.bload_selective_scan.restype = _int
+_lib.bload_selective_scan.argtypes = [_sp, _hp, _vp, _vp, _vp, _sz, _vp]
+_lib.bload_selective_scan_backward.restype = _int
+_lib.bload_selective_scan_backward.argtypes = [_sp, _hp, _vp, _vp, _hp, _hp, _vp, _hp, _hp, _vp, _hp, _vp, _vp, _vp, _sz, _vp]
 
 
 class BloadError(RuntimeError):
@@ -686,3 +718,201 @@ def bload_rotary(x: torch.Tensor, positions: torch.Tensor, frequencies: torch.Te
                              _ptr(frequencies, torch.float32), 2 * frequencies.shape[0], ROTARY_LAYOUTS[layout], scale, int(inverse),
                              _heads(out, x.shape, x.dtype, "out"), _stream()))
     return out
+
+
+def _frames(t: torch.Tensor, shape, dtype, name: str) -> Heads:
+    """A tensor [B, T, D] of any strides with the features of a slot side by side."""
+    h = _heads(t, shape, dtype, name)
+    h.slot_stride, h.head_stride = h.head_stride, 0
+    return h
+
+
+def _rows(t: torch.Tensor, shape, dtype, name: str) -> Heads:
+    """A tensor [B, T, heads, D], or [B, T, D] for one head."""
+    return _heads(t, shape, dtype, name) if len(shape) == 4 else _frames(t, shape, dtype, name)
+
+
+def bload_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                     residual: torch.Tensor | None = None, valid: torch.Tensor | None = None, eps: float = 1e-5, center: bool = True,
+                     training: bool = False, out: torch.Tensor | None = None, total: torch.Tensor | None = None):
+    """Layer norm (center) or root mean square norm of the last dimension of x: [B, T, D] or [B, T, heads, D] of float16, bfloat16 or
+    float32, any strides with the elements of a row side by side; weight, bias: float32[D].  residual (like x): their
+    rounded sum is normalised.  valid (uint8[B, T]): padding is not read and becomes 0.  Returns the result; with residual also the sum
+    (written to `total`); with training also float32[B, T(, heads), 2] for ``bload_layer_norm_backward``.  out may be x, total may be
+    residual.  Asynchronous on the current stream."""
+    shape, dtype, code = x.shape, x.dtype, _type_code(x)
+    B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+    if out is None:
+        out = x.new_empty(shape)
+    hr = hs = None
+    if residual is not None:
+        if total is None:
+            total = x.new_empty(shape)
+        hr, hs = _rows(residual, shape, dtype, "residual"), _rows(total, shape, dtype, "total")
+    elif total is not None:
+        raise ValueError("total is the sum with a residual")
+    stats = x.new_empty((*shape[:-1], 2), dtype=torch.float32) if training else None
+    _check(_lib.bload_layer_norm(_rows(x, shape, dtype, "x"), hr, _sized(valid, (B, T), torch.uint8, "valid"), B, T, H, D, code, int(center),
+                                 eps, _sized(weight, (D,), torch.float32, "weight"), _sized(bias, (D,), torch.float32, "bias"),
+                                 _rows(out, shape, dtype, "out"), hs, stats.data_ptr() if training else 0, _stream()))
+    result = (out,) if residual is None else (out, total)
+    if training:
+        result += (stats,)
+    return result if len(result) > 1 else out
+
+
+def bload_layer_norm_backward_workspace_bytes(num_blocks: int, t_blk: int, heads: int, dim: int, dtype: torch.dtype) -> int:
+    return int(_lib.bload_layer_norm_backward_workspace_bytes(num_blocks, t_blk, heads, dim, TYPE_CODE[dtype]))
+
+
+def bload_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, weight: torch.Tensor | None = None,
+                              valid: torch.Tensor | None = None, dsum: torch.Tensor | None = None, center: bool = True, grads=None,
+                              workspace: torch.Tensor | None = None):
+    """Gradients (dx, dweight, dbias) of sum(out * dout) + sum(total * dsum); x is what was normalised: the forward call's x, or its
+    sum where it had a residual.  dx is the gradient of both then.  grads: three tensors to write into, the last two float32[D] or None
+    to leave them out.  Asynchronous on the current stream."""
+    shape, dtype, code = x.shape, x.dtype, _type_code(x)
+    B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+    if grads is None:
+        both = x.new_empty((2, D), dtype=torch.float32)
+        grads = x.new_empty(shape), both[0], both[1]
+    dx, dweight, dbias = grads
+    if workspace is None and (dweight is not None or dbias is not None):
+        need = _lib.bload_layer_norm_backward_workspace_bytes(B, T, H, D, code)
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
+    _check(_lib.bload_layer_norm_backward(
+        _rows(dout, shape, dtype, "dout"), _rows(x, shape, dtype, "x"), _sized(stats, (*shape[:-1], 2), torch.float32, "stats"),
+        _sized(valid, (B, T), torch.uint8, "valid"), B, T, H, D, code, int(center), _sized(weight, (D,), torch.float32, "weight"),
+        None if dsum is None else _rows(dsum, shape, dtype, "dsum"), _rows(dx, shape, dtype, "dx"),
+        _sized(dweight, (D,), torch.float32, "dweight"), _sized(dbias, (D,), torch.float32, "dbias"), _ptr(workspace), _room(workspace),
+        _stream()))
+    return dx, dweight, dbias
+
+
+def bload_segment_conv(x: torch.Tensor, weight: torch.Tensor, reset: torch.Tensor, valid: torch.Tensor, bias: torch.Tensor | None = None,
+                       silu: bool = False, state_in: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                       state: torch.Tensor | None = None):
+    """A short causal convolution of every feature inside the sequences of packed blocks, with silu p / (1 + e^-p) of it; 0 on padding.
+    x: [B, T, D] of float16, bfloat16 or float32, any strides with the features of a slot side by side; weight: float32[D, taps],
+    taps up to 8, the last one for the slot itself; bias: float32[D]; state_in: [B, taps - 1, D] like x, the inputs in front of the
+    blocks, the oldest first.  Returns the result and the last inputs of every block, written to `state`, which may be state_in where
+    T <= 8 and is refused where it meets state_in in any other way.  Asynchronous on the current stream."""
+    B, T, D = shape = x.shape
+    dtype, code, K = x.dtype, _type_code(x), weight.shape[-1]
+    if out is None:
+        out = x.new_empty((B, T, D))
+    if state is None:
+        state = x.new_empty((B, K - 1, D))
+    _check(_lib.bload_segment_conv(_frames(x, shape, dtype, "x"), _sized(weight, (D, K), torch.float32, "weight"),
+                                   _sized(bias, (D,), torch.float32, "bias"), _sized(reset, (B, T), torch.uint8, "reset"),
+                                   _sized(valid, (B, T), torch.uint8, "valid"), B, T, D, K, code, int(silu),
+                                   _sized(state_in, (B, K - 1, D), dtype, "state_in"), _frames(out, shape, dtype, "out"),
+                                   _sized(state, (B, K - 1, D), dtype, "state"), _stream()))
+    return out, state
+
+
+def bload_segment_conv_backward_workspace_bytes(num_blocks: int, t_blk: int, feat_dim: int, taps: int, dtype: torch.dtype) -> int:
+    return int(_lib.bload_segment_conv_backward_workspace_bytes(num_blocks, t_blk, feat_dim, taps, TYPE_CODE[dtype]))
+
+
+def bload_segment_conv_backward(dout: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, reset: torch.Tensor, valid: torch.Tensor,
+                                bias: torch.Tensor | None = None, silu: bool = False, state_in: torch.Tensor | None = None,
+                                dstate: torch.Tensor | None = None, grads=None, workspace: torch.Tensor | None = None):
+    """Gradients (dx, dweight, dbias, dstate_in) of sum(out * dout) + sum(state * dstate).  grads: four tensors to write into, the
+    last three None to leave them out.  Asynchronous on the current stream."""
+    B, T, D = shape = x.shape
+    dtype, code, K = x.dtype, _type_code(x), weight.shape[-1]
+    if grads is None:
+        both = x.new_empty(D * (K + 1), dtype=torch.float32)
+        grads = x.new_empty((B, T, D)), both[:D * K].view(D, K), both[D * K:], x.new_empty((B, K - 1, D))
+    dx, dweight, dbias, dstate_in = grads
+    if workspace is None and (dweight is not None or dbias is not None):
+        need = _lib.bload_segment_conv_backward_workspace_bytes(B, T, D, K, code)
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
+    _check(_lib.bload_segment_conv_backward(
+        _frames(dout, shape, dtype, "dout"), _frames(x, shape, dtype, "x"), _sized(weight, (D, K), torch.float32, "weight"),
+        _sized(bias, (D,), torch.float32, "bias"), _sized(reset, (B, T), torch.uint8, "reset"), _sized(valid, (B, T), torch.uint8, "valid"),
+        B, T, D, K, code, int(silu), _sized(state_in, (B, K - 1, D), dtype, "state_in"), _sized(dstate, (B, K - 1, D), dtype, "dstate"),
+        _frames(dx, shape, dtype, "dx"), _sized(dweight, (D, K), torch.float32, "dweight"), _sized(dbias, (D,), torch.float32, "dbias"),
+        _sized(dstate_in, (B, K - 1, D), dtype, "dstate_in"), _ptr(workspace), _room(workspace), _stream()))
+    return dx, dweight, dbias, dstate_in
+
+
+def bload_selective_scan_workspace_bytes(num_blocks: int, t_blk: int, feat_dim: int, states: int, groups: int = 1) -> int:
+    return int(_lib.bload_selective_scan_workspace_bytes(num_blocks, t_blk, feat_dim, states, groups))
+
+
+def bload_selective_scan_saved_bytes(num_blocks: int, t_blk: int, feat_dim: int, states: int, groups: int = 1) -> int:
+    return int(_lib.bload_selective_scan_saved_bytes(num_blocks, t_blk, feat_dim, states, groups))
+
+
+def bload_selective_scan_backward_workspace_bytes(num_blocks: int, t_blk: int, feat_dim: int, states: int, groups: int = 1) -> int:
+    return int(_lib.bload_selective_scan_backward_workspace_bytes(num_blocks, t_blk, feat_dim, states, groups))
+
+
+def _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0) -> Selective:
+    B, T, D = shape = x.shape
+    dtype, code = x.dtype, _type_code(x)
+    pair = (B, T, *b.shape[2:]) if b.dim() == 4 else (B, T, 1, rate.shape[-1])
+    G, N = pair[2:]
+    return Selective(_frames(x, shape, dtype, "x"), _frames(dt, shape, dtype, "dt"),
+                     Heads() if z is None else _frames(z, shape, dtype, "z"), _heads(b, pair, dtype, "b"), _heads(c, pair, dtype, "c"),
+                     _sized(rate, (D, N), torch.float32, "rate"), _sized(skip, (D,), torch.float32, "skip"),
+                     _sized(dt_bias, (D,), torch.float32, "dt_bias"), _sized(reset, (B, T), torch.uint8, "reset"),
+                     _sized(valid, (B, T), torch.uint8, "valid"), _sized(h0, (B, D, N), torch.float32, "h0"), B, T, D, N, G, code,
+                     int(softplus))
+
+
+def bload_selective_scan(x: torch.Tensor, dt: torch.Tensor, rate: torch.Tensor, b: torch.Tensor, c: torch.Tensor, reset: torch.Tensor,
+                         valid: torch.Tensor, skip: torch.Tensor | None = None, z: torch.Tensor | None = None,
+                         dt_bias: torch.Tensor | None = None, softplus: bool = True, h0: torch.Tensor | None = None,
+                         training: bool = False, out: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None):
+    """A selective state space inside the sequences of packed blocks: step = softplus(dt + dt_bias), h = e^(step rate) h + step b x,
+    y = c.h + skip x, times z sigmoid(z).  x, dt, z: [B, T, D] and b, c: [B, T, groups, N] of float16, bfloat16 or
+    float32, any strides with the elements of a row side by side; rate: float32[D, N], N up to 64; skip, dt_bias: float32[D];
+    h0: float32[B, D, N], the state in front of the blocks.  Returns the result and the state behind the last slots (float32[B, D, N]),
+    written to `state`, which may be h0 where T <= 8 and is refused where it meets h0 in any other way; with training also what
+    ``bload_selective_scan_backward`` needs.  Asynchronous on the current stream."""
+    B, T, D = x.shape
+    s = _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0)
+    N, G = s.states, s.groups
+    if out is None:
+        out = x.new_empty((B, T, D))
+    if state is None:
+        state = x.new_empty((B, D, N), dtype=torch.float32)
+    saved = x.new_empty((B, -(-T // 16), D, N), dtype=torch.float32) if training else None
+    if workspace is None:
+        need = _lib.bload_selective_scan_workspace_bytes(B, T, D, N, G)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    _check(_lib.bload_selective_scan(s, _frames(out, x.shape, x.dtype, "out"), _sized(state, (B, D, N), torch.float32, "state"),
+                                     saved.data_ptr() if training else 0, _ptr(workspace), _room(workspace), _stream()))
+    return (out, state, saved) if training else (out, state)
+
+
+def bload_selective_scan_backward(dout: torch.Tensor, x: torch.Tensor, dt: torch.Tensor, rate: torch.Tensor, b: torch.Tensor,
+                                  c: torch.Tensor, reset: torch.Tensor, valid: torch.Tensor, saved: torch.Tensor,
+                                  skip: torch.Tensor | None = None, z: torch.Tensor | None = None, dt_bias: torch.Tensor | None = None,
+                                  softplus: bool = True, h0: torch.Tensor | None = None, dstate: torch.Tensor | None = None, grads=None,
+                                  workspace: torch.Tensor | None = None):
+    """Gradients (dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0) of sum(out * dout) + sum(state * dstate), None in the place of
+    inputs that are None; saved is the forward call's.  grads: nine tensors to write into, None for drate, dskip, ddt_bias and dh0
+    to leave them out.  Asynchronous on the current stream."""
+    B, T, D = shape = x.shape
+    s = _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0)
+    N, G, dtype = s.states, s.groups, x.dtype
+    if grads is None:
+        like = lambda t: None if t is None else x.new_empty(t.shape, dtype=t.dtype)
+        grads = tuple(like(t) for t in (x, dt, rate, b, c, skip, z, dt_bias, h0))
+    dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0 = grads
+    if workspace is None:
+        need = _lib.bload_selective_scan_backward_workspace_bytes(B, T, D, N, G)
+        workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
+    real = torch.float32
+    _check(_lib.bload_selective_scan_backward(
+        s, _frames(dout, shape, dtype, "dout"), _sized(saved, (B, -(-T // 16), D, N), real, "saved"), _sized(dstate, (B, D, N), real, "dstate"),
+        _frames(dx, shape, dtype, "dx"), _frames(ddt, shape, dtype, "ddt"), _sized(drate, (D, N), real, "drate"),
+        _heads(db, (B, T, G, N), dtype, "db"), _heads(dc, (B, T, G, N), dtype, "dc"), _sized(dskip, (D,), real, "dskip"),
+        None if z is None else _frames(dz, shape, dtype, "dz"), _sized(ddt_bias, (D,), real, "ddt_bias"),
+        _sized(dh0, (B, D, N), real, "dh0"), _ptr(workspace), _room(workspace), _stream()))
+    return dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0

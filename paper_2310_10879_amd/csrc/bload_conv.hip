@@ -1,0 +1,486 @@
+// bload_segment_conv: a short causal convolution per feature inside the sequences of packed blocks, forward and backward.
+//
+//     p_t = bias + sum_j w[K-1-j] x_{t-j}   over the taps j < K that reach no further back than slot t's sequence does,
+//     y = p or p sigmoid(p);  0 on padding
+// Backward, with dp = dout (or dout s (1 + p (1 - s)), s = sigmoid(p)):
+//     dx_t = sum_j w[K-1-j] dp_{t+j} over the slots t+j that reach back to t;  dw[K-1-j] = sum dp_t x_{t-j};  dbias = sum dp
+// A block may go on from the K - 1 inputs in front of it, and leaves those that the next one goes on from.
+//
+// HBM bound: x is read and y written once; backward x and dout are read and dx is written, p formed again.  A lane takes V
+// features (16 bytes) and a run of slots, holds the last K - 1 inputs in registers, and a slot's age (how many slots of its
+// sequence lie in front of it, up to K - 1) says which of them to forget.  Ages of a run lie in LDS.  Runs begin with the K - 1 inputs in
+// front of them, which their neighbour reads as well (from L2); backward a run also forms dp of the K - 1 slots
+// behind it.  The weights' gradients stay in registers over all runs of a lane, are added inside the workgroup
+// and left in the workspace, and column_sums adds the workgroups' in a fixed order.
+#include <algorithm>
+
+#include "bload_rows.hpp"
+
+namespace bload {
+namespace {
+
+struct ConvArgs {
+    AttTensor x, out, dout;          // out: y, backward dx
+    const uint8_t *reset, *valid;
+    const float *weight, *bias;      // [D, K], [D] or null
+    const void* in;                  // [B, K - 1, D] or null
+    void* last;                      // the same, or null; backward: din
+    const void* dlast;
+    float* parts;                    // [groups of items][D K + D]
+    int64_t items, groups;           // items: runs of all blocks; groups: of items, one to a workgroup at a time
+    int32_t T, D, F, slices, runs, run;        // runs of a block, slots of a run
+    int32_t silu;
+};
+
+// 1 + the slots of its sequence in front of slot t, up to most; 0 on padding.
+__device__ __forceinline__ int slot_age(const uint8_t* reset, const uint8_t* valid, int t, bool has_state, int most)
+{
+    int what = slot_does(reset, valid, t, has_state), age = 0;
+    if (what == 0) return 0;
+    while (what == 2 && age < most) {
+        ++age;
+        if (--t < 0) return 1 + most;
+        what = slot_does(reset, valid, t, has_state);
+    }
+    return 1 + age;
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
+
+template <typename T, bool BACK, int K> constexpr int kConvPiece = K <= 4 && !BACK ? kRowPiece<T> : kRowPiece<T> / 2;
+
+// What both passes set up: a lane's features and its weights.
+template <int V, int K>
+struct ConvLane {
+    int d, skip;
+    bool mine;
+    float w[K][V], bias[V];
+    __device__ __forceinline__ ConvLane(const ConvArgs& a, int f, int slice)
+    {
+        const int d0 = (slice * a.F + f) * V;
+        mine = d0 < a.D;
+        d = min(d0, a.D - V);
+        skip = min(d0 - d, V);
+        float rows[V * K];
+        load_floats<V * K>(a.weight + (int64_t)d * K, rows);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            bias[v] = a.bias ? a.bias[d + v] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) w[k][v] = rows[v * K + k];
+        }
+    }
+};
+
+template <typename T, int V, int K>
+__device__ __forceinline__ void load_slot(RowPiece<T, V>& piece, const ConvArgs& a, int64_t b, int t, int d)
+{
+    piece.zero();
+    if (t >= 0) {
+        if (t < a.T) piece.load(att_at<T>(a.x, b, t, 0) + d);
+    } else if (a.in) {
+        piece.load(reinterpret_cast<const T*>(a.in) + (b * (K - 1) + K - 1 + t) * a.D + d);
+    }
+}
+
+// R: slots of a run.
+template <typename T, int V, int K, int R>
+__global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
+{
+    __shared__ uint8_t ages[kThreads * R];
+    const int f = (int)threadIdx.x & (a.F - 1), lane_item = (int)threadIdx.x / a.F, each = kThreads / a.F;
+    const int slice = (int)(blockIdx.x % a.slices);
+    const int64_t item0 = (int64_t)(blockIdx.x / a.slices) * each, item = item0 + lane_item;
+    for (int n = (int)threadIdx.x; n < each * R; n += kThreads) {
+        const int64_t i = item0 + n / R, b = i / a.runs;
+        const int t = (int)(i - b * a.runs) * R + n % R;
+        ages[n] = i < a.items && t < a.T ? (uint8_t)slot_age(a.reset + b * a.T, a.valid + b * a.T, t, a.in != nullptr, K - 1) : 0;
+    }
+    __syncthreads();
+    const ConvLane<V, K> lane(a, f, slice);
+    if (item >= a.items || !lane.mine) return;
+    const int64_t b = item / a.runs;
+    const int t0 = (int)(item - b * a.runs) * R;
+    RowPiece<T, V> x[K - 1 + R];
+#pragma unroll
+    for (int i = 0; i < K - 1 + R; ++i) load_slot<T, V, K>(x[i], a, b, t0 - (K - 1) + i, lane.d);
+    const bool last = a.last && t0 + R >= a.T;
+    float seen[K][V];                // seen[j]: the input of j slots before
+#pragma unroll
+    for (int j = 1; j < K; ++j)
+#pragma unroll
+        for (int v = 0; v < V; ++v) seen[j][v] = x[K - 1 - j][v];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        if (t0 + i >= a.T) break;
+        const int age = ages[lane_item * R + i];
+        float p[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) seen[0][v] = x[K - 1 + i][v];
+        if (age < K)
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+                if (j >= age)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) seen[j][v] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            p[v] = lane.bias[v];
+#pragma unroll
+            for (int j = K - 1; j >= 0; --j) p[v] = fmaf(lane.w[K - 1 - j][v], seen[j][v], p[v]);
+            if (a.silu) p[v] *= sigmoid(p[v]);
+            if (age == 0) p[v] = 0.0f;
+        }
+        store_row<T, V>(att_at<T>(a.out, b, t0 + i, 0) + lane.d, p, lane.skip);
+        if (last && t0 + i == a.T - 1)
+#pragma unroll
+            for (int j = 0; j < K - 1; ++j)
+                store_row<T, V>(reinterpret_cast<T*>(a.last) + (b * (K - 1) + K - 2 - j) * a.D + lane.d, seen[j], lane.skip);
+#pragma unroll
+        for (int j = K - 1; j > 0; --j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) seen[j][v] = seen[j - 1][v];
+    }
+}
+
+constexpr int kConvStep = 8, kConvRun = 64;      // slots whose loads are on their way together; most slots of a run, backward
+
+template <typename T, int V, int K>
+__global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
+{
+    constexpr int S = kConvStep;
+    extern __shared__ float shared[];
+    const int f = (int)threadIdx.x & (a.F - 1), lane_item = (int)threadIdx.x / a.F, each = kThreads / a.F;
+    const int reach = a.run + K - 1;                       // slots whose dp a run needs
+    const int slice = (int)(blockIdx.x % a.slices);
+    uint8_t* ages = reinterpret_cast<uint8_t*>(shared);    // [each][reach], and the last slot's of each run's block
+    uint8_t* last_age = ages + each * reach;
+    const ConvLane<V, K> lane(a, f, slice);
+    float dw[K][V], db[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        db[v] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) dw[k][v] = 0.0f;
+    }
+    for (int64_t group = blockIdx.x / a.slices; group < a.groups; group += gridDim.x / a.slices) {
+        const int64_t item0 = group * each, item = item0 + lane_item;
+        __syncthreads();
+        for (int n = (int)threadIdx.x; n < each * (reach + 1); n += kThreads) {
+            const bool final = n >= each * reach;
+            const int64_t i = item0 + (final ? n - each * reach : n / reach), b = i / a.runs;
+            const int t = final ? a.T - 1 : (int)(i - b * a.runs) * a.run + n % reach;
+            ages[n] = i < a.items && t < a.T ? (uint8_t)slot_age(a.reset + b * a.T, a.valid + b * a.T, t, a.in != nullptr, K - 1) : 0;
+        }
+        __syncthreads();
+        if (item >= a.items || !lane.mine) continue;
+        const int64_t b = item / a.runs;
+        const int t0 = (int)(item - b * a.runs) * a.run, t1 = min(t0 + a.run, a.T), end = t1 + K - 1;
+        const int kept = a.dlast ? last_age[lane_item] : 0;
+        float seen[K][V], acc[K][V];                       // acc[j]: of dx of the slot j before, from the slots up to here
+#pragma unroll
+        for (int j = 1; j < K; ++j) {
+            RowPiece<T, V> x;
+            load_slot<T, V, K>(x, a, b, t0 - j, lane.d);
+#pragma unroll
+            for (int v = 0; v < V; ++v) seen[j][v] = x[v], acc[j][v] = 0.0f;
+        }
+        for (int s0 = t0; s0 < end; s0 += S) {
+            RowPiece<T, V> x[S], dy[S];
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                x[i].zero();
+                dy[i].zero();
+                if (s0 + i < min(end, a.T)) {
+                    x[i].load(att_at<T>(a.x, b, s0 + i, 0) + lane.d);
+                    dy[i].load(att_at<T>(a.dout, b, s0 + i, 0) + lane.d);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                const int s = s0 + i;
+                if (s >= end) break;
+                const int age = ages[lane_item * reach + s - t0];
+                float dp[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    seen[0][v] = x[i][v];
+                    acc[0][v] = 0.0f;
+                    dp[v] = age ? dy[i][v] : 0.0f;
+                }
+                if (age < K)
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+                        if (j >= age)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) seen[j][v] = 0.0f;
+                if (a.silu && age) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        float p = lane.bias[v];
+#pragma unroll
+                        for (int j = K - 1; j >= 0; --j) p = fmaf(lane.w[K - 1 - j][v], seen[j][v], p);
+                        const float sg = sigmoid(p);
+                        dp[v] *= sg * fmaf(p, 1.0f - sg, 1.0f);
+                    }
+                }
+                const bool count = s < t1;
+                if (count)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) db[v] += dp[v];
+                if (age >= K) {
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            acc[j][v] = fmaf(lane.w[K - 1 - j][v], dp[v], acc[j][v]);
+                            if (count) dw[K - 1 - j][v] = fmaf(dp[v], seen[j][v], dw[K - 1 - j][v]);
+                        }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < K; ++j)
+                        if (j < age)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) {
+                                acc[j][v] = fmaf(lane.w[K - 1 - j][v], dp[v], acc[j][v]);
+                                if (count) dw[K - 1 - j][v] = fmaf(dp[v], seen[j][v], dw[K - 1 - j][v]);
+                            }
+                }
+                // slot u has heard from all that look back to it
+                const int u = s - (K - 1), row = u - (a.T - (K - 1));
+                if (u >= t0 || (t0 == 0 && a.last)) {
+                    if (row >= 0 && row < K - 1 && kept >= K - 1 - row) {
+                        const T* p = reinterpret_cast<const T*>(a.dlast) + (b * (K - 1) + row) * a.D + lane.d;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) acc[K - 1][v] += (float)p[v];
+                    }
+                    T* to = u >= 0 ? att_at<T>(a.out, b, u, 0) : reinterpret_cast<T*>(a.last) + (b * (K - 1) + K - 1 + u) * a.D;
+                    store_row<T, V>(to + lane.d, acc[K - 1], lane.skip);
+                }
+#pragma unroll
+                for (int j = K - 1; j > 0; --j)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        seen[j][v] = seen[j - 1][v];
+                        acc[j][v] = acc[j - 1][v];
+                    }
+            }
+        }
+    }
+    if (!a.parts) return;
+    // runs of a wavefront, then the wavefronts one after another
+    __syncthreads();
+    float sums[K + 1][V];
+#pragma unroll
+    for (int k = 0; k <= K; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            sums[k][v] = k < K ? dw[k < K ? k : 0][v] : db[v];
+            for (int dist = a.F; dist < kWave; dist <<= 1) sums[k][v] += __shfl_xor(sums[k][v], dist);
+        }
+    const int at = f * V;                                  // [K + 1][F * V]
+    for (int turn = 0; turn < kThreads / kWave; ++turn) {
+        if (wave_id() == turn && lane_id() < a.F)
+#pragma unroll
+            for (int k = 0; k <= K; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float* p = shared + k * a.F * V + at + v;
+                    *p = sums[k][v] + (turn ? *p : 0.0f);
+                }
+        __syncthreads();
+    }
+    if ((int)threadIdx.x >= a.F || !lane.mine) return;
+    float* part = a.parts + (int64_t)(blockIdx.x / a.slices) * a.D * (K + 1);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v >= lane.skip) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) part[(int64_t)(lane.d + v) * K + k] = shared[k * a.F * V + at + v];
+            part[(int64_t)a.D * K + lane.d + v] = shared[K * a.F * V + at + v];
+        }
+}
+
+// ---------------------------------------------------------------- host
+
+struct ConvPlan {
+    int32_t V, F, slices, runs, run;
+    int64_t items, groups, workgroups;       // workgroups: along the items
+};
+
+inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtype dtype, bool back)
+{
+    ConvPlan p = {};
+    p.V = (K <= 4 && !back ? 16 : 8) / (int)att_elem_bytes(dtype);
+    if (D < p.V) p.V = 1;
+    const int64_t lanes = ceil_div(D, p.V);
+    p.F = 1;
+    while (p.F < kWave && p.F < lanes) p.F *= 2;
+    p.slices = (int32_t)ceil_div(lanes, p.F);
+    const int64_t each = kThreads / p.F;
+    if (!back) {
+        p.run = T == 1 ? 1 : 16;
+    } else {
+        // long runs read little twice; short ones where long ones would leave the card empty
+        p.run = kConvRun;
+        while (p.run > 16 && ceil_div(B * ceil_div(T, p.run), each) * p.slices < 1024) p.run /= 2;
+    }
+    p.runs = (int32_t)ceil_div(T, p.run);
+    p.items = B * p.runs;
+    p.groups = ceil_div(p.items, each);
+    p.workgroups = back ? std::min<int64_t>(p.groups, 1024) : p.groups;
+    return p;
+}
+
+// f(type, V, K)
+template <typename T, bool BACK, typename F>
+inline void conv_dispatch_taps(int32_t D, int32_t K, F f)
+{
+    using std::integral_constant;
+    auto by_taps = [&](auto k) {
+        constexpr int V = kConvPiece<T, BACK, decltype(k)::value>;
+        if (D < V) f(type_is<T>(), integral_constant<int, 1>(), k);
+        else f(type_is<T>(), integral_constant<int, V>(), k);
+    };
+    if (K == 1) by_taps(integral_constant<int, 1>());
+    else if (K == 2) by_taps(integral_constant<int, 2>());
+    else if (K == 3) by_taps(integral_constant<int, 3>());
+    else if (K == 4) by_taps(integral_constant<int, 4>());
+    else if (K == 5) by_taps(integral_constant<int, 5>());
+    else if (K == 6) by_taps(integral_constant<int, 6>());
+    else if (K == 7) by_taps(integral_constant<int, 7>());
+    else by_taps(integral_constant<int, 8>());
+}
+
+inline bload_status conv_check(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t taps, bload_dtype dtype)
+{
+    if (num_blocks < 0 || t_blk < 1 || feat_dim < 1 || taps < 1 || taps > BLOAD_CONV_MAX_TAPS || !att_dtype(dtype)) return BLOAD_EINVAL;
+    if (t_blk > (1 << 30) || feat_dim > (1 << 26) || num_blocks >= ((int64_t)1 << 40) / t_blk) return BLOAD_EOVERFLOW;
+    return BLOAD_OK;
+}
+
+inline bool conv_states_apart(const void* in, const void* out, int64_t bytes, int32_t t_blk)
+{
+    if (!in || !out || (in == out && t_blk <= 8)) return true;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(in), q = reinterpret_cast<uintptr_t>(out);
+    return (p < q ? q - p : p - q) >= (uintptr_t)bytes;
+}
+
+inline ConvArgs conv_args(const ConvPlan& p, int32_t T, int32_t D, int32_t silu)
+{
+    ConvArgs a = {};
+    a.items = p.items;
+    a.groups = p.groups;
+    a.T = T;
+    a.D = D;
+    a.F = p.F;
+    a.slices = p.slices;
+    a.runs = p.runs;
+    a.run = p.run;
+    a.silu = silu;
+    return a;
+}
+
+}  // namespace
+}  // namespace bload
+
+using namespace bload;
+
+extern "C" bload_status bload_segment_conv(const bload_heads* x, const float* d_weight, const float* d_bias, const uint8_t* d_reset,
+                                           const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t taps,
+                                           bload_dtype dtype, int32_t silu, const void* d_state_in, const bload_heads* out,
+                                           void* d_state_out, void* hip_stream)
+{
+    bload_status st = conv_check(num_blocks, t_blk, feat_dim, taps, dtype);
+    if (st != BLOAD_OK) return st;
+    if (silu < 0 || silu > 1) return BLOAD_EINVAL;
+    if (num_blocks == 0) return BLOAD_OK;
+    const ConvPlan p = conv_plan(num_blocks, t_blk, feat_dim, taps, dtype, false);
+    if (p.workgroups > kMaxGroups / p.slices) return BLOAD_EOVERFLOW;
+    ConvArgs a = conv_args(p, t_blk, feat_dim, silu);
+    if ((st = att_tensor(a.x, x, dtype)) != BLOAD_OK || (st = att_tensor(a.out, out, dtype)) != BLOAD_OK) return st;
+    if (!d_weight || !d_reset || !d_valid) return BLOAD_EINVAL;
+    const size_t e = att_elem_bytes(dtype);
+    if (!aligned_to(d_weight, 4) || !aligned_to(d_bias, 4) || !aligned_to(d_state_in, e) || !aligned_to(d_state_out, e)) return BLOAD_EALIGN;
+    if (!conv_states_apart(d_state_in, d_state_out, num_blocks * (taps - 1) * feat_dim * (int64_t)e, t_blk)) return BLOAD_EINVAL;
+    a.reset = d_reset;
+    a.valid = d_valid;
+    a.weight = d_weight;
+    a.bias = d_bias;
+    a.in = d_state_in;
+    a.last = d_state_out;
+    const dim3 grid((unsigned)(p.workgroups * p.slices)), block(kThreads);
+    by_dtype(dtype, [&](auto type) {
+        conv_dispatch_taps<typename decltype(type)::type, false>(feat_dim, taps, [&](auto t, auto v, auto k) {
+            using T = typename decltype(t)::type;
+            if (p.run == 1) conv_kernel<T, v, k, 1><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
+            else conv_kernel<T, v, k, 16><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
+        });
+    });
+    return launch_status();
+}
+
+extern "C" size_t bload_segment_conv_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t taps, bload_dtype dtype)
+{
+    if (num_blocks <= 0 || conv_check(num_blocks, t_blk, feat_dim, taps, dtype) != BLOAD_OK) return 0;
+    return round_up((size_t)conv_plan(num_blocks, t_blk, feat_dim, taps, dtype, true).workgroups * feat_dim * (taps + 1) * sizeof(float), 16);
+}
+
+extern "C" bload_status bload_segment_conv_backward(const bload_heads* dout, const bload_heads* x, const float* d_weight, const float* d_bias,
+                                                    const uint8_t* d_reset, const uint8_t* d_valid, int64_t num_blocks, int32_t t_blk,
+                                                    int32_t feat_dim, int32_t taps, bload_dtype dtype, int32_t silu, const void* d_state_in,
+                                                    const void* d_dstate_out, const bload_heads* dx, float* d_dweight, float* d_dbias,
+                                                    void* d_dstate_in, void* d_workspace, size_t workspace_bytes, void* hip_stream)
+{
+    bload_status st = conv_check(num_blocks, t_blk, feat_dim, taps, dtype);
+    if (st != BLOAD_OK) return st;
+    if (silu < 0 || silu > 1) return BLOAD_EINVAL;
+    if (!aligned_to(d_dweight, 4) || !aligned_to(d_dbias, 4)) return BLOAD_EALIGN;
+    const bool sums = d_dweight || d_dbias;
+    ColumnSums c = {};
+    c.dst[0] = d_dweight;
+    c.dst[1] = d_dbias;
+    c.end[0] = (int64_t)feat_dim * taps;
+    c.end[1] = c.columns = (int64_t)feat_dim * (taps + 1);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (num_blocks > 0) {
+        const ConvPlan p = conv_plan(num_blocks, t_blk, feat_dim, taps, dtype, true);
+        if (p.workgroups > kMaxGroups / p.slices) return BLOAD_EOVERFLOW;
+        ConvArgs a = conv_args(p, t_blk, feat_dim, silu);
+        if ((st = att_tensor(a.x, x, dtype)) != BLOAD_OK || (st = att_tensor(a.dout, dout, dtype)) != BLOAD_OK ||
+            (st = att_tensor(a.out, dx, dtype)) != BLOAD_OK)
+            return st;
+        if (!d_weight || !d_reset || !d_valid) return BLOAD_EINVAL;
+        const size_t e = att_elem_bytes(dtype);
+        if (!aligned_to(d_weight, 4) || !aligned_to(d_bias, 4) || !aligned_to(d_state_in, e) || !aligned_to(d_dstate_out, e) ||
+            !aligned_to(d_dstate_in, e))
+            return BLOAD_EALIGN;
+        const int64_t state = num_blocks * (taps - 1) * feat_dim * (int64_t)e;
+        if (!conv_states_apart(d_dstate_out, d_dstate_in, state, 9) || !conv_states_apart(d_state_in, d_dstate_in, state, 9)) return BLOAD_EINVAL;
+        if (sums) {
+            if (!d_workspace) return BLOAD_EINVAL;
+            if (!aligned_to(d_workspace, 16)) return BLOAD_EALIGN;
+            if (workspace_bytes < (size_t)p.workgroups * c.columns * sizeof(float)) return BLOAD_EWORKSPACE;
+            a.parts = static_cast<float*>(d_workspace);
+        }
+        a.reset = d_reset;
+        a.valid = d_valid;
+        a.weight = d_weight;
+        a.bias = d_bias;
+        a.in = d_state_in;
+        a.dlast = d_dstate_out;
+        a.last = d_dstate_in;
+        const dim3 grid((unsigned)(p.workgroups * p.slices)), block(kThreads);
+        const int64_t each = kThreads / p.F;
+        const size_t lds = std::max<size_t>(each * (p.run + taps), (size_t)p.F * p.V * (taps + 1) * sizeof(float));
+        by_dtype(dtype, [&](auto type) {
+            conv_dispatch_taps<typename decltype(type)::type, true>(feat_dim, taps, [&](auto t, auto v, auto k) {
+                conv_backward_kernel<typename decltype(t)::type, v, k><<<grid, block, lds, stream>>>(a);
+            });
+        });
+        if ((st = launch_status()) != BLOAD_OK) return st;
+        c.parts = a.parts;
+        c.n_parts = p.workgroups;
+    }
+    return sums ? column_sums(c, stream) : BLOAD_OK;
+}

@@ -1,0 +1,598 @@
+// bload_layer_norm: layer norm and root mean square norm of rows of features, forward and backward.
+//
+// A row is one slot's head (or all of a slot's features); with s = x, or the rounded sum of x and a residual,
+//     m = mean(s) (0 where it is not centred),  r = 1 / sqrt(mean((s - m)^2) + eps),  y = (s - m) r w + b
+// Backward, with g = dy w and u = (s - m) r:
+//     ds = r (g - mean(g) - u mean(g u)) + dsum  (no mean(g) where it is not centred),  dw = sum dy u,  db = sum dy
+//
+// HBM bound: a row is read once into registers and everything else is done there, the variance from the differences to
+// the mean, not from the squares.  A team of L lanes takes a row, P pieces of 16 bytes to a lane: 4 to 64 lanes of a wavefront, or a
+// workgroup.  The gradients of weights are a sum over all rows: every team keeps that of the rows it takes in registers,
+// workgroups leave theirs in the workspace, and a second kernel adds those in a fixed order, so the
+// same inputs give the same bits.  Rows too long for registers are read again from the cache.
+#include <algorithm>
+
+#include "bload_rows.hpp"
+
+namespace bload {
+namespace {
+
+struct NormArgs {
+    AttTensor x, res, out, sum;              // backward: x the rows that were normalised, res dsum, out dx
+    AttTensor dout;
+    const uint8_t* valid;                    // [B, T] or null
+    const float *weight, *bias;
+    float2* stats;                           // [rows]: mean, 1 / deviation
+    float* parts;                            // backward: [groups][2][D] or null
+    uint32_t rows;
+    Divisor H, T;
+    int32_t D, center;
+    float eps, inv;                          // inv: 1 / D
+};
+
+struct RowAt {
+    int64_t b, t, h;
+    __device__ __forceinline__ RowAt(const NormArgs& a, uint32_t row)
+    {
+        const uint32_t slot = over(row, a.H), block = over(slot, a.T);
+        h = row - slot * a.H.d;
+        t = slot - block * a.T.d;
+        b = block;
+    }
+    __device__ __forceinline__ bool live(const NormArgs& a) const { return !a.valid || a.valid[b * a.T.d + t]; }
+};
+
+// Sums over a team; a workgroup's goes through LDS, in one of two buffers in turn.
+template <int L>
+struct Team {
+    float (*room)[2][kThreads / kWave];
+    int turn = 0;
+    __device__ __forceinline__ void sum(float& a, float& b)
+    {
+        lanes_sum<(L < kWave ? L : kWave)>(a, b);
+        if constexpr (L > kWave) {
+            if (lane_id() == 0) {
+                room[turn][0][wave_id()] = a;
+                room[turn][1][wave_id()] = b;
+            }
+            __syncthreads();
+            a = b = 0.0f;
+#pragma unroll
+            for (int w = 0; w < L / kWave; ++w) a += room[turn][0][w], b += room[turn][1][w];
+            turn ^= 1;
+        }
+    }
+    __device__ __forceinline__ float sum(float a)
+    {
+        float none = 0.0f;
+        if constexpr (L <= kWave) return lanes_sum<L>(a);
+        sum(a, none);
+        return a;
+    }
+};
+
+// A lane's pieces of a row: where they begin, and how many elements in front of each are a neighbour's (all: V, none of it).
+template <int V, int P, int L>
+struct Places {
+    int at[P], skip[P];
+    __device__ __forceinline__ Places(int D, int lane)
+    {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const int d = (p * L + lane) * V;
+            at[p] = min(d, D - V);
+            skip[p] = min(d - at[p], V);
+        }
+    }
+};
+
+template <int V>
+__device__ __forceinline__ void blank(float (&x)[V], int skip)
+{
+    if (skip)
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = v < skip ? 0.0f : x[v];
+}
+
+// Teams of lanes of a wavefront take their rows alike; a lane without a row of its own takes part in the sums.
+template <typename T, int V, int P, int L>
+__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
+{
+    __shared__ float room[2][2][kThreads / kWave];
+    constexpr int kTeams = kThreads / L;
+    constexpr bool kHold = P * V <= 16;      // weights stay in registers from row to row
+    const int lane = (int)threadIdx.x % L;
+    const Places<V, P, L> places(a.D, lane);
+    Team<L> team{room};
+    float w[kHold ? P : 1][V], bias[kHold ? P : 1][V];
+    auto weights = [&](int p, float (&w)[V], float (&b)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) w[v] = 1.0f, b[v] = 0.0f;
+        if (a.weight) load_floats<V>(a.weight + places.at[p], w);
+        if (a.bias) load_floats<V>(a.bias + places.at[p], b);
+    };
+    if constexpr (kHold)
+#pragma unroll
+        for (int p = 0; p < P; ++p) weights(p, w[p], bias[p]);
+
+    const uint32_t step = gridDim.x * kTeams;
+    for (uint32_t row0 = blockIdx.x * kTeams; row0 < a.rows; row0 += step) {
+        const uint32_t row = row0 + (int)threadIdx.x / L;
+        const bool here = row < a.rows;
+        const RowAt at(a, here ? row : 0);
+        const bool live = here && at.live(a);
+        float x[P][V];
+        {
+            RowPiece<T, V> piece[P], more[P];
+            const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const bool mine = live && places.skip[p] < V;
+                piece[p].zero();
+                more[p].zero();
+                if (mine) piece[p].load(px + places.at[p]);
+                if (mine && a.res.p) more[p].load(pr + places.at[p]);
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[p][v] = piece[p][v];
+                if (a.res.p)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[p][v] = (float)(T)(x[p][v] + more[p][v]);
+                if (here && a.sum.p && places.skip[p] < V) store_row<T, V>(att_at<T>(a.sum, at.b, at.t, at.h) + places.at[p], x[p], places.skip[p]);
+                blank<V>(x[p], places.skip[p]);
+            }
+        }
+        float mean = 0.0f;
+        if (a.center) {
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int v = 0; v < V; ++v) mean += x[p][v];
+            mean = team.sum(mean) * a.inv;
+        }
+        float square = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[p][v] -= mean;
+            blank<V>(x[p], places.skip[p]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) square = fmaf(x[p][v], x[p][v], square);
+        }
+        const float r = rsqrtf(fmaf(team.sum(square), a.inv, a.eps));
+        if (!here) continue;
+        if (lane == 0 && a.stats) a.stats[row] = live ? make_float2(mean, r) : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (places.skip[p] >= V) continue;
+            float ww[V], bb[V], y[V];
+            if constexpr (!kHold) weights(p, ww, bb);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (kHold) ww[v] = w[p][v], bb[v] = bias[p][v];
+                y[v] = live ? fmaf(x[p][v] * r, ww[v], bb[v]) : 0.0f;
+            }
+            store_row<T, V>(att_at<T>(a.out, at.b, at.t, at.h) + places.at[p], y, places.skip[p]);
+        }
+    }
+}
+
+template <typename T, int V, int P, int L>
+__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a)
+{
+    __shared__ float room[2][2][kThreads / kWave];
+    constexpr int kTeams = kThreads / L;
+    constexpr bool kHold = P * V <= 16;
+    const int lane = (int)threadIdx.x % L;
+    const Places<V, P, L> places(a.D, lane);
+    Team<L> team{room};
+    float w[kHold ? P : 1][V], dw[P][V], db[P][V];
+    auto weights = [&](int p, float (&w)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) w[v] = 1.0f;
+        if (a.weight) load_floats<V>(a.weight + places.at[p], w);
+    };
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        if constexpr (kHold) weights(p, w[p]);
+#pragma unroll
+        for (int v = 0; v < V; ++v) dw[p][v] = db[p][v] = 0.0f;
+    }
+    const uint32_t step = gridDim.x * kTeams;
+    for (uint32_t row0 = blockIdx.x * kTeams; row0 < a.rows; row0 += step) {
+        const uint32_t row = row0 + (int)threadIdx.x / L;
+        const bool here = row < a.rows;
+        const RowAt at(a, here ? row : 0);
+        const bool live = here && at.live(a);
+        const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pd = att_at<T>(a.dout, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
+        RowPiece<T, V> x[P], dy[P], more[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool mine = live && places.skip[p] < V;
+            x[p].zero();
+            dy[p].zero();
+            more[p].zero();
+            if (mine) x[p].load(px + places.at[p]);
+            if (mine) dy[p].load(pd + places.at[p]);
+            if (mine && a.res.p) more[p].load(pr + places.at[p]);
+        }
+        const float2 stat = live ? a.stats[row] : make_float2(0.0f, 0.0f);
+        const float mean = a.center ? stat.x : 0.0f, r = stat.y;
+        float sum_g = 0.0f, sum_gu = 0.0f;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            float ww[V];
+            if constexpr (!kHold) weights(p, ww);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (kHold) ww[v] = w[p][v];
+                const float d = v < places.skip[p] ? 0.0f : dy[p][v], u = v < places.skip[p] ? 0.0f : (x[p][v] - mean) * r;
+                const float g = d * ww[v];
+                dw[p][v] = fmaf(d, u, dw[p][v]);
+                db[p][v] += d;
+                sum_g += g;
+                sum_gu = fmaf(g, u, sum_gu);
+            }
+        }
+        team.sum(sum_g, sum_gu);
+        const float c1 = a.center ? sum_g * a.inv : 0.0f, c2 = sum_gu * a.inv;
+        if (!here) continue;
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (places.skip[p] >= V) continue;
+            float ww[V], y[V];
+            if constexpr (!kHold) weights(p, ww);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if constexpr (kHold) ww[v] = w[p][v];
+                const float u = (x[p][v] - mean) * r;
+                y[v] = live ? fmaf(r, fmaf(-u, c2, fmaf(dy[p][v], ww[v], -c1)), more[p][v]) : 0.0f;
+            }
+            store_row<T, V>(att_at<T>(a.out, at.b, at.t, at.h) + places.at[p], y, places.skip[p]);
+        }
+    }
+    if (!a.parts) return;
+    float* part = a.parts + (int64_t)blockIdx.x * 2 * a.D;
+    if constexpr (L < kThreads) {
+        // the teams of a wavefront, then the wavefronts one after another
+        __shared__ float whole[2][P * L * V];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int d = L; d < kWave; d <<= 1) {
+                    dw[p][v] += __shfl_xor(dw[p][v], d);
+                    db[p][v] += __shfl_xor(db[p][v], d);
+                }
+        for (int turn = 0; turn < kThreads / kWave; ++turn) {
+            if (wave_id() == turn && lane_id() < L)
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const int n = (p * L + lane) * V + v;
+                        whole[0][n] = dw[p][v] + (turn ? whole[0][n] : 0.0f);
+                        whole[1][n] = db[p][v] + (turn ? whole[1][n] : 0.0f);
+                    }
+            __syncthreads();
+        }
+        // (element v of a piece is its row's element at + v; the last piece of a row lies `skip` further on in here)
+        if ((int)threadIdx.x < L)
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (v >= places.skip[p]) {
+                        const int n = (p * L + lane) * V + v;
+                        part[places.at[p] + v] = whole[0][n];
+                        part[a.D + places.at[p] + v] = whole[1][n];
+                    }
+    } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v >= places.skip[p]) {
+                    part[places.at[p] + v] = dw[p][v];
+                    part[a.D + places.at[p] + v] = db[p][v];
+                }
+    }
+}
+
+// Rows that no workgroup holds in its registers: one element a lane at a time, the row three times over, from the cache.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_long_kernel(NormArgs a)
+{
+    __shared__ float room[2][2][kThreads / kWave];
+    Team<kThreads> team{room};
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const RowAt at(a, row);
+        const bool live = at.live(a);
+        const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
+        T *po = att_at<T>(a.out, at.b, at.t, at.h), *ps = att_at<T>(a.sum, at.b, at.t, at.h);
+        if (!live) {
+            for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
+                po[d] = (T)0.0f;
+                if (a.sum.p) ps[d] = (T)0.0f;
+            }
+            if (threadIdx.x == 0 && a.stats) a.stats[row] = make_float2(0.0f, 0.0f);
+            continue;
+        }
+        auto value = [&](int d) { return a.res.p ? (float)(T)((float)px[d] + (float)pr[d]) : (float)px[d]; };
+        float mean = 0.0f, square = 0.0f;
+        if (a.center) {
+            for (int d = (int)threadIdx.x; d < a.D; d += kThreads) mean += value(d);
+            mean = team.sum(mean) * a.inv;
+        }
+        for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
+            const float x = value(d) - mean;
+            square = fmaf(x, x, square);
+        }
+        const float r = rsqrtf(fmaf(team.sum(square), a.inv, a.eps));
+        if (threadIdx.x == 0 && a.stats) a.stats[row] = make_float2(mean, r);
+        for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
+            const float s = value(d);
+            if (a.sum.p) ps[d] = (T)s;
+            po[d] = (T)fmaf((s - mean) * r, a.weight ? a.weight[d] : 1.0f, a.bias ? a.bias[d] : 0.0f);
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_long_backward_kernel(NormArgs a)
+{
+    __shared__ float room[2][2][kThreads / kWave];
+    Team<kThreads> team{room};
+    for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const RowAt at(a, row);
+        T* po = att_at<T>(a.out, at.b, at.t, at.h);
+        if (!at.live(a)) {
+            for (int d = (int)threadIdx.x; d < a.D; d += kThreads) po[d] = (T)0.0f;
+            continue;
+        }
+        const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pd = att_at<T>(a.dout, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
+        const float2 stat = a.stats[row];
+        const float mean = a.center ? stat.x : 0.0f, r = stat.y;
+        float sum_g = 0.0f, sum_gu = 0.0f;
+        for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
+            const float g = (float)pd[d] * (a.weight ? a.weight[d] : 1.0f);
+            sum_g += g;
+            sum_gu = fmaf(g, ((float)px[d] - mean) * r, sum_gu);
+        }
+        team.sum(sum_g, sum_gu);
+        const float c1 = a.center ? sum_g * a.inv : 0.0f, c2 = sum_gu * a.inv;
+        for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
+            const float g = (float)pd[d] * (a.weight ? a.weight[d] : 1.0f), u = ((float)px[d] - mean) * r;
+            po[d] = (T)fmaf(r, fmaf(-u, c2, g - c1), a.res.p ? (float)pr[d] : 0.0f);
+        }
+    }
+}
+
+// Its gradients of weights: a lane takes a column, a workgroup some of the rows.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_long_columns_kernel(NormArgs a, uint32_t each)
+{
+    const int d = (int)(blockIdx.y * kThreads + threadIdx.x);
+    if (d >= a.D) return;
+    float dw = 0.0f, db = 0.0f;
+    const uint32_t first = blockIdx.x * each;
+    for (uint32_t row = first; row < min(first + each, a.rows); ++row) {
+        const RowAt at(a, row);
+        if (!at.live(a)) continue;
+        const float2 stat = a.stats[row];
+        const float dy = (float)att_at<T>(a.dout, at.b, at.t, at.h)[d];
+        dw = fmaf(dy, ((float)att_at<T>(a.x, at.b, at.t, at.h)[d] - (a.center ? stat.x : 0.0f)) * stat.y, dw);
+        db += dy;
+    }
+    a.parts[(int64_t)blockIdx.x * 2 * a.D + d] = dw;
+    a.parts[((int64_t)blockIdx.x * 2 + 1) * a.D + d] = db;
+}
+
+// 64 columns to a workgroup, 16 lanes of four columns and 16 shares of the parts, whose sums are added in their order.
+__global__ __launch_bounds__(kThreads) void column_sums_kernel(ColumnSums a)
+{
+    constexpr int kShares = 16;
+    __shared__ float sums[kShares][64];
+    const int c = ((int)threadIdx.x % 16) * 4, share = (int)threadIdx.x / 16;
+    const int64_t first = (int64_t)blockIdx.x * 64 + c, each = (a.n_parts + kShares - 1) / kShares;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (first + 4 <= a.columns) {
+#pragma unroll 4
+        for (int64_t p = share * each; p < min((share + 1) * each, a.n_parts); ++p) {
+            float x[4];
+            load_floats<4>(a.parts + p * a.columns + first, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += x[i];
+        }
+    } else {
+        for (int64_t p = share * each; p < min((share + 1) * each, a.n_parts); ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (first + i < a.columns) s[i] += a.parts[p * a.columns + first + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[share][c + i] = s[i];
+    __syncthreads();
+    const int64_t column = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || column >= a.columns) return;
+    float y = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kShares; ++i) y += sums[i][threadIdx.x];
+    int64_t from = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (column >= from && column < a.end[i] && a.dst[i]) a.dst[i][column - from] = y;
+        from = a.end[i];
+    }
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int64_t kNormGroups = 1024;        // of the backward pass: each leaves a part of the weights' gradients
+
+// Pieces and lanes of a team.
+template <typename T, typename F>
+inline bool norm_dispatch(int32_t D, F f)
+{
+    constexpr int V = kRowPiece<T>;
+    using std::integral_constant;
+#define BLOAD_NORM_CASE(v, p, l) f(integral_constant<int, v>(), integral_constant<int, p>(), integral_constant<int, l>())
+    const int64_t n = ceil_div(D, V);
+    if (D < V) BLOAD_NORM_CASE(1, 1, 8);
+    else if (n <= 4) BLOAD_NORM_CASE(V, 1, 4);
+    else if (n <= 8) BLOAD_NORM_CASE(V, 1, 8);
+    else if (n <= 16) BLOAD_NORM_CASE(V, 1, 16);
+    else if (n <= 32) BLOAD_NORM_CASE(V, 1, 32);
+    else if (n <= 64) BLOAD_NORM_CASE(V, 1, 64);
+    else if (n <= 128) BLOAD_NORM_CASE(V, 2, 64);
+    else if (n <= 256) BLOAD_NORM_CASE(V, 1, 256);
+    else if (n <= 512) BLOAD_NORM_CASE(V, 2, 256);
+    else if (n <= 1024) BLOAD_NORM_CASE(V, 4, 256);
+    else if (n <= 2048) BLOAD_NORM_CASE(V, 8, 256);
+    else return false;
+#undef BLOAD_NORM_CASE
+    return true;
+}
+
+inline bload_status norm_check(int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype)
+{
+    if (num_blocks < 0 || t_blk < 1 || heads < 1 || dim < 1 || !att_dtype(dtype)) return BLOAD_EINVAL;
+    if (t_blk > (1 << 30) || dim > (1 << 30) || num_blocks > 0x7fffffffLL / t_blk / heads) return BLOAD_EOVERFLOW;
+    return BLOAD_OK;
+}
+
+// Workgroups of the backward pass and with that the parts that are added behind it.
+inline int64_t norm_groups(int64_t rows, int32_t dim, bload_dtype dtype)
+{
+    int64_t groups = 0;
+    auto by_type = [&](auto type) {
+        if (!norm_dispatch<typename decltype(type)::type>(dim, [&](auto, auto, auto l) {
+                groups = std::min<int64_t>(kNormGroups, ceil_div(rows, kThreads / decltype(l)::value));
+            }))
+            groups = std::min<int64_t>(kNormGroups, rows);
+    };
+    if (dtype == BLOAD_F32) by_type(type_is<float>());
+    else by_type(type_is<att_half>());
+    return groups;
+}
+
+inline NormArgs norm_args(int64_t rows, int32_t t_blk, int32_t heads, int32_t dim, int32_t center)
+{
+    NormArgs a = {};
+    a.rows = (uint32_t)rows;
+    a.H = divisor(heads);
+    a.T = divisor(t_blk);
+    a.D = dim;
+    a.center = center;
+    a.inv = 1.0f / (float)dim;
+    return a;
+}
+
+}  // namespace
+
+bload_status column_sums(const ColumnSums& a, hipStream_t stream)
+{
+    const int64_t groups = ceil_div(a.columns, 64);
+    if (groups > kMaxGroups) return BLOAD_EOVERFLOW;
+    if (groups > 0) column_sums_kernel<<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a);
+    return launch_status();
+}
+
+}  // namespace bload
+
+using namespace bload;
+
+extern "C" bload_status bload_layer_norm(const bload_heads* x, const bload_heads* residual, const uint8_t* d_valid, int64_t num_blocks,
+                                         int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype, int32_t center, float eps,
+                                         const float* d_weight, const float* d_bias, const bload_heads* out, const bload_heads* sum,
+                                         float* d_stats, void* hip_stream)
+{
+    bload_status st = norm_check(num_blocks, t_blk, heads, dim, dtype);
+    if (st != BLOAD_OK) return st;
+    if (center < 0 || center > 1 || !(eps >= 0.0f) || !std::isfinite(eps)) return BLOAD_EINVAL;
+    if (num_blocks == 0) return BLOAD_OK;
+    const int64_t rows = num_blocks * t_blk * heads;
+    NormArgs a = norm_args(rows, t_blk, heads, dim, center);
+    a.eps = eps;
+    if ((st = att_tensor(a.x, x, dtype)) != BLOAD_OK || (st = att_tensor(a.out, out, dtype)) != BLOAD_OK) return st;
+    if (residual && (st = att_tensor(a.res, residual, dtype)) != BLOAD_OK) return st;
+    if (sum && (st = att_tensor(a.sum, sum, dtype)) != BLOAD_OK) return st;
+    if (!aligned_to(d_weight, 4) || !aligned_to(d_bias, 4) || !aligned_to(d_stats, 8)) return BLOAD_EALIGN;
+    a.valid = d_valid;
+    a.weight = d_weight;
+    a.bias = d_bias;
+    a.stats = reinterpret_cast<float2*>(d_stats);
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    by_dtype(dtype, [&](auto type) {
+        using T = typename decltype(type)::type;
+        const bool held = norm_dispatch<T>(dim, [&](auto v, auto p, auto l) {
+            const int64_t groups = std::min<int64_t>(4096, ceil_div(rows, kThreads / l));
+            norm_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a);
+        });
+        if (!held) norm_long_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);
+    });
+    return launch_status();
+}
+
+extern "C" size_t bload_layer_norm_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype)
+{
+    if (num_blocks <= 0 || norm_check(num_blocks, t_blk, heads, dim, dtype) != BLOAD_OK) return 0;
+    return round_up((size_t)norm_groups(num_blocks * t_blk * heads, dim, dtype) * 2 * dim * sizeof(float), 16);
+}
+
+extern "C" bload_status bload_layer_norm_backward(const bload_heads* dout, const bload_heads* x, const float* d_stats, const uint8_t* d_valid,
+                                                  int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype,
+                                                  int32_t center, const float* d_weight, const bload_heads* dsum, const bload_heads* dx,
+                                                  float* d_dweight, float* d_dbias, void* d_workspace, size_t workspace_bytes,
+                                                  void* hip_stream)
+{
+    bload_status st = norm_check(num_blocks, t_blk, heads, dim, dtype);
+    if (st != BLOAD_OK) return st;
+    if (center < 0 || center > 1) return BLOAD_EINVAL;
+    if (!aligned_to(d_dweight, 4) || !aligned_to(d_dbias, 4)) return BLOAD_EALIGN;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t rows = num_blocks * t_blk * heads;
+    const bool sums = d_dweight || d_dbias;
+    ColumnSums c = {};
+    c.dst[0] = d_dweight;
+    c.dst[1] = d_dbias;
+    c.end[0] = dim;
+    c.end[1] = c.columns = 2 * (int64_t)dim;
+    if (rows > 0) {
+        NormArgs a = norm_args(rows, t_blk, heads, dim, center);
+        if ((st = att_tensor(a.x, x, dtype)) != BLOAD_OK || (st = att_tensor(a.dout, dout, dtype)) != BLOAD_OK ||
+            (st = att_tensor(a.out, dx, dtype)) != BLOAD_OK)
+            return st;
+        if (dsum && (st = att_tensor(a.res, dsum, dtype)) != BLOAD_OK) return st;
+        if (!d_stats) return BLOAD_EINVAL;
+        if (!aligned_to(d_stats, 8) || !aligned_to(d_weight, 4)) return BLOAD_EALIGN;
+        const int64_t groups = norm_groups(rows, dim, dtype);
+        if (sums) {
+            if (!d_workspace) return BLOAD_EINVAL;
+            if (!aligned_to(d_workspace, 16)) return BLOAD_EALIGN;
+            if (workspace_bytes < (size_t)groups * 2 * dim * sizeof(float)) return BLOAD_EWORKSPACE;
+            a.parts = static_cast<float*>(d_workspace);
+        }
+        a.valid = d_valid;
+        a.weight = d_weight;
+        a.stats = reinterpret_cast<float2*>(const_cast<float*>(d_stats));
+        by_dtype(dtype, [&](auto type) {
+            using T = typename decltype(type)::type;
+            const bool held = norm_dispatch<T>(dim, [&](auto v, auto p, auto l) {
+                norm_backward_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a);
+            });
+            if (held) return;
+            norm_long_backward_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);
+            const uint32_t each = (uint32_t)ceil_div(rows, groups);
+            if (sums)
+                norm_long_columns_kernel<T><<<dim3((unsigned)groups, (unsigned)ceil_div(dim, kThreads)), dim3(kThreads), 0, stream>>>(a, each);
+        });
+        if ((st = launch_status()) != BLOAD_OK) return st;
+        c.parts = a.parts;
+        c.n_parts = groups;
+    }
+    return sums ? column_sums(c, stream) : BLOAD_OK;
+}

@@ -1,0 +1,105 @@
+// What the kernels that go through rows of features share: pieces of 16 bytes at any alignment, division by sizes, slot flags.
+#pragma once
+
+#include "bload_attention_host.hpp"
+
+namespace bload {
+
+// V elements side by side, as they lie in memory; any alignment.
+template <typename T, int V>
+struct RowPiece {
+    T t[V];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(&t, p, sizeof(t)); }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] = (T)0.0f;
+    }
+    __device__ __forceinline__ float operator[](int v) const { return (float)t[v]; }
+};
+
+// Elements from `skip` on: those in front belong to the neighbouring lane.  A row that is no whole number of pieces ends with
+// a piece that overlaps the one in front of it, so that every load and nearly every store is whole.
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T* p, const float (&x)[V], int skip)
+{
+    if (skip == 0) {
+        T t[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] = (T)x[v];
+        __builtin_memcpy(p, &t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int v = 1; v < V; ++v)
+            if (v >= skip) p[v] = (T)x[v];
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float (&x)[V])
+{
+    __builtin_memcpy(&x, p, sizeof(x));
+}
+
+// Elements of a lane's piece: 16 bytes.
+template <typename T> constexpr int kRowPiece = 16 / (int)sizeof(T);
+
+// n / d for 0 <= n < 2^31: m = 2^(31 + s) / d rounded up, s = the bits of d - 1, is off by less than 1, so n m is off by less
+// than 2^31 of 2^(31 + s), which is below the 1 / d that separates two quotients.
+struct Divisor {
+    uint32_t d, m, s;
+};
+inline Divisor divisor(int64_t d)
+{
+    Divisor r = {(uint32_t)d, 0, 0};
+    while (((int64_t)1 << r.s) < d) ++r.s;
+    if (r.s) r.m = (uint32_t)((((uint64_t)1 << (31 + r.s)) + (uint64_t)d - 1) / (uint64_t)d);
+    return r;
+}
+__device__ __forceinline__ uint32_t over(uint32_t n, const Divisor& d) { return d.s ? __umulhi(n, d.m) >> (d.s - 1) : n; }
+
+// The sum of two values over the lanes of an aligned group of L (a power of two up to 64), in every lane of it.
+template <int L>
+__device__ __forceinline__ void lanes_sum(float& a, float& b)
+{
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) {
+        a += __shfl_xor(a, d);
+        b += __shfl_xor(b, d);
+    }
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float a)
+{
+#pragma unroll
+    for (int d = 1; d < L; d <<= 1) a += __shfl_xor(a, d);
+    return a;
+}
+
+// What a slot does: 0 padding, 1 starts a sequence, 2 goes on from the slot in front of it (the first one from a state).
+__device__ __forceinline__ int slot_does(const uint8_t* reset, const uint8_t* valid, int t, bool has_state)
+{
+    if (!valid[t]) return 0;
+    if (reset[t]) return 1;
+    return (t == 0 ? has_state : valid[t - 1] != 0) ? 2 : 1;
+}
+
+// Sums over what workgroups left, [n_parts][columns] float32 -> [columns], the parts in a fixed order (bload_norm.hip).
+// The columns up to end[0] go to dst[0], those from there to end[1] to dst[1] and so on; where it is null, nowhere.
+struct ColumnSums {
+    const float* parts;
+    int64_t n_parts, columns;
+    float* dst[4];
+    int64_t end[4];
+};
+bload_status column_sums(const ColumnSums& a, hipStream_t stream);
+
+template <typename F>
+inline void by_dtype(bload_dtype dtype, F f)
+{
+    if (dtype == BLOAD_F16) f(type_is<att_half>());
+    else if (dtype == BLOAD_BF16) f(type_is<att_bf16>());
+    else f(type_is<float>());
+}
+
+}  // namespace bload

@@ -1,0 +1,431 @@
+// bload_selective_scan_backward: the gradients of bload_selective_scan.
+//
+// With dy = dout z sigmoid(z) (or dout), and from the last slot to the first
+//     g_n = C_n dy + u_n,   u_n = a_n g_n for the slot in front (0 where this one does not go on),   p_n = u_n h_n(front)
+//     dC_n = sum_d dy h_n,   dB_n = sum_d step x g_n,   q = sum_n g_n B_n,   w = sum_n p_n A_n
+//     dx = step q + skip dy,   dstep = w + x q,   ddt = dstep sigmoid(dt + bias),   dA_n = sum p_n step,
+//     dskip = sum dy x,   dbias = sum ddt,   dz = dout y sigmoid(z) (1 + z (1 - sigmoid(z)))
+//
+// Lanes, tiles and chunks are those of the forward pass, whose state in front of every tile of 16 slots is read
+// back: from it a lane forms the tile's states again and keeps them, and the decays, in registers on the way back.  Sums over states
+// are exchanges between the four lanes of a channel; sums over channels (dB, dC) halve 2 NS values four times between 16 lanes,
+// then the workgroup's wavefronts through LDS, and leave a share for each slice of 64 channels, which a
+// last kernel adds in a fixed order.  The gradients of A, skip and bias stay in registers and are added by column_sums.
+#include <algorithm>
+
+#include "bload_selective.hpp"
+
+namespace bload {
+namespace {
+
+// One halving: of n values in every lane, n / 2, each with the partner's; lanes with `upper` keep the upper half.
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(float (&v)[N], int n, bool upper)
+{
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        if (i >= n / 2) break;
+        const float keep = upper ? v[i + n / 2] : v[i], send = upper ? v[i] : v[i + n / 2];
+        v[i] = keep + dpp_move<CTRL>(send, 0.0f);
+    }
+}
+constexpr int kMirror = 0x140, kHalfMirror = 0x141, kQuadSwap2 = 0x4e, kQuadSwap1 = 0xb1;
+
+// Of N (2, 4 or 8) values in every lane the sums over the 16 lanes of a row: the lane gets that of value `channel_value`.
+template <int N>
+__device__ __forceinline__ float sum_channels(float (&v)[N])
+{
+    const int lane = lane_id();
+    halve<kMirror, N>(v, N, lane & 8);
+    if constexpr (N >= 4) halve<kHalfMirror, N>(v, N / 2, lane & 4);
+    else v[0] += dpp_move<kHalfMirror>(v[0], 0.0f);
+    if constexpr (N >= 8) halve<kQuadSwap2, N>(v, N / 4, lane & 2);
+    else v[0] += dpp_move<kQuadSwap2>(v[0], 0.0f);
+    return v[0] + dpp_move<kQuadSwap1>(v[0], 0.0f);
+}
+template <int N>
+__device__ __forceinline__ int channel_value(int lane)
+{
+    return N == 8 ? lane >> 1 & 7 : (N == 4 ? lane >> 2 & 3 : lane >> 3 & 1);
+}
+template <int N> constexpr int kIdleLanes = N == 8 ? 1 : (N == 4 ? 3 : 7);      // bits of lanes that hold a copy
+
+// A thread's part of a tile.
+template <typename T, int NP>
+struct Staged {
+    static constexpr int kBC = (NP + 15) / 16;
+    Four<T> x, dt, z, dout;
+    T b[kBC], c[kBC];
+    __device__ __forceinline__ void load(const ScanArgs& a, const ScanPlace& at, int t0, int end, bool maps)
+    {
+        const int t = t0 + at.slot;
+        const bool here = t < end && t >= 0;
+        x.zero(), dt.zero(), z.zero(), dout.zero();
+        if (here && at.n_four) {
+            if (!maps) x.load(a.x, at.b, t, at.four, at.n_four);
+            dt.load(a.dt, at.b, t, at.four, at.n_four);
+            dout.load(a.dout, at.b, t, at.four, at.n_four);
+            if (a.z.p) z.load(a.z, at.b, t, at.four, at.n_four);
+        }
+#pragma unroll
+        for (int k = 0; k < kBC; ++k) {
+            const int n = 16 * k + (int)threadIdx.x % 16;
+            b[k] = c[k] = (T)0.0f;
+            if (here && n < a.N) {
+                if (!maps) b[k] = att_at<T>(a.b, at.b, t, at.group)[n];
+                c[k] = att_at<T>(a.c, at.b, t, at.group)[n];
+            }
+        }
+    }
+};
+
+// A chunk's own part of the gradient in front of it, from its end to its start.
+template <typename T, int NS, int PARTS>
+__global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a)
+{
+    constexpr int NP = 4 * NS * PARTS;
+    __shared__ float2 steps[kTile][kGroupC];               // step, dy
+    __shared__ __attribute__((aligned(16))) float cs[kTile][NP];
+    const ScanPlace at(a, blockIdx.x);
+    const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
+    float u[PARTS][NS], rate[PARTS][NS], bias[4];
+    load_states<NS, PARTS>(a.rate, 0, a, at, rate);
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) rate[p][i] *= kLog2e, u[p][i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bias[i] = a.dt_bias && i < at.n_four ? a.dt_bias[at.four + i] : 0.0f;
+    float span = 0.0f;
+    bool any_cut = false;
+    Staged<T, NP> in;
+    const int last_tile = first + (end - first - 1) / kTile * kTile;
+    in.load(a, at, last_tile, end, true);
+    for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
+        const TileFlags flags(a, at.b, t0, end, a.in != nullptr);
+        const bool live = flags.live >> at.slot & 1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v = in.dt[i] + bias[i];
+            float dy = in.dout[i];
+            if (a.z.p) dy *= in.z[i] * logistic(in.z[i]);
+            steps[at.slot][4 * (threadIdx.x % 16) + i] = make_float2(live ? (a.softplus ? softplus(v) : v) : 0.0f, live ? dy : 0.0f);
+        }
+#pragma unroll
+        for (int k = 0; k < in.kBC; ++k) {
+            const int n = 16 * k + (int)threadIdx.x % 16;
+            if (n < NP) cs[at.slot][n] = live ? (float)in.c[k] : 0.0f;
+        }
+        __syncthreads();
+        if (t0 > first) in.load(a, at, t0 - kTile, end, true);
+#pragma unroll
+        for (int t = kTile - 1; t >= 0; --t) {
+            const float2 s = steps[t][col];
+            span += s.x;
+            if (flags.live >> t & 1)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    float cc[NS];
+                    __builtin_memcpy(&cc, &cs[t][(p * 4 + at.q) * NS], sizeof(cc));
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) u[p][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]) * fmaf(cc[i], s.y, u[p][i]);
+                }
+            if (flags.cut >> t & 1)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
+        }
+        any_cut |= flags.cut != 0;
+        __syncthreads();
+    }
+    const int64_t row = at.b * a.chunks + at.chunk;
+    store_states<NS, PARTS>(a.maps, row, a, at, u);
+    if (at.mine && at.q == 0) a.spans[row * a.D + at.d] = span;
+    if (threadIdx.x == 0 && at.d0 == 0) a.cut[row] = any_cut;
+}
+
+template <typename T, int NS, int PARTS>
+__global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanArgs a)
+{
+    constexpr int NP = 4 * NS * PARTS, kWaves = kThreads / kWave;
+    __shared__ float2 steps[kTile][kGroupC];               // step, step x
+    __shared__ float dys[kTile][kGroupC], ys[kTile][kGroupC], qs[kTile][kGroupC], ws[kTile][kGroupC];
+    __shared__ __attribute__((aligned(16))) float bs[kTile][NP], cs[kTile][NP];
+    __shared__ float sums[kWaves][kTile][2][NP];           // dB and dC of a wavefront's channels
+    ScanPlace at(a, blockIdx.x);
+    const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
+    const int64_t part = at.b * a.chunks + at.chunk;
+    const bool has_state = a.in != nullptr, gated = a.z.p != nullptr;
+
+    float rate[PARTS][NS], drate[PARTS][NS];
+    load_states<NS, PARTS>(a.rate, 0, a, at, rate);
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) rate[p][i] *= kLog2e, drate[p][i] = 0.0f;
+    float skip[4], bias[4], dskip[4], dbias[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        skip[i] = a.skip && i < at.n_four ? a.skip[at.four + i] : 0.0f;
+        bias[i] = a.dt_bias && i < at.n_four ? a.dt_bias[at.four + i] : 0.0f;
+        dskip[i] = dbias[i] = 0.0f;
+    }
+    for (; at.b < a.B; at.b += a.blocks) {
+        float u[PARTS][NS];
+        if (a.chunks > 1) load_states<NS, PARTS>(a.maps, at.b * a.chunks + at.chunk, a, at, u);
+        else load_states<NS, PARTS>(a.dlast, at.b, a, at, u);
+        Staged<T, NP> in;
+        const int last_tile = first + (end - first - 1) / kTile * kTile;
+        in.load(a, at, last_tile, end, false);
+        for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
+            const TileFlags flags(a, at.b, t0, end, has_state);
+            const bool live = flags.live >> at.slot & 1;
+            const Staged<T, NP> now = in;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = now.dt[i] + bias[i], step = live ? (a.softplus ? softplus(v) : v) : 0.0f;
+                float dy = now.dout[i];
+                if (gated) dy *= now.z[i] * logistic(now.z[i]);
+                const int c = 4 * (threadIdx.x % 16) + i;
+                steps[at.slot][c] = make_float2(step, live ? step * now.x[i] : 0.0f);
+                dys[at.slot][c] = live ? dy : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < now.kBC; ++k) {
+                const int n = 16 * k + (int)threadIdx.x % 16;
+                if (n < NP) {
+                    bs[at.slot][n] = live ? (float)now.b[k] : 0.0f;
+                    cs[at.slot][n] = live ? (float)now.c[k] : 0.0f;
+                }
+            }
+            float h0[PARTS][NS];
+            load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0);
+            __syncthreads();
+            if (t0 > first) in.load(a, at, t0 - kTile, end, false);
+
+            float y[kTile], q[kTile], w[kTile];
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) y[t] = q[t] = w[t] = 0.0f;
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const int n0 = (p * 4 + at.q) * NS;
+                float h[kTile + 1][NS], decay[kTile][NS];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) h[0][i] = h0[p][i];
+#pragma unroll
+                for (int t = 0; t < kTile; ++t) {
+                    const float2 s = steps[t][col];
+                    float bb[NS];
+                    __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
+                    const bool cut = flags.cut >> t & 1;
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) {
+                        decay[t][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]);
+                        h[t + 1][i] = fmaf(decay[t][i], cut ? 0.0f : h[t][i], s.y * bb[i]);
+                    }
+                    if (gated) {
+                        float cc[NS];
+                        __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) y[t] = fmaf(cc[i], h[t + 1][i], y[t]);
+                    }
+                }
+#pragma unroll
+                for (int t = kTile - 1; t >= 0; --t) {
+                    if (flags.live >> t & 1) {
+                        const float2 s = steps[t][col];
+                        const float dy = dys[t][col];
+                        const bool cut = flags.cut >> t & 1;
+                        float bb[NS], cc[NS], v[2 * NS];
+                        __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
+                        __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) {
+                            const float g = fmaf(cc[i], dy, u[p][i]);
+                            v[i] = s.y * g;
+                            v[NS + i] = dy * h[t + 1][i];
+                            q[t] = fmaf(g, bb[i], q[t]);
+                            u[p][i] = cut ? 0.0f : decay[t][i] * g;
+                            const float k = u[p][i] * (cut ? 0.0f : h[t][i]);
+                            w[t] = fmaf(k, rate[p][i], w[t]);
+                            drate[p][i] = fmaf(k, s.x, drate[p][i]);
+                        }
+                        const float sum = sum_channels<2 * NS>(v);
+                        const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);
+                        if ((lane & kIdleLanes<2 * NS>) == 0) sums[wave_id()][t][value / NS][n0 + value % NS] = sum;
+                    } else if (flags.cut >> t & 1) {
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTile; t += 4) {
+                qs[t + at.q][col] = sum_states(q[t], q[t + 1], q[t + 2], q[t + 3]);
+                ws[t + at.q][col] = sum_states(w[t], w[t + 1], w[t + 2], w[t + 3]);
+                if (gated) ys[t + at.q][col] = sum_states(y[t], y[t + 1], y[t + 2], y[t + 3]);
+            }
+            __syncthreads();
+            if (t0 + at.slot < end && at.n_four) {
+                float dx[4], ddt[4], dz[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = 4 * (threadIdx.x % 16) + i;
+                    const float x = now.x[i], dy = dys[at.slot][c], qq = qs[at.slot][c];
+                    dx[i] = fmaf(steps[at.slot][c].x, qq, skip[i] * dy);
+                    ddt[i] = fmaf(x, qq, ws[at.slot][c] * kLn2);
+                    if (a.softplus) ddt[i] *= logistic(now.dt[i] + bias[i]);
+                    if (gated) {
+                        const float z = now.z[i], sg = logistic(z);
+                        dz[i] = now.dout[i] * fmaf(skip[i], x, ys[at.slot][c]) * sg * fmaf(z, 1.0f - sg, 1.0f);
+                    }
+                    if (!live) dx[i] = ddt[i] = dz[i] = 0.0f;
+                    else dskip[i] = fmaf(dy, x, dskip[i]), dbias[i] += ddt[i];
+                }
+                store_four<T>(a.dx, at.b, t0 + at.slot, at.four, at.n_four, dx);
+                store_four<T>(a.ddt, at.b, t0 + at.slot, at.four, at.n_four, ddt);
+                if (gated) store_four<T>(a.dz, at.b, t0 + at.slot, at.four, at.n_four, dz);
+            }
+            // this slice's share of dB and dC
+            const int64_t slice = (at.d0 - at.group * a.per) / kGroupC;
+            for (int n = (int)threadIdx.x; n < kTile * 2 * NP; n += kThreads) {
+                const int t = n / (2 * NP), which = n / NP % 2, k = n % NP;
+                if (k >= a.N || t0 + t >= end) continue;
+                float s = 0.0f;
+                if (flags.live >> t & 1)
+#pragma unroll
+                    for (int wave = 0; wave < kWaves; ++wave) s += sums[wave][t][which][k];
+                a.shares[((((slice * a.B + at.b) * a.T + t0 + t) * a.G + at.group) * 2 + which) * a.N + k] = s;
+            }
+            __syncthreads();
+        }
+        if (a.last && a.chunks == 1) store_states<NS, PARTS>(a.last, at.b, a, at, u);
+    }
+    float* to = a.parts + part * a.D * (a.N + 2);
+    store_states<NS, PARTS>(to, 0, a, at, drate);
+    // dskip and dbias of the 16 slots of a tile, one after another
+    to += (int64_t)a.D * a.N;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        qs[at.slot][4 * (threadIdx.x % 16) + i] = dskip[i];
+        ws[at.slot][4 * (threadIdx.x % 16) + i] = dbias[i];
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < kGroupC && at.d0 + (int)threadIdx.x < at.d1) {
+        float s = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kTile; ++t) s += qs[t][threadIdx.x], b += ws[t][threadIdx.x];
+        to[at.d0 + threadIdx.x] = s;
+        to[a.D + at.d0 + threadIdx.x] = b;
+    }
+}
+
+// dB and dC: the slices' shares, added in their order.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void scan_shares_kernel(ScanArgs a, int64_t all)
+{
+    const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (n >= all) return;
+    float s = 0.0f;
+#pragma unroll 8
+    for (int slice = 0; slice < a.slices; ++slice) s += a.shares[slice * all + n];
+    const int64_t row = n / a.N, pair = row / 2, slot = pair / a.G, b = slot / a.T;
+    att_at<T>(row % 2 ? a.dc : a.db, b, slot - b * a.T, pair - slot * a.G)[n - row * a.N] = (T)s;
+}
+
+struct BackRoom {
+    size_t maps, spans, cut, shares, parts, bytes;
+    int64_t n_parts;
+};
+inline BackRoom back_room(ScanArgs& a)
+{
+    BackRoom r = {};
+    const int64_t each = (int64_t)a.chunks * a.G * a.slices;
+    a.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(a.B, ceil_div(4096, each)));
+    r.n_parts = (int64_t)a.blocks * a.chunks;
+    if (a.chunks > 1) {
+        r.maps = round_up((size_t)a.B * a.chunks * a.D * a.N * sizeof(float), 16);
+        r.spans = round_up((size_t)a.B * a.chunks * a.D * sizeof(float), 16);
+        r.cut = round_up((size_t)a.B * a.chunks, 16);
+    }
+    r.shares = round_up((size_t)a.slices * a.B * a.T * a.G * 2 * a.N * sizeof(float), 16);
+    r.parts = round_up((size_t)r.n_parts * a.D * (a.N + 2) * sizeof(float), 16);
+    r.bytes = r.maps + r.spans + r.cut + r.shares + r.parts;
+    return r;
+}
+
+}  // namespace
+}  // namespace bload
+
+using namespace bload;
+
+extern "C" size_t bload_selective_scan_backward_workspace_bytes(int64_t num_blocks, int32_t t_blk, int32_t feat_dim, int32_t states, int32_t groups)
+{
+    ScanArgs a = {};
+    if (num_blocks <= 0 || scan_sizes(a, num_blocks, t_blk, feat_dim, states, groups, BLOAD_F32) != BLOAD_OK) return 0;
+    return back_room(a).bytes;
+}
+
+extern "C" bload_status bload_selective_scan_backward(const bload_selective* s, const bload_heads* dout, const float* d_saved,
+                                                      const float* d_dstate_out, const bload_heads* dx, const bload_heads* ddt,
+                                                      float* d_drate, const bload_heads* db, const bload_heads* dc, float* d_dskip,
+                                                      const bload_heads* dz, float* d_ddt_bias, float* d_dstate_in, void* d_workspace,
+                                                      size_t workspace_bytes, void* hip_stream)
+{
+    ScanArgs a;
+    bload_status st = scan_args(a, s);
+    if (st != BLOAD_OK) return st;
+    if (!aligned_to(d_drate, 4) || !aligned_to(d_dskip, 4) || !aligned_to(d_ddt_bias, 4)) return BLOAD_EALIGN;
+    ColumnSums c = {};
+    c.dst[0] = d_drate;
+    c.dst[1] = d_dskip;
+    c.dst[2] = d_ddt_bias;
+    c.end[0] = (int64_t)s->feat_dim * s->states;
+    c.end[1] = c.end[0] + s->feat_dim;
+    c.end[2] = c.columns = c.end[1] + s->feat_dim;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    if (a.B > 0) {
+        const bload_dtype dtype = s->dtype;
+        if ((st = att_tensor(a.dout, dout, dtype)) != BLOAD_OK || (st = att_tensor(a.dx, dx, dtype)) != BLOAD_OK ||
+            (st = att_tensor(a.ddt, ddt, dtype)) != BLOAD_OK || (st = att_tensor(a.db, db, dtype)) != BLOAD_OK ||
+            (st = att_tensor(a.dc, dc, dtype)) != BLOAD_OK)
+            return st;
+        if (a.z.p && (st = att_tensor(a.dz, dz, dtype)) != BLOAD_OK) return st;
+        if (!d_saved) return BLOAD_EINVAL;
+        if (!aligned_to(d_saved, 4) || !aligned_to(d_dstate_out, 4) || !aligned_to(d_dstate_in, 4)) return BLOAD_EALIGN;
+        if (states_meet(d_dstate_out, d_dstate_in, a, false) || states_meet(a.in, d_dstate_in, a, false)) return BLOAD_EINVAL;
+        const BackRoom room = back_room(a);
+        if (!d_workspace) return BLOAD_EINVAL;
+        if (!aligned_to(d_workspace, 16)) return BLOAD_EALIGN;
+        if (workspace_bytes < room.bytes) return BLOAD_EWORKSPACE;
+        const int64_t all = a.B * (int64_t)a.T * a.G * 2 * a.N, groups = ceil_div(all, kThreads);
+        if (groups > kMaxGroups) return BLOAD_EOVERFLOW;
+        char* p = static_cast<char*>(d_workspace);
+        a.maps = reinterpret_cast<float*>(p);
+        a.spans = reinterpret_cast<float*>(p += room.maps);
+        a.cut = reinterpret_cast<uint8_t*>(p += room.spans);
+        a.shares = reinterpret_cast<float*>(p += room.cut);
+        a.parts = reinterpret_cast<float*>(p += room.shares);
+        a.saved = const_cast<float*>(d_saved);
+        a.dlast = d_dstate_out;
+        a.last = d_dstate_in;
+        const dim3 block(kThreads);
+        const int64_t each = (int64_t)a.chunks * a.G * a.slices;
+        by_dtype(dtype, [&](auto type) {
+            scan_by_states(a.N, [&](auto ns, auto parts) {
+                using T = typename decltype(type)::type;
+                if (a.chunks > 1) {
+                    scan_backward_maps_kernel<T, ns, parts><<<dim3((unsigned)(a.B * each)), block, 0, stream>>>(a);
+                    scan_join(a, a.dlast, true, stream);
+                }
+                scan_backward_kernel<T, ns, parts><<<dim3((unsigned)(a.blocks * each)), block, 0, stream>>>(a);
+                scan_shares_kernel<T><<<dim3((unsigned)groups), block, 0, stream>>>(a, all);
+            });
+        });
+        if ((st = launch_status()) != BLOAD_OK) return st;
+        c.parts = a.parts;
+        c.n_parts = room.n_parts;
+    }
+    return d_drate || d_dskip || d_ddt_bias ? column_sums(c, stream) : BLOAD_OK;
+}
