@@ -5,17 +5,31 @@
 
 namespace bload {
 
-// V elements side by side, as they lie in memory; any alignment.
+// V elements side by side, as they lie in memory; any alignment.  They stay the words that were loaded until they are used: taken
+// apart behind the load, each load is waited for before the next is sent.
 template <typename T, int V>
 struct RowPiece {
-    T t[V];
-    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(&t, p, sizeof(t)); }
+    static constexpr int kWords = V * sizeof(T) >= 4 ? V * (int)sizeof(T) / 4 : 1;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(&w, p, V * sizeof(T)); }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) t[v] = (T)0.0f;
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
     }
-    __device__ __forceinline__ float operator[](int v) const { return (float)t[v]; }
+    __device__ __forceinline__ float operator[](int v) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(w[v]);
+        } else if constexpr (std::is_same<T, att_bf16>::value) {
+            return __uint_as_float(v % 2 ? w[v / 2] & 0xffff0000u : w[v / 2] << 16);
+        } else {
+            const uint16_t half = (uint16_t)(v % 2 ? w[v / 2] >> 16 : w[v / 2]);
+            T t;
+            __builtin_memcpy(&t, &half, 2);
+            return (float)t;
+        }
+    }
 };
 
 // Elements from `skip` on: those in front belong to the neighbouring lane.  A row that is no whole number of pieces ends with

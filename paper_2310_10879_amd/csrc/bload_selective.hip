@@ -22,15 +22,18 @@
 namespace bload {
 namespace {
 
+// LDS holds two tiles: while one is computed the next is staged and the results of the one in front go out, with one barrier a tile.
+// What a lane reads of LDS for four slots it reads while it computes the four in front of them.
 template <typename T, int NS, int PARTS, bool MAPS>
-__global__ __launch_bounds__(kThreads) void scan_kernel(ScanArgs a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))) void scan_kernel(ScanArgs a)
 {
     constexpr int NP = 4 * NS * PARTS;
-    __shared__ float2 steps[kTile][kGroupC];               // step, step x
-    __shared__ __attribute__((aligned(16))) float bs[kTile][NP], cs[MAPS ? 1 : kTile][NP];
-    __shared__ float ys[MAPS ? 1 : kTile][kGroupC];
+    __shared__ __attribute__((aligned(16))) float2 steps[2][kTile][kGroupC];           // step, step x
+    __shared__ __attribute__((aligned(16))) float bs[2][kTile][NP], cs[2][MAPS ? 1 : kTile][NP];
+    __shared__ __attribute__((aligned(16))) float ys[2][MAPS ? 1 : kTile][kGroupC];
     const ScanPlace at(a, blockIdx.x);
     const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
+    const int four = at.four - at.d0;
     const bool has_state = a.in != nullptr;
 
     float h[PARTS][NS], rate[PARTS][NS];
@@ -52,102 +55,108 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(ScanArgs a)
     float span = 0.0f;                                     // MAPS: the lane's channel's steps so far
     bool any_cut = false;
 
-    // what a thread stages of a tile, on its way while the tile in front is computed
-    constexpr int kBC = (NP + 15) / 16;
-    Four<T> x, dt, z;
-    T b[kBC], c[kBC];
+    Stream<T> px(a.x, at, first), pdt(a.dt, at, first), pz(a.z, at, first), pout(a.out, at, first);
+    PairStream<T, NP> pb(a.b, a, at, first), pc(a.c, a, at, first);
+    Four<T> x, dt, z;                                      // of the tile that is staged next
     auto load = [&](int t0) {
-        const int t = t0 + at.slot;
-        const bool here = t < end;
-        x.zero(), dt.zero(), z.zero();
-        if (here && at.n_four) {
-            x.load(a.x, at.b, t, at.four, at.n_four);
-            dt.load(a.dt, at.b, t, at.four, at.n_four);
-            if (!MAPS && a.z.p) z.load(a.z, at.b, t, at.four, at.n_four);
-        }
-#pragma unroll
-        for (int k = 0; k < kBC; ++k) {
-            const int n = 16 * k + (int)threadIdx.x % 16;
-            b[k] = c[k] = (T)0.0f;
-            if (here && n < a.N) {
-                b[k] = att_at<T>(a.b, at.b, t, at.group)[n];
-                if (!MAPS) c[k] = att_at<T>(a.c, at.b, t, at.group)[n];
-            }
-        }
+        const bool here = t0 + at.slot < end;
+        px.load(x, here);
+        pdt.load(dt, here);
+        if (!MAPS) pz.load(z, here && a.z.p);
+        pb.load(here);
+        if (!MAPS) pc.load(here);
     };
-    load(first);
-    for (int t0 = first; t0 < end; t0 += kTile) {
-        const TileFlags flags(a, at.b, t0, end, has_state);
+    auto stage = [&](int buf, const TileFlags& flags) {
         const bool live = flags.live >> at.slot & 1;
+        float2 s[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float v = dt[i] + bias[i], step = live ? (a.softplus ? softplus(v) : v) : 0.0f;
-            steps[at.slot][4 * (threadIdx.x % 16) + i] = make_float2(step, live ? step * x[i] : 0.0f);
+            const float v = dt[i] + bias[i], step = a.softplus ? softplus(v) : v;
+            s[i] = live ? make_float2(step, step * x[i]) : make_float2(0.0f, 0.0f);
         }
+        if (at.n_four) __builtin_memcpy(&steps[buf][at.slot][four], &s, sizeof(s));
+        pb.stage(bs[buf][at.slot], live);
+        if (!MAPS) pc.stage(cs[buf][MAPS ? 0 : at.slot], live);
+    };
+    // results of a tile: the thread's four channels of its slot
+    auto finish = [&](int buf, bool here, bool live, const Four<T>& x, const Four<T>& z) {
+        if (!here) return;
+        float y[4];
+        __builtin_memcpy(&y, &ys[buf][MAPS ? 0 : at.slot][four], sizeof(y));
 #pragma unroll
-        for (int k = 0; k < kBC; ++k) {
-            const int n = 16 * k + (int)threadIdx.x % 16;
-            if (n < NP) {
-                bs[at.slot][n] = live ? (float)b[k] : 0.0f;
-                if (!MAPS) cs[at.slot][n] = live ? (float)c[k] : 0.0f;
-            }
+        for (int i = 0; i < 4; ++i) {
+            y[i] = fmaf(skip[i], x[i], y[i]);
+            if (a.z.p) y[i] *= z[i] * logistic(z[i]);
+            if (!live) y[i] = 0.0f;
         }
-        const Four<T> x_now = x, z_now = z;
-        __syncthreads();
-        if (t0 + kTile < end) load(t0 + kTile);
+        pout.store(y);
+    };
+
+    load(first);
+    for (int n = (int)threadIdx.x; n < 2 * kTile * kGroupC; n += kThreads) (&steps[0][0][0])[n] = make_float2(0.0f, 0.0f);
+    __syncthreads();                                       // (columns without a channel stay 0)
+    TileFlags flags(a, at.b, first, end, has_state);
+    stage(0, flags);
+    Four<T> x_now = x, z_now = z, x_before = x, z_before = z;
+    bool live_before = false;
+    int buf = 0;
+    for (int t0 = first; t0 < end; t0 += kTile, buf ^= 1) {
+        __syncthreads();                                   // this tile is staged, the results of the one in front are there
+        const bool more = t0 + kTile < end;
+        if (more) load(t0 + kTile);
         if (!MAPS && a.saved) store_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h);
 
-        auto slot = [&](int t) {
-            const float2 s = steps[t][col];
-            float y = 0.0f;
+        float2 s[2][4];
+        float bb[2][4][NS], cc[2][4][NS], y[4];
+        auto read = [&](int e) {                           // four slots of one part
+            const int g = e / PARTS, p = e % PARTS, n0 = (p * 4 + at.q) * NS;
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                float bb[NS], cc[NS];
-                __builtin_memcpy(&bb, &bs[t][(p * 4 + at.q) * NS], sizeof(bb));
-                if constexpr (!MAPS) __builtin_memcpy(&cc, &cs[t][(p * 4 + at.q) * NS], sizeof(cc));
-#pragma unroll
-                for (int i = 0; i < NS; ++i) {
-                    h[p][i] = fmaf(__builtin_amdgcn_exp2f(s.x * rate[p][i]), h[p][i], s.y * bb[i]);
-                    if constexpr (!MAPS) y = fmaf(cc[i], h[p][i], y);
-                }
+            for (int i = 0; i < 4; ++i) {
+                if (p == 0) s[g & 1][i] = steps[buf][4 * g + i][col];
+                __builtin_memcpy(&bb[e & 1][i], &bs[buf][4 * g + i][n0], sizeof(bb[0][0]));
+                if (!MAPS) __builtin_memcpy(&cc[e & 1][i], &cs[buf][MAPS ? 0 : 4 * g + i][n0], sizeof(cc[0][0]));
             }
-            if (MAPS) span += s.x;
-            return y;
         };
-        auto drop = [&] {
+        read(0);
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p)
+        for (int e = 0; e < 4 * PARTS; ++e) {
+            const int g = e / PARTS, p = e % PARTS;
+            if (e + 1 < 4 * PARTS) read(e + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (p == 0)
 #pragma unroll
-                for (int i = 0; i < NS; ++i) h[p][i] = 0.0f;
-        };
+                for (int i = 0; i < 4; ++i) y[i] = 0.0f;
+            auto slot = [&](int i) {
+                const float2 v = s[g & 1][i];
 #pragma unroll
-        for (int t = 0; t < kTile; t += 4) {
-            float y[4];
-            if ((flags.cut >> t & 15) == 0) {
+                for (int k = 0; k < NS; ++k) {
+                    h[p][k] = fmaf(__builtin_amdgcn_exp2f(v.x * rate[p][k]), h[p][k], v.y * bb[e & 1][i][k]);
+                    if constexpr (!MAPS) y[i] = fmaf(cc[e & 1][i][k], h[p][k], y[i]);
+                }
+                if (MAPS && p == 0) span += v.x;
+            };
+            if ((flags.cut >> (4 * g) & 15) == 0) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = slot(t + i);
+                for (int i = 0; i < 4; ++i) slot(i);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (flags.cut >> (t + i) & 1) drop();
-                    y[i] = slot(t + i);
+                    if (flags.cut >> (4 * g + i) & 1)
+#pragma unroll
+                        for (int k = 0; k < NS; ++k) h[p][k] = 0.0f;
+                    slot(i);
                 }
             }
-            if constexpr (!MAPS) ys[t + at.q][col] = sum_states(y[0], y[1], y[2], y[3]);
+            if (!MAPS && p == PARTS - 1) ys[buf][MAPS ? 0 : 4 * g + at.q][col] = sum_states(y[0], y[1], y[2], y[3]);
         }
         any_cut |= flags.cut != 0;
-        __syncthreads();
-        if constexpr (!MAPS) {
-            if (t0 + at.slot < end && at.n_four) {
-                float y[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    y[i] = fmaf(skip[i], x_now[i], ys[at.slot][4 * (threadIdx.x % 16) + i]);
-                    if (a.z.p) y[i] *= z_now[i] * logistic(z_now[i]);
-                    if (!live) y[i] = 0.0f;
-                }
-                store_four<T>(a.out, at.b, t0 + at.slot, at.four, at.n_four, y);
-            }
+        if (!MAPS && t0 > first) finish(buf ^ 1, at.n_four > 0, live_before, x_before, z_before);
+        live_before = flags.live >> at.slot & 1;
+        x_before = x_now, z_before = z_now;
+        if (more) {
+            flags = TileFlags(a, at.b, t0 + kTile, end, has_state);
+            stage(buf ^ 1, flags);
+            x_now = x, z_now = z;
         }
     }
     if (MAPS) {
@@ -155,8 +164,10 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(ScanArgs a)
         store_states<NS, PARTS>(a.maps, row, a, at, h);
         if (at.mine && at.q == 0) a.spans[row * a.D + at.d] = span;
         if (threadIdx.x == 0 && at.d0 == 0) a.cut[row] = any_cut;
-    } else if (a.last && end == a.T) {
-        store_states<NS, PARTS>(a.last, at.b, a, at, h);
+    } else {
+        __syncthreads();
+        finish(buf ^ 1, at.n_four > 0 && (end - 1) / kTile * kTile + at.slot < end, live_before, x_before, z_before);
+        if (a.last && end == a.T) store_states<NS, PARTS>(a.last, at.b, a, at, h);
     }
 }
 

@@ -47,51 +47,18 @@ __device__ __forceinline__ float softplus(float x)
 }
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-// Four channels of one slot, as a thread stages them; `n` of them are there.
-template <typename T>
-struct Four {
-    T t[4];
-    __device__ __forceinline__ void load(const AttTensor& from, int64_t b, int slot, int d, int n)
-    {
-        const T* p = att_at<T>(from, b, slot, 0) + d;
-        if (n == 4) {
-            __builtin_memcpy(&t, p, sizeof(t));
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] = i < n ? p[i] : (T)0.0f;
-        }
-    }
-    __device__ __forceinline__ void zero()
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (T)0.0f;
-    }
-    __device__ __forceinline__ float operator[](int i) const { return (float)t[i]; }
-};
-template <typename T>
-__device__ __forceinline__ void store_four(const AttTensor& to, int64_t b, int slot, int d, int n, const float (&x)[4])
-{
-    T* p = att_at<T>(to, b, slot, 0) + d;
-    if (n == 4) {
-        T t[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = (T)x[i];
-        __builtin_memcpy(p, &t, sizeof(t));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) p[i] = (T)x[i];
-    }
-}
+// Four channels of one slot, as a thread stages them.
+template <typename T> using Four = RowPiece<T, 4>;
 
 // Where a workgroup and its threads are.  States: lane l of a wavefront has channel 16 wave + l % 16 and, of every part of
-// 4 NS states, the NS from NS (l / 16) on.  Staging: thread t has slot t / 16 of a tile and channels 4 (t % 16) on.
+// 4 NS states, the NS from NS (l / 16) on.  Staging: thread t has slot t / 16 of a tile and channels 4 (t % 16) on; where the
+// workgroup's channels are no multiple of four, the last threads' overlap, and both stage and store the same.
 struct ScanPlace {
     int64_t b;
     int group, chunk, d0, d1;        // channels of the workgroup
     int d, q;                        // the lane's
     bool mine;
-    int slot, four, n_four;          // the thread's, staging
+    int slot, four, n_four;          // the thread's, staging: its slot, first channel, and how many (0, or 4 but for groups of fewer)
     __device__ __forceinline__ ScanPlace(const ScanArgs& a, int64_t n)
     {
         const int slice = (int)(n % a.slices);
@@ -107,8 +74,77 @@ struct ScanPlace {
         q = lane_id() / kLanesC;
         mine = d < d1;
         slot = tid / 16;
-        four = d0 + 4 * (tid % 16);
-        n_four = min(max(d1 - four, 0), 4);
+        const int all = d1 - d0;
+        four = d0 + max(min(4 * (tid % 16), all - 4), 0);
+        n_four = 4 * (tid % 16) < all ? min(all, 4) : 0;
+    }
+};
+
+// The thread's four channels of its slot, a tile further on with every load or store; BACK: a tile back.
+template <typename T, bool BACK = false>
+struct Stream {
+    T* p;
+    int64_t tile;
+    int n;
+    __device__ __forceinline__ Stream(const AttTensor& x, const ScanPlace& at, int t0)
+        : p(att_at<T>(x, at.b, t0 + at.slot, 0) + at.four), tile((BACK ? -kTile : kTile) * x.st), n(at.n_four)
+    {
+    }
+    __device__ __forceinline__ void load(Four<T>& x, bool here)
+    {
+        x.zero();
+        if (here && n == 4) x.load(p);
+        if (here && n && n < 4) {
+            T t[4] = {};
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) t[i] = p[i];
+            __builtin_memcpy(&x.w, &t, sizeof(t));
+        }
+        p += tile;
+    }
+    __device__ __forceinline__ void store(const float (&x)[4])
+    {
+        if (n == 4) {
+            T t[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] = (T)x[i];
+            __builtin_memcpy(p, &t, sizeof(t));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) p[i] = (T)x[i];
+        }
+        p += tile;
+    }
+    __device__ __forceinline__ void pass() { p += tile; }
+};
+// The same for B and C: elements threadIdx % 16 and every 16th behind it of the thread's slot.
+template <typename T, int NP, bool BACK = false>
+struct PairStream {
+    static constexpr int kEach = (NP + 15) / 16;
+    const T* p;
+    int64_t tile;
+    int n, N;
+    T v[kEach];
+    __device__ __forceinline__ PairStream(const AttTensor& x, const ScanArgs& a, const ScanPlace& at, int t0)
+        : p(att_at<T>(x, at.b, t0 + at.slot, at.group) + threadIdx.x % 16), tile((BACK ? -kTile : kTile) * x.st), n((int)threadIdx.x % 16), N(a.N)
+    {
+    }
+    __device__ __forceinline__ void load(bool here)
+    {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            v[k] = (T)0.0f;
+            if (here && n + 16 * k < N) v[k] = p[16 * k];
+        }
+        p += tile;
+    }
+    __device__ __forceinline__ void stage(float* row, bool live) const
+    {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (NP % 16 == 0 || n + 16 * k < NP) row[n + 16 * k] = live ? (float)v[k] : 0.0f;
     }
 };
 

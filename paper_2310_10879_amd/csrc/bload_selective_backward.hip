@@ -50,44 +50,16 @@ __device__ __forceinline__ int channel_value(int lane)
 }
 template <int N> constexpr int kIdleLanes = N == 8 ? 1 : (N == 4 ? 3 : 7);      // bits of lanes that hold a copy
 
-// A thread's part of a tile.
-template <typename T, int NP>
-struct Staged {
-    static constexpr int kBC = (NP + 15) / 16;
-    Four<T> x, dt, z, dout;
-    T b[kBC], c[kBC];
-    __device__ __forceinline__ void load(const ScanArgs& a, const ScanPlace& at, int t0, int end, bool maps)
-    {
-        const int t = t0 + at.slot;
-        const bool here = t < end && t >= 0;
-        x.zero(), dt.zero(), z.zero(), dout.zero();
-        if (here && at.n_four) {
-            if (!maps) x.load(a.x, at.b, t, at.four, at.n_four);
-            dt.load(a.dt, at.b, t, at.four, at.n_four);
-            dout.load(a.dout, at.b, t, at.four, at.n_four);
-            if (a.z.p) z.load(a.z, at.b, t, at.four, at.n_four);
-        }
-#pragma unroll
-        for (int k = 0; k < kBC; ++k) {
-            const int n = 16 * k + (int)threadIdx.x % 16;
-            b[k] = c[k] = (T)0.0f;
-            if (here && n < a.N) {
-                if (!maps) b[k] = att_at<T>(a.b, at.b, t, at.group)[n];
-                c[k] = att_at<T>(a.c, at.b, t, at.group)[n];
-            }
-        }
-    }
-};
-
 // A chunk's own part of the gradient in front of it, from its end to its start.
 template <typename T, int NS, int PARTS>
 __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a)
 {
     constexpr int NP = 4 * NS * PARTS;
-    __shared__ float2 steps[kTile][kGroupC];               // step, dy
-    __shared__ __attribute__((aligned(16))) float cs[kTile][NP];
+    __shared__ __attribute__((aligned(16))) float2 steps[2][kTile][kGroupC];           // step, dy
+    __shared__ __attribute__((aligned(16))) float cs[2][kTile][NP];
     const ScanPlace at(a, blockIdx.x);
     const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
+    const int four = at.four - at.d0, last_tile = first + (end - first - 1) / kTile * kTile;
     float u[PARTS][NS], rate[PARTS][NS], bias[4];
     load_states<NS, PARTS>(a.rate, 0, a, at, rate);
 #pragma unroll
@@ -98,35 +70,48 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
     for (int i = 0; i < 4; ++i) bias[i] = a.dt_bias && i < at.n_four ? a.dt_bias[at.four + i] : 0.0f;
     float span = 0.0f;
     bool any_cut = false;
-    Staged<T, NP> in;
-    const int last_tile = first + (end - first - 1) / kTile * kTile;
-    in.load(a, at, last_tile, end, true);
-    for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
-        const TileFlags flags(a, at.b, t0, end, a.in != nullptr);
+    Stream<T, true> pdt(a.dt, at, last_tile), pz(a.z, at, last_tile), pdo(a.dout, at, last_tile);
+    PairStream<T, NP, true> pc(a.c, a, at, last_tile);
+    Four<T> dt, z, dout;
+    auto load = [&](int t0) {
+        const bool here = t0 + at.slot < end;
+        pdt.load(dt, here);
+        pdo.load(dout, here);
+        pz.load(z, here && a.z.p);
+        pc.load(here);
+    };
+    auto stage = [&](int buf, const TileFlags& flags) {
         const bool live = flags.live >> at.slot & 1;
+        float2 s[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float v = in.dt[i] + bias[i];
-            float dy = in.dout[i];
-            if (a.z.p) dy *= in.z[i] * logistic(in.z[i]);
-            steps[at.slot][4 * (threadIdx.x % 16) + i] = make_float2(live ? (a.softplus ? softplus(v) : v) : 0.0f, live ? dy : 0.0f);
+            const float v = dt[i] + bias[i], step = a.softplus ? softplus(v) : v;
+            float dy = dout[i];
+            if (a.z.p) dy *= z[i] * logistic(z[i]);
+            s[i] = live ? make_float2(step, dy) : make_float2(0.0f, 0.0f);
         }
-#pragma unroll
-        for (int k = 0; k < in.kBC; ++k) {
-            const int n = 16 * k + (int)threadIdx.x % 16;
-            if (n < NP) cs[at.slot][n] = live ? (float)in.c[k] : 0.0f;
-        }
+        if (at.n_four) __builtin_memcpy(&steps[buf][at.slot][four], &s, sizeof(s));
+        pc.stage(cs[buf][at.slot], live);
+    };
+    load(last_tile);
+    for (int n = (int)threadIdx.x; n < 2 * kTile * kGroupC; n += kThreads) (&steps[0][0][0])[n] = make_float2(0.0f, 0.0f);
+    __syncthreads();
+    TileFlags flags(a, at.b, last_tile, end, a.in != nullptr);
+    stage(0, flags);
+    int buf = 0;
+    for (int t0 = last_tile; t0 >= first; t0 -= kTile, buf ^= 1) {
         __syncthreads();
-        if (t0 > first) in.load(a, at, t0 - kTile, end, true);
+        const bool more = t0 > first;
+        if (more) load(t0 - kTile);
 #pragma unroll
         for (int t = kTile - 1; t >= 0; --t) {
-            const float2 s = steps[t][col];
+            const float2 s = steps[buf][t][col];
             span += s.x;
             if (flags.live >> t & 1)
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
                     float cc[NS];
-                    __builtin_memcpy(&cc, &cs[t][(p * 4 + at.q) * NS], sizeof(cc));
+                    __builtin_memcpy(&cc, &cs[buf][t][(p * 4 + at.q) * NS], sizeof(cc));
 #pragma unroll
                     for (int i = 0; i < NS; ++i) u[p][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]) * fmaf(cc[i], s.y, u[p][i]);
                 }
@@ -137,7 +122,10 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
                     for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
         }
         any_cut |= flags.cut != 0;
-        __syncthreads();
+        if (more) {
+            flags = TileFlags(a, at.b, t0 - kTile, end, a.in != nullptr);
+            stage(buf ^ 1, flags);
+        }
     }
     const int64_t row = at.b * a.chunks + at.chunk;
     store_states<NS, PARTS>(a.maps, row, a, at, u);
@@ -146,149 +134,232 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
 }
 
 template <typename T, int NS, int PARTS>
-__global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanArgs a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void scan_backward_kernel(ScanArgs a)
 {
-    constexpr int NP = 4 * NS * PARTS, kWaves = kThreads / kWave;
-    __shared__ float2 steps[kTile][kGroupC];               // step, step x
-    __shared__ float dys[kTile][kGroupC], ys[kTile][kGroupC], qs[kTile][kGroupC], ws[kTile][kGroupC];
+    constexpr int NP = 4 * NS * PARTS, kWaves = kThreads / kWave, kRun = 8;
+    __shared__ __attribute__((aligned(16))) float2 steps[kTile][kGroupC];              // step, step x
+    __shared__ __attribute__((aligned(16))) float dys[kTile][kGroupC], ys[kTile][kGroupC], qs[kTile][kGroupC], ws[kTile][kGroupC];
     __shared__ __attribute__((aligned(16))) float bs[kTile][NP], cs[kTile][NP];
     __shared__ float sums[kWaves][kTile][2][NP];           // dB and dC of a wavefront's channels
+    __shared__ __attribute__((aligned(16))) float skips[kGroupC], biases[kGroupC], dskips[kTile][kGroupC], dbiases[kTile][kGroupC];
     ScanPlace at(a, blockIdx.x);
     const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
+    const int four = at.four - at.d0, last_tile = first + (end - first - 1) / kTile * kTile;
     const int64_t part = at.b * a.chunks + at.chunk;
     const bool has_state = a.in != nullptr, gated = a.z.p != nullptr;
+    const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);              // whose sum over channels the lane gets
+    float* my_sums = &sums[wave_id()][0][value / NS][at.q * NS + value % NS];
+    const bool writes = (lane & kIdleLanes<2 * NS>) == 0;
 
-    float rate[PARTS][NS], drate[PARTS][NS];
+    float rate[PARTS][NS], drate[PARTS][NS], lost[PARTS][NS];
     load_states<NS, PARTS>(a.rate, 0, a, at, rate);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) rate[p][i] *= kLog2e, drate[p][i] = 0.0f;
-    float skip[4], bias[4], dskip[4], dbias[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        skip[i] = a.skip && i < at.n_four ? a.skip[at.four + i] : 0.0f;
-        bias[i] = a.dt_bias && i < at.n_four ? a.dt_bias[at.four + i] : 0.0f;
-        dskip[i] = dbias[i] = 0.0f;
+        for (int i = 0; i < NS; ++i) rate[p][i] *= kLog2e, drate[p][i] = lost[p][i] = 0.0f;
+    if ((int)threadIdx.x < kGroupC) {
+        const int d = at.d0 + (int)threadIdx.x;
+        skips[threadIdx.x] = a.skip && d < at.d1 ? a.skip[d] : 0.0f;
+        biases[threadIdx.x] = a.dt_bias && d < at.d1 ? a.dt_bias[d] : 0.0f;
     }
+    for (int n = (int)threadIdx.x; n < kTile * kGroupC; n += kThreads) {               // (columns without a channel stay 0)
+        (&steps[0][0])[n] = make_float2(0.0f, 0.0f);
+        (&dys[0][0])[n] = (&dskips[0][0])[n] = (&dbiases[0][0])[n] = 0.0f;
+    }
+    __syncthreads();
     for (; at.b < a.B; at.b += a.blocks) {
         float u[PARTS][NS];
         if (a.chunks > 1) load_states<NS, PARTS>(a.maps, at.b * a.chunks + at.chunk, a, at, u);
         else load_states<NS, PARTS>(a.dlast, at.b, a, at, u);
-        Staged<T, NP> in;
-        const int last_tile = first + (end - first - 1) / kTile * kTile;
-        in.load(a, at, last_tile, end, false);
+        Stream<T, true> px(a.x, at, last_tile), pdt(a.dt, at, last_tile), pz(a.z, at, last_tile), pdo(a.dout, at, last_tile);
+        Stream<T, true> pdx(a.dx, at, last_tile), pddt(a.ddt, at, last_tile), pdz(a.dz, at, last_tile);
+        PairStream<T, NP, true> pb(a.b, a, at, last_tile), pc(a.c, a, at, last_tile);
+        Four<T> x, dt, z, dout;
+        float h0[PARTS][NS];
+        auto load = [&](int t0) {
+            const bool here = t0 + at.slot < end;
+            px.load(x, here);
+            pdt.load(dt, here);
+            pdo.load(dout, here);
+            pz.load(z, here && gated);
+            pb.load(here);
+            pc.load(here);
+            load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0);
+        };
+        load(last_tile);
         for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
             const TileFlags flags(a, at.b, t0, end, has_state);
             const bool live = flags.live >> at.slot & 1;
-            const Staged<T, NP> now = in;
+            {
+                float2 s[4];
+                float dy[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = now.dt[i] + bias[i], step = live ? (a.softplus ? softplus(v) : v) : 0.0f;
-                float dy = now.dout[i];
-                if (gated) dy *= now.z[i] * logistic(now.z[i]);
-                const int c = 4 * (threadIdx.x % 16) + i;
-                steps[at.slot][c] = make_float2(step, live ? step * now.x[i] : 0.0f);
-                dys[at.slot][c] = live ? dy : 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < now.kBC; ++k) {
-                const int n = 16 * k + (int)threadIdx.x % 16;
-                if (n < NP) {
-                    bs[at.slot][n] = live ? (float)now.b[k] : 0.0f;
-                    cs[at.slot][n] = live ? (float)now.c[k] : 0.0f;
+                for (int i = 0; i < 4; ++i) {
+                    const float v = dt[i] + biases[four + i], step = a.softplus ? softplus(v) : v;
+                    dy[i] = dout[i];
+                    if (gated) dy[i] *= z[i] * logistic(z[i]);
+                    s[i] = live ? make_float2(step, step * x[i]) : make_float2(0.0f, 0.0f);
+                    dy[i] = live ? dy[i] : 0.0f;
                 }
+                if (at.n_four) {
+                    __builtin_memcpy(&steps[at.slot][four], &s, sizeof(s));
+                    __builtin_memcpy(&dys[at.slot][four], &dy, sizeof(dy));
+                }
+                pb.stage(bs[at.slot], live);
+                pc.stage(cs[at.slot], live);
             }
-            float h0[PARTS][NS];
-            load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0);
+            const Four<T> x_now = x, dt_now = dt, z_now = z, dout_now = dout;
+            float h_now[PARTS][NS];
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                for (int i = 0; i < NS; ++i) h_now[p][i] = h0[p][i];
             __syncthreads();
-            if (t0 > first) in.load(a, at, t0 - kTile, end, false);
+            if (t0 > first) load(t0 - kTile);
 
-            float y[kTile], q[kTile], w[kTile];
+            // A lane keeps the states and decays of kRun slots in registers: the tile's runs from the last to the first, their states
+            // from that in front of the tile.
+            auto tile = [&](auto all_go_on) {
+                constexpr bool kAll = decltype(all_go_on)::value;
 #pragma unroll
-            for (int t = 0; t < kTile; ++t) y[t] = q[t] = w[t] = 0.0f;
+                for (int p = 0; p < PARTS; ++p) {
+                    const int n0 = (p * 4 + at.q) * NS;
+                    float start[kTile / kRun][NS], dr[NS];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const int n0 = (p * 4 + at.q) * NS;
-                float h[kTile + 1][NS], decay[kTile][NS];
+                    for (int i = 0; i < NS; ++i) start[0][i] = h_now[p][i], dr[i] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < NS; ++i) h[0][i] = h0[p][i];
+                    for (int r = 1; r < kTile / kRun; ++r) {
 #pragma unroll
-                for (int t = 0; t < kTile; ++t) {
-                    const float2 s = steps[t][col];
-                    float bb[NS];
-                    __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
-                    const bool cut = flags.cut >> t & 1;
+                        for (int i = 0; i < NS; ++i) start[r][i] = start[r - 1][i];
+#pragma unroll
+                        for (int t = (r - 1) * kRun; t < r * kRun; ++t) {
+                            const float2 s = steps[t][col];
+                            float bb[NS];
+                            __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
+                            const bool cut = !kAll && (flags.cut >> t & 1);
+#pragma unroll
+                            for (int i = 0; i < NS; ++i)
+                                start[r][i] = fmaf(__builtin_amdgcn_exp2f(s.x * rate[p][i]), cut ? 0.0f : start[r][i], s.y * bb[i]);
+                        }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int r = kTile / kRun - 1; r >= 0; --r) {
+                        float h[kRun + 1][NS], decay[kRun][NS];
+#pragma unroll
+                        for (int i = 0; i < NS; ++i) h[0][i] = start[r][i];
+#pragma unroll
+                        for (int k0 = 0; k0 < kRun; k0 += 4) {
+                            float y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                            for (int k = k0; k < k0 + 4; ++k) {
+                                const int t = r * kRun + k;
+                                const float2 s = steps[t][col];
+                                float bb[NS];
+                                __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
+                                const bool cut = !kAll && (flags.cut >> t & 1);
+#pragma unroll
+                                for (int i = 0; i < NS; ++i) {
+                                    decay[k][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]);
+                                    h[k + 1][i] = fmaf(decay[k][i], cut ? 0.0f : h[k][i], s.y * bb[i]);
+                                }
+                                if (gated) {
+                                    float cc[NS];
+                                    __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
+#pragma unroll
+                                    for (int i = 0; i < NS; ++i) y[k - k0] = fmaf(cc[i], h[k + 1][i], y[k - k0]);
+                                }
+                            }
+                            if (gated) {
+                                const float sum = sum_states(y[0], y[1], y[2], y[3]);
+                                float& to = ys[r * kRun + k0 + at.q][col];
+                                to = p ? to + sum : sum;
+                            }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int k0 = kRun - 4; k0 >= 0; k0 -= 4) {
+                            float q[4] = {0.0f, 0.0f, 0.0f, 0.0f}, w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                            for (int k = k0 + 3; k >= k0; --k) {
+                                const int t = r * kRun + k;
+                                if (kAll || (flags.live >> t & 1)) {
+                                    const float2 s = steps[t][col];
+                                    const float dy = dys[t][col];
+                                    const bool cut = !kAll && (flags.cut >> t & 1);
+                                    float bb[NS], cc[NS], v[2 * NS];
+                                    __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
+                                    __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
+#pragma unroll
+                                    for (int i = 0; i < NS; ++i) {
+                                        const float grad = fmaf(cc[i], dy, u[p][i]);
+                                        v[i] = s.y * grad;
+                                        v[NS + i] = dy * h[k + 1][i];
+                                        q[k - k0] = fmaf(grad, bb[i], q[k - k0]);
+                                        u[p][i] = cut ? 0.0f : decay[k][i] * grad;
+                                        const float m = u[p][i] * (cut ? 0.0f : h[k][i]);
+                                        w[k - k0] = fmaf(m, rate[p][i], w[k - k0]);
+                                        dr[i] = fmaf(m, s.x, dr[i]);
+                                    }
+                                    const float sum = sum_channels<2 * NS>(v);
+                                    if (writes) my_sums[t * 2 * NP + p * 4 * NS] = sum;
+                                } else if (flags.cut >> t & 1) {
+#pragma unroll
+                                    for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
+                                }
+                            }
+                            const float sq = sum_states(q[0], q[1], q[2], q[3]), sw = sum_states(w[0], w[1], w[2], w[3]);
+                            float &to_q = qs[r * kRun + k0 + at.q][col], &to_w = ws[r * kRun + k0 + at.q][col];
+                            to_q = p ? to_q + sq : sq;
+                            to_w = p ? to_w + sw : sw;
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    // tiles are added with what the additions round off kept beside: there may be thousands
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
-                        decay[t][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]);
-                        h[t + 1][i] = fmaf(decay[t][i], cut ? 0.0f : h[t][i], s.y * bb[i]);
-                    }
-                    if (gated) {
-                        float cc[NS];
-                        __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) y[t] = fmaf(cc[i], h[t + 1][i], y[t]);
+                        const float more = dr[i] - lost[p][i], sum = drate[p][i] + more;
+                        lost[p][i] = (sum - drate[p][i]) - more;
+                        drate[p][i] = sum;
                     }
                 }
-#pragma unroll
-                for (int t = kTile - 1; t >= 0; --t) {
-                    if (flags.live >> t & 1) {
-                        const float2 s = steps[t][col];
-                        const float dy = dys[t][col];
-                        const bool cut = flags.cut >> t & 1;
-                        float bb[NS], cc[NS], v[2 * NS];
-                        __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
-                        __builtin_memcpy(&cc, &cs[t][n0], sizeof(cc));
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) {
-                            const float g = fmaf(cc[i], dy, u[p][i]);
-                            v[i] = s.y * g;
-                            v[NS + i] = dy * h[t + 1][i];
-                            q[t] = fmaf(g, bb[i], q[t]);
-                            u[p][i] = cut ? 0.0f : decay[t][i] * g;
-                            const float k = u[p][i] * (cut ? 0.0f : h[t][i]);
-                            w[t] = fmaf(k, rate[p][i], w[t]);
-                            drate[p][i] = fmaf(k, s.x, drate[p][i]);
-                        }
-                        const float sum = sum_channels<2 * NS>(v);
-                        const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);
-                        if ((lane & kIdleLanes<2 * NS>) == 0) sums[wave_id()][t][value / NS][n0 + value % NS] = sum;
-                    } else if (flags.cut >> t & 1) {
-#pragma unroll
-                        for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
-                    }
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < kTile; t += 4) {
-                qs[t + at.q][col] = sum_states(q[t], q[t + 1], q[t + 2], q[t + 3]);
-                ws[t + at.q][col] = sum_states(w[t], w[t + 1], w[t + 2], w[t + 3]);
-                if (gated) ys[t + at.q][col] = sum_states(y[t], y[t + 1], y[t + 2], y[t + 3]);
-            }
+            };
+            if (flags.live == 0xffffu && flags.cut == 0) tile(std::true_type());
+            else tile(std::false_type());
             __syncthreads();
             if (t0 + at.slot < end && at.n_four) {
                 float dx[4], ddt[4], dz[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int c = 4 * (threadIdx.x % 16) + i;
-                    const float x = now.x[i], dy = dys[at.slot][c], qq = qs[at.slot][c];
-                    dx[i] = fmaf(steps[at.slot][c].x, qq, skip[i] * dy);
+                    const int c = four + i;
+                    const float x = x_now[i], dy = dys[at.slot][c], qq = qs[at.slot][c], skip = skips[c];
+                    dx[i] = fmaf(steps[at.slot][c].x, qq, skip * dy);
                     ddt[i] = fmaf(x, qq, ws[at.slot][c] * kLn2);
-                    if (a.softplus) ddt[i] *= logistic(now.dt[i] + bias[i]);
+                    if (a.softplus) ddt[i] *= logistic(dt_now[i] + biases[c]);
+                    dz[i] = 0.0f;
                     if (gated) {
-                        const float z = now.z[i], sg = logistic(z);
-                        dz[i] = now.dout[i] * fmaf(skip[i], x, ys[at.slot][c]) * sg * fmaf(z, 1.0f - sg, 1.0f);
+                        const float z = z_now[i], sg = logistic(z);
+                        dz[i] = dout_now[i] * fmaf(skip, x, ys[at.slot][c]) * sg * fmaf(z, 1.0f - sg, 1.0f);
                     }
                     if (!live) dx[i] = ddt[i] = dz[i] = 0.0f;
-                    else dskip[i] = fmaf(dy, x, dskip[i]), dbias[i] += ddt[i];
                 }
-                store_four<T>(a.dx, at.b, t0 + at.slot, at.four, at.n_four, dx);
-                store_four<T>(a.ddt, at.b, t0 + at.slot, at.four, at.n_four, ddt);
-                if (gated) store_four<T>(a.dz, at.b, t0 + at.slot, at.four, at.n_four, dz);
+                // (the slot's sums over all tiles, its thread's own; twice by threads whose channels overlap would be once too often)
+                if (live)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (four + i >= 4 * ((int)threadIdx.x % 16)) {
+                            dskips[at.slot][four + i] = fmaf(dys[at.slot][four + i], x_now[i], dskips[at.slot][four + i]);
+                            dbiases[at.slot][four + i] += ddt[i];
+                        }
+                pdx.store(dx);
+                pddt.store(ddt);
+                if (gated) pdz.store(dz);
+            } else {
+                pdx.pass(), pddt.pass(), pdz.pass();
             }
             // this slice's share of dB and dC
             const int64_t slice = (at.d0 - at.group * a.per) / kGroupC;
+            float* share = a.shares + (((slice * a.B + at.b) * a.T + t0) * a.G + at.group) * 2 * a.N;
             for (int n = (int)threadIdx.x; n < kTile * 2 * NP; n += kThreads) {
                 const int t = n / (2 * NP), which = n / NP % 2, k = n % NP;
                 if (k >= a.N || t0 + t >= end) continue;
@@ -296,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanArgs a)
                 if (flags.live >> t & 1)
 #pragma unroll
                     for (int wave = 0; wave < kWaves; ++wave) s += sums[wave][t][which][k];
-                a.shares[((((slice * a.B + at.b) * a.T + t0 + t) * a.G + at.group) * 2 + which) * a.N + k] = s;
+                share[(int64_t)t * a.G * 2 * a.N + which * a.N + k] = s;
             }
             __syncthreads();
         }
@@ -306,16 +377,10 @@ __global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanArgs a)
     store_states<NS, PARTS>(to, 0, a, at, drate);
     // dskip and dbias of the 16 slots of a tile, one after another
     to += (int64_t)a.D * a.N;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        qs[at.slot][4 * (threadIdx.x % 16) + i] = dskip[i];
-        ws[at.slot][4 * (threadIdx.x % 16) + i] = dbias[i];
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < kGroupC && at.d0 + (int)threadIdx.x < at.d1) {
+    if ((int)threadIdx.x < at.d1 - at.d0) {
         float s = 0.0f, b = 0.0f;
 #pragma unroll
-        for (int t = 0; t < kTile; ++t) s += qs[t][threadIdx.x], b += ws[t][threadIdx.x];
+        for (int t = 0; t < kTile; ++t) s += dskips[t][threadIdx.x], b += dbiases[t][threadIdx.x];
         to[at.d0 + threadIdx.x] = s;
         to[a.D + at.d0 + threadIdx.x] = b;
     }
