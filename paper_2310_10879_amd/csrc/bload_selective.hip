@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
             const float v = dt[i] + bias[i], step = a.softplus ? softplus(v) : v;
             s[i] = live ? make_float2(step, step * x[i]) : make_float2(0.0f, 0.0f);
         }
-        if (at.n_four) __builtin_memcpy(&steps[buf][at.slot][four], &s, sizeof(s));
+        put_steps(&steps[buf][at.slot][four], s);
         pb.stage(bs[buf][at.slot], live);
         if (!MAPS) pc.stage(cs[buf][MAPS ? 0 : at.slot], live);
     };
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
     auto finish = [&](int buf, bool here, bool live, const Four<T>& x, const Four<T>& z) {
         if (!here) return;
         float y[4];
-        __builtin_memcpy(&y, &ys[buf][MAPS ? 0 : at.slot][four], sizeof(y));
+        get_four(y, &ys[buf][MAPS ? 0 : at.slot][four]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             y[i] = fmaf(skip[i], x[i], y[i]);
@@ -93,8 +93,6 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
     };
 
     load(first);
-    for (int n = (int)threadIdx.x; n < 2 * kTile * kGroupC; n += kThreads) (&steps[0][0][0])[n] = make_float2(0.0f, 0.0f);
-    __syncthreads();                                       // (columns without a channel stay 0)
     TileFlags flags(a, at.b, first, end, has_state);
     stage(0, flags);
     Four<T> x_now = x, z_now = z, x_before = x, z_before = z;

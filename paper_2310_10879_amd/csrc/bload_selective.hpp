@@ -51,14 +51,14 @@ __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcp
 template <typename T> using Four = RowPiece<T, 4>;
 
 // Where a workgroup and its threads are.  States: lane l of a wavefront has channel 16 wave + l % 16 and, of every part of
-// 4 NS states, the NS from NS (l / 16) on.  Staging: thread t has slot t / 16 of a tile and channels 4 (t % 16) on; where the
-// workgroup's channels are no multiple of four, the last threads' overlap, and both stage and store the same.
+// 4 NS states, the NS from NS (l / 16) on.  Staging: thread t has slot t / 16 of a tile and channels 4 (t % 16) on, zeros where
+// there are none.
 struct ScanPlace {
     int64_t b;
     int group, chunk, d0, d1;        // channels of the workgroup
     int d, q;                        // the lane's
     bool mine;
-    int slot, four, n_four;          // the thread's, staging: its slot, first channel, and how many (0, or 4 but for groups of fewer)
+    int slot, four, n_four;          // the thread's, staging: its slot, first channel, and how many there are
     __device__ __forceinline__ ScanPlace(const ScanArgs& a, int64_t n)
     {
         const int slice = (int)(n % a.slices);
@@ -74,9 +74,8 @@ struct ScanPlace {
         q = lane_id() / kLanesC;
         mine = d < d1;
         slot = tid / 16;
-        const int all = d1 - d0;
-        four = d0 + max(min(4 * (tid % 16), all - 4), 0);
-        n_four = 4 * (tid % 16) < all ? min(all, 4) : 0;
+        four = d0 + 4 * (tid % 16);
+        n_four = min(max(d1 - four, 0), 4);
     }
 };
 
@@ -182,6 +181,12 @@ __device__ __forceinline__ void store_states(float* base, int64_t row, const Sca
     }
 }
 
+// Four columns of a row in LDS, 16 bytes aligned.
+__device__ __forceinline__ void get_four(float (&x)[4], const float* p) { __builtin_memcpy(&x, __builtin_assume_aligned(p, 16), 16); }
+__device__ __forceinline__ void put_four(float* p, const float (&x)[4]) { __builtin_memcpy(__builtin_assume_aligned(p, 16), &x, 16); }
+__device__ __forceinline__ void get_steps(float2 (&s)[4], const float2* p) { __builtin_memcpy(&s, __builtin_assume_aligned(p, 16), 32); }
+__device__ __forceinline__ void put_steps(float2* p, const float2 (&s)[4]) { __builtin_memcpy(__builtin_assume_aligned(p, 16), &s, 32); }
+
 // Of four values for four slots in every lane, the sum over the four lanes of a channel (l % 16): lane q = l / 16
 // gets that of slot q.  Each exchange leaves half of the values, whole where the other half went.
 __device__ __forceinline__ float sum_states(float y0, float y1, float y2, float y3)
@@ -235,7 +240,7 @@ inline bload_status scan_sizes(ScanArgs& a, int64_t B, int32_t T, int32_t D, int
     a.tiles = (int32_t)ceil_div(T, kTile);
     const int64_t alone = B * G * a.slices;
     a.chunks = 1;
-    if (alone > 0 && alone < 384) a.chunks = (int32_t)std::min<int64_t>({ceil_div(1024, alone), a.tiles, 64});
+    if (alone > 0 && alone < 384) a.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, alone), a.tiles / 4, 64}));
     const int64_t each = ceil_div(a.tiles, a.chunks);
     a.chunk = (int32_t)each * kTile;
     a.chunks = (int32_t)ceil_div(a.tiles, each);

@@ -31,7 +31,8 @@ __device__ __forceinline__ void halve(float (&v)[N], int n, bool upper)
 }
 constexpr int kMirror = 0x140, kHalfMirror = 0x141, kQuadSwap2 = 0x4e, kQuadSwap1 = 0xb1;
 
-// Of N (2, 4 or 8) values in every lane the sums over the 16 lanes of a row: the lane gets that of value `channel_value`.
+// Of N (2, 4 or 8) values of one slot in every lane the sums over the 16 lanes of a row, but for the last step, from lane to
+// neighbour: the lane has that of value `channel_value`.  The last step is for two slots together: even lanes get the first one's.
 template <int N>
 __device__ __forceinline__ float sum_channels(float (&v)[N])
 {
@@ -41,14 +42,19 @@ __device__ __forceinline__ float sum_channels(float (&v)[N])
     else v[0] += dpp_move<kHalfMirror>(v[0], 0.0f);
     if constexpr (N >= 8) halve<kQuadSwap2, N>(v, N / 4, lane & 2);
     else v[0] += dpp_move<kQuadSwap2>(v[0], 0.0f);
-    return v[0] + dpp_move<kQuadSwap1>(v[0], 0.0f);
+    return v[0];
+}
+__device__ __forceinline__ float sum_pairs(float even, float odd)
+{
+    const bool upper = lane_id() & 1;
+    const float keep = upper ? odd : even, send = upper ? even : odd;
+    return keep + dpp_move<kQuadSwap1>(send, 0.0f);
 }
 template <int N>
 __device__ __forceinline__ int channel_value(int lane)
 {
     return N == 8 ? lane >> 1 & 7 : (N == 4 ? lane >> 2 & 3 : lane >> 3 & 1);
 }
-template <int N> constexpr int kIdleLanes = N == 8 ? 1 : (N == 4 ? 3 : 7);      // bits of lanes that hold a copy
 
 // A chunk's own part of the gradient in front of it, from its end to its start.
 template <typename T, int NS, int PARTS>
@@ -90,12 +96,10 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
             if (a.z.p) dy *= z[i] * logistic(z[i]);
             s[i] = live ? make_float2(step, dy) : make_float2(0.0f, 0.0f);
         }
-        if (at.n_four) __builtin_memcpy(&steps[buf][at.slot][four], &s, sizeof(s));
+        put_steps(&steps[buf][at.slot][four], s);
         pc.stage(cs[buf][at.slot], live);
     };
     load(last_tile);
-    for (int n = (int)threadIdx.x; n < 2 * kTile * kGroupC; n += kThreads) (&steps[0][0][0])[n] = make_float2(0.0f, 0.0f);
-    __syncthreads();
     TileFlags flags(a, at.b, last_tile, end, a.in != nullptr);
     stage(0, flags);
     int buf = 0;
@@ -134,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
 }
 
 template <typename T, int NS, int PARTS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void scan_backward_kernel(ScanArgs a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS == 1 ? 2 : 1, 2))) void scan_backward_kernel(ScanArgs a)
 {
     constexpr int NP = 4 * NS * PARTS, kWaves = kThreads / kWave, kRun = 8;
     __shared__ __attribute__((aligned(16))) float2 steps[kTile][kGroupC];              // step, step x
@@ -147,9 +151,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     const int four = at.four - at.d0, last_tile = first + (end - first - 1) / kTile * kTile;
     const int64_t part = at.b * a.chunks + at.chunk;
     const bool has_state = a.in != nullptr, gated = a.z.p != nullptr;
-    const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);              // whose sum over channels the lane gets
-    float* my_sums = &sums[wave_id()][0][value / NS][at.q * NS + value % NS];
-    const bool writes = (lane & kIdleLanes<2 * NS>) == 0;
+    const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);              // whose sums over channels the lane gets
+    float* my_sums = &sums[wave_id()][lane & 1][value / NS][at.q * NS + value % NS];    // of even slots or odd ones
 
     float rate[PARTS][NS], drate[PARTS][NS], lost[PARTS][NS];
     load_states<NS, PARTS>(a.rate, 0, a, at, rate);
@@ -162,9 +165,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         skips[threadIdx.x] = a.skip && d < at.d1 ? a.skip[d] : 0.0f;
         biases[threadIdx.x] = a.dt_bias && d < at.d1 ? a.dt_bias[d] : 0.0f;
     }
-    for (int n = (int)threadIdx.x; n < kTile * kGroupC; n += kThreads) {               // (columns without a channel stay 0)
-        (&steps[0][0])[n] = make_float2(0.0f, 0.0f);
-        (&dys[0][0])[n] = (&dskips[0][0])[n] = (&dbiases[0][0])[n] = 0.0f;
+    {
+        const float none[4] = {};
+        put_four(&dskips[at.slot][four], none);
+        put_four(&dbiases[at.slot][four], none);
     }
     __syncthreads();
     for (; at.b < a.B; at.b += a.blocks) {
@@ -192,19 +196,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             const bool live = flags.live >> at.slot & 1;
             {
                 float2 s[4];
-                float dy[4];
+                float dy[4], bias[4];
+                get_four(bias, &biases[four]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float v = dt[i] + biases[four + i], step = a.softplus ? softplus(v) : v;
+                    const float v = dt[i] + bias[i], step = a.softplus ? softplus(v) : v;
                     dy[i] = dout[i];
                     if (gated) dy[i] *= z[i] * logistic(z[i]);
                     s[i] = live ? make_float2(step, step * x[i]) : make_float2(0.0f, 0.0f);
                     dy[i] = live ? dy[i] : 0.0f;
                 }
-                if (at.n_four) {
-                    __builtin_memcpy(&steps[at.slot][four], &s, sizeof(s));
-                    __builtin_memcpy(&dys[at.slot][four], &dy, sizeof(dy));
-                }
+                put_steps(&steps[at.slot][four], s);
+                put_four(&dys[at.slot][four], dy);
                 pb.stage(bs[at.slot], live);
                 pc.stage(cs[at.slot], live);
             }
@@ -275,13 +278,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                                 float& to = ys[r * kRun + k0 + at.q][col];
                                 to = p ? to + sum : sum;
                             }
+                            __builtin_amdgcn_sched_barrier(0);
                         }
-                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                         for (int k0 = kRun - 4; k0 >= 0; k0 -= 4) {
-                            float q[4] = {0.0f, 0.0f, 0.0f, 0.0f}, w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                            float q[4] = {0.0f, 0.0f, 0.0f, 0.0f}, w[4] = {0.0f, 0.0f, 0.0f, 0.0f}, odd = 0.0f;
 #pragma unroll
                             for (int k = k0 + 3; k >= k0; --k) {
+                                float sum = 0.0f;
                                 const int t = r * kRun + k;
                                 if (kAll || (flags.live >> t & 1)) {
                                     const float2 s = steps[t][col];
@@ -301,19 +305,20 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                                         w[k - k0] = fmaf(m, rate[p][i], w[k - k0]);
                                         dr[i] = fmaf(m, s.x, dr[i]);
                                     }
-                                    const float sum = sum_channels<2 * NS>(v);
-                                    if (writes) my_sums[t * 2 * NP + p * 4 * NS] = sum;
+                                    sum = sum_channels<2 * NS>(v);
                                 } else if (flags.cut >> t & 1) {
 #pragma unroll
                                     for (int i = 0; i < NS; ++i) u[p][i] = 0.0f;
                                 }
+                                if (k % 2) odd = sum;
+                                else my_sums[t * 2 * NP + p * 4 * NS] = sum_pairs(sum, odd);
                             }
                             const float sq = sum_states(q[0], q[1], q[2], q[3]), sw = sum_states(w[0], w[1], w[2], w[3]);
                             float &to_q = qs[r * kRun + k0 + at.q][col], &to_w = ws[r * kRun + k0 + at.q][col];
                             to_q = p ? to_q + sq : sq;
                             to_w = p ? to_w + sw : sw;
+                            __builtin_amdgcn_sched_barrier(0);
                         }
-                        __builtin_amdgcn_sched_barrier(0);
                     }
                     // tiles are added with what the additions round off kept beside: there may be thousands
 #pragma unroll
@@ -328,29 +333,36 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             else tile(std::false_type());
             __syncthreads();
             if (t0 + at.slot < end && at.n_four) {
-                float dx[4], ddt[4], dz[4];
+                float dx[4], ddt[4], dz[4], dy[4], q[4], w[4], y[4], skip[4], bias[4];
+                float2 s[4];
+                get_four(dy, &dys[at.slot][four]);
+                get_four(q, &qs[at.slot][four]);
+                get_four(w, &ws[at.slot][four]);
+                if (gated) get_four(y, &ys[at.slot][four]);
+                get_four(skip, &skips[four]);
+                get_four(bias, &biases[four]);
+                get_steps(s, &steps[at.slot][four]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int c = four + i;
-                    const float x = x_now[i], dy = dys[at.slot][c], qq = qs[at.slot][c], skip = skips[c];
-                    dx[i] = fmaf(steps[at.slot][c].x, qq, skip * dy);
-                    ddt[i] = fmaf(x, qq, ws[at.slot][c] * kLn2);
-                    if (a.softplus) ddt[i] *= logistic(dt_now[i] + biases[c]);
+                    const float x = x_now[i];
+                    dx[i] = fmaf(s[i].x, q[i], skip[i] * dy[i]);
+                    ddt[i] = fmaf(x, q[i], w[i] * kLn2);
+                    if (a.softplus) ddt[i] *= logistic(dt_now[i] + bias[i]);
                     dz[i] = 0.0f;
                     if (gated) {
                         const float z = z_now[i], sg = logistic(z);
-                        dz[i] = dout_now[i] * fmaf(skip, x, ys[at.slot][c]) * sg * fmaf(z, 1.0f - sg, 1.0f);
+                        dz[i] = dout_now[i] * fmaf(skip[i], x, y[i]) * sg * fmaf(z, 1.0f - sg, 1.0f);
                     }
                     if (!live) dx[i] = ddt[i] = dz[i] = 0.0f;
                 }
-                // (the slot's sums over all tiles, its thread's own; twice by threads whose channels overlap would be once too often)
-                if (live)
+                if (live) {                                // (the slot's sums over all tiles are its threads' own)
+                    get_four(skip, &dskips[at.slot][four]);
+                    get_four(bias, &dbiases[at.slot][four]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (four + i >= 4 * ((int)threadIdx.x % 16)) {
-                            dskips[at.slot][four + i] = fmaf(dys[at.slot][four + i], x_now[i], dskips[at.slot][four + i]);
-                            dbiases[at.slot][four + i] += ddt[i];
-                        }
+                    for (int i = 0; i < 4; ++i) skip[i] = fmaf(dy[i], x_now[i], skip[i]), bias[i] += ddt[i];
+                    put_four(&dskips[at.slot][four], skip);
+                    put_four(&dbiases[at.slot][four], bias);
+                }
                 pdx.store(dx);
                 pddt.store(ddt);
                 if (gated) pdz.store(dz);
