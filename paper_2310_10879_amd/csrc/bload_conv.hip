@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
             if (a.silu) p[v] *= sigmoid(p[v]);
             if (age == 0) p[v] = 0.0f;
         }
-        store_row<T, V>(att_at<T>(a.out, b, t0 + i, 0) + lane.d, p, lane.skip);
+        store_row_once<T, V>(att_at<T>(a.out, b, t0 + i, 0) + lane.d, p, lane.skip);
         if (last && t0 + i == a.T - 1)
 #pragma unroll
             for (int j = 0; j < K - 1; ++j)
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
                         for (int v = 0; v < V; ++v) acc[K - 1][v] += (float)p[v];
                     }
                     T* to = u >= 0 ? att_at<T>(a.out, b, u, 0) : reinterpret_cast<T*>(a.last) + (b * (K - 1) + K - 1 + u) * a.D;
-                    store_row<T, V>(to + lane.d, acc[K - 1], lane.skip);
+                    store_row_once<T, V>(to + lane.d, acc[K - 1], lane.skip);
                 }
 #pragma unroll
                 for (int j = K - 1; j > 0; --j)

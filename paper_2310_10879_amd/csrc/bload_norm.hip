@@ -7,7 +7,7 @@
 //
 // HBM bound: a row is read once into registers and everything else is done there, the variance from the differences to
 // the mean, not from the squares.  A team of L lanes takes a row, P pieces of 16 bytes to a lane: 4 to 64 lanes of a wavefront, or a
-// workgroup.  The gradients of weights are a sum over all rows: every team keeps that of the rows it takes in registers,
+// workgroup of 256 or 512.  The gradients of weights are a sum over all rows: every team keeps that of the rows it takes in registers,
 // workgroups leave theirs in the workspace, and a second kernel adds those in a fixed order, so the
 // same inputs give the same bits.  Rows too long for registers are read again from the cache.
 #include <algorithm>
@@ -42,32 +42,46 @@ struct RowAt {
     __device__ __forceinline__ bool live(const NormArgs& a) const { return !a.valid || a.valid[b * a.T.d + t]; }
 };
 
-// Sums over a team; a workgroup's goes through LDS, in one of two buffers in turn.
-template <int L>
+// Threads of a workgroup whose teams have L lanes.
+template <int L> constexpr int kNormThreads = L > kThreads ? L : kThreads;
+
+// Sums over a team of R rows' values; a workgroup's go through LDS, in one of two buffers in turn.
+template <int L, int R>
 struct Team {
-    float (*room)[2][kThreads / kWave];
+    float (*room)[R][2][kNormThreads<L> / kWave];
     int turn = 0;
-    __device__ __forceinline__ void sum(float& a, float& b)
+    __device__ __forceinline__ void sum(float (&a)[R], float (&b)[R])
     {
-        lanes_sum<(L < kWave ? L : kWave)>(a, b);
-        if constexpr (L > kWave) {
-            if (lane_id() == 0) {
-                room[turn][0][wave_id()] = a;
-                room[turn][1][wave_id()] = b;
-            }
-            __syncthreads();
-            a = b = 0.0f;
 #pragma unroll
-            for (int w = 0; w < L / kWave; ++w) a += room[turn][0][w], b += room[turn][1][w];
+        for (int r = 0; r < R; ++r) lanes_sum<(L < kWave ? L : kWave)>(a[r], b[r]);
+        if constexpr (L > kWave) {
+            if (lane_id() == 0)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    room[turn][r][0][wave_id()] = a[r];
+                    room[turn][r][1][wave_id()] = b[r];
+                }
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                a[r] = b[r] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < L / kWave; ++w) a[r] += room[turn][r][0][w], b[r] += room[turn][r][1][w];
+            }
             turn ^= 1;
         }
     }
-    __device__ __forceinline__ float sum(float a)
+    __device__ __forceinline__ void sum(float (&a)[R])
     {
-        float none = 0.0f;
-        if constexpr (L <= kWave) return lanes_sum<L>(a);
-        sum(a, none);
-        return a;
+        if constexpr (L <= kWave) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) a[r] = lanes_sum<L>(a[r]);
+        } else {
+            float none[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) none[r] = 0.0f;
+            sum(a, none);
+        }
     }
 };
 
@@ -94,16 +108,17 @@ __device__ __forceinline__ void blank(float (&x)[V], int skip)
         for (int v = 0; v < V; ++v) x[v] = v < skip ? 0.0f : x[v];
 }
 
-// Teams of lanes of a wavefront take their rows alike; a lane without a row of its own takes part in the sums.
-template <typename T, int V, int P, int L>
-__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
+// A team takes R rows at a time, whose loads are on their way together.  Teams of lanes of a wavefront take theirs alike; a
+// lane without a row of its own takes part in the sums.
+template <typename T, int V, int P, int L, int R>
+__global__ __launch_bounds__(kNormThreads<L>) void norm_kernel(NormArgs a)
 {
-    __shared__ float room[2][2][kThreads / kWave];
-    constexpr int kTeams = kThreads / L;
+    __shared__ float room[2][R][2][kNormThreads<L> / kWave];
+    constexpr int kTeams = kNormThreads<L> / L;
     constexpr bool kHold = P * V <= 16;      // weights stay in registers from row to row
     const int lane = (int)threadIdx.x % L;
     const Places<V, P, L> places(a.D, lane);
-    Team<L> team{room};
+    Team<L, R> team{room};
     float w[kHold ? P : 1][V], bias[kHold ? P : 1][V];
     auto weights = [&](int p, float (&w)[V], float (&b)[V]) {
 #pragma unroll
@@ -115,79 +130,121 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a)
 #pragma unroll
         for (int p = 0; p < P; ++p) weights(p, w[p], bias[p]);
 
-    const uint32_t step = gridDim.x * kTeams;
-    for (uint32_t row0 = blockIdx.x * kTeams; row0 < a.rows; row0 += step) {
-        const uint32_t row = row0 + (int)threadIdx.x / L;
-        const bool here = row < a.rows;
-        const RowAt at(a, here ? row : 0);
-        const bool live = here && at.live(a);
-        float x[P][V];
-        {
-            RowPiece<T, V> piece[P], more[P];
+    const uint32_t step = gridDim.x * kTeams * R;
+    for (uint32_t row0 = blockIdx.x * kTeams * R; row0 < a.rows; row0 += step) {
+        RowPiece<T, V> piece[R][P], more[R][P];
+        bool here[R], live[R];
+        float x[R][P][V];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t row = row0 + r * kTeams + (int)threadIdx.x / L;
+            here[r] = row < a.rows;
+            const RowAt at(a, here[r] ? row : 0);
+            live[r] = here[r] && at.live(a);
             const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const bool mine = live && places.skip[p] < V;
-                piece[p].zero();
-                more[p].zero();
-                if (mine) piece[p].load(px + places.at[p]);
-                if (mine && a.res.p) more[p].load(pr + places.at[p]);
+                const bool mine = live[r] && places.skip[p] < V;
+                piece[r][p].zero();
+                more[r][p].zero();
+                if (mine) piece[r][p].load_once(px + places.at[p]);
+                if (mine && a.res.p) more[r][p].load_once(pr + places.at[p]);
             }
+        }
+        float mean[R], square[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = square[r] = 0.0f;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) x[p][v] = piece[p][v];
+                for (int v = 0; v < V; ++v) x[r][p][v] = piece[r][p][v];
                 if (a.res.p)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) x[p][v] = (float)(T)(x[p][v] + more[p][v]);
-                if (here && a.sum.p && places.skip[p] < V) store_row<T, V>(att_at<T>(a.sum, at.b, at.t, at.h) + places.at[p], x[p], places.skip[p]);
-                blank<V>(x[p], places.skip[p]);
+                    for (int v = 0; v < V; ++v) x[r][p][v] = (float)(T)(x[r][p][v] + more[r][p][v]);
+                if (a.sum.p && here[r] && places.skip[p] < V) {
+                    const RowAt at(a, row0 + r * kTeams + (int)threadIdx.x / L);
+                    store_row_once<T, V>(att_at<T>(a.sum, at.b, at.t, at.h) + places.at[p], x[r][p], places.skip[p]);
+                }
+                blank<V>(x[r][p], places.skip[p]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) mean[r] += x[r][p][v];
             }
         }
-        float mean = 0.0f;
-        if (a.center) {
+        if (a.center) team.sum(mean);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
+        for (int r = 0; r < R; ++r) {
+            mean[r] = a.center ? mean[r] * a.inv : 0.0f;
 #pragma unroll
-                for (int v = 0; v < V; ++v) mean += x[p][v];
-            mean = team.sum(mean) * a.inv;
-        }
-        float square = 0.0f;
+            for (int p = 0; p < P; ++p) {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
+                for (int v = 0; v < V; ++v) x[r][p][v] -= mean[r];
+                blank<V>(x[r][p], places.skip[p]);
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[p][v] -= mean;
-            blank<V>(x[p], places.skip[p]);
-#pragma unroll
-            for (int v = 0; v < V; ++v) square = fmaf(x[p][v], x[p][v], square);
-        }
-        const float r = rsqrtf(fmaf(team.sum(square), a.inv, a.eps));
-        if (!here) continue;
-        if (lane == 0 && a.stats) a.stats[row] = live ? make_float2(mean, r) : make_float2(0.0f, 0.0f);
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (places.skip[p] >= V) continue;
-            float ww[V], bb[V], y[V];
-            if constexpr (!kHold) weights(p, ww, bb);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (kHold) ww[v] = w[p][v], bb[v] = bias[p][v];
-                y[v] = live ? fmaf(x[p][v] * r, ww[v], bb[v]) : 0.0f;
+                for (int v = 0; v < V; ++v) square[r] = fmaf(x[r][p][v], x[r][p][v], square[r]);
             }
-            store_row<T, V>(att_at<T>(a.out, at.b, at.t, at.h) + places.at[p], y, places.skip[p]);
+        }
+        team.sum(square);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (!here[r]) continue;
+            const uint32_t row = row0 + r * kTeams + (int)threadIdx.x / L;
+            const RowAt at(a, row);
+            const float inv = rsqrtf(fmaf(square[r], a.inv, a.eps));
+            if (lane == 0 && a.stats) a.stats[row] = live[r] ? make_float2(mean[r], inv) : make_float2(0.0f, 0.0f);
+            T* po = att_at<T>(a.out, at.b, at.t, at.h);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if (places.skip[p] >= V) continue;
+                float ww[V], bb[V], y[V];
+                if constexpr (!kHold) weights(p, ww, bb);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if constexpr (kHold) ww[v] = w[p][v], bb[v] = bias[p][v];
+                    y[v] = live[r] ? fmaf(x[r][p][v] * inv, ww[v], bb[v]) : 0.0f;
+                }
+                store_row_once<T, V>(po + places.at[p], y, places.skip[p]);
+            }
         }
     }
 }
 
+// One row's pieces on their way while the row in front of it is computed.
+template <typename T, int V, int P>
+struct BackRow {
+    RowPiece<T, V> x[P], dy[P], more[P];
+    float2 stat;
+    bool here, live;
+    template <int L>
+    __device__ __forceinline__ void load(const NormArgs& a, const Places<V, P, L>& places, uint32_t row)
+    {
+        here = row < a.rows;
+        const RowAt at(a, here ? row : 0);
+        live = here && at.live(a);
+        const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pd = att_at<T>(a.dout, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            const bool mine = live && places.skip[p] < V;
+            x[p].zero();
+            dy[p].zero();
+            more[p].zero();
+            if (mine) x[p].load_once(px + places.at[p]);
+            if (mine) dy[p].load_once(pd + places.at[p]);
+            if (mine && a.res.p) more[p].load_once(pr + places.at[p]);
+        }
+        stat = live ? a.stats[row] : make_float2(0.0f, 0.0f);
+    }
+};
+
 template <typename T, int V, int P, int L>
-__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a)
+__global__ __launch_bounds__(kNormThreads<L>) void norm_backward_kernel(NormArgs a)
 {
-    __shared__ float room[2][2][kThreads / kWave];
-    constexpr int kTeams = kThreads / L;
+    __shared__ float room[2][1][2][kNormThreads<L> / kWave];
+    constexpr int kTeams = kNormThreads<L> / L;
     constexpr bool kHold = P * V <= 16;
     const int lane = (int)threadIdx.x % L;
     const Places<V, P, L> places(a.D, lane);
-    Team<L> team{room};
+    Team<L, 1> team{room};
     float w[kHold ? P : 1][V], dw[P][V], db[P][V];
     auto weights = [&](int p, float (&w)[V]) {
 #pragma unroll
@@ -200,62 +257,59 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < V; ++v) dw[p][v] = db[p][v] = 0.0f;
     }
-    const uint32_t step = gridDim.x * kTeams;
+    const uint32_t step = gridDim.x * kTeams, mine = (int)threadIdx.x / L;
+    BackRow<T, V, P> next;
+    next.load(a, places, blockIdx.x * kTeams + mine);
     for (uint32_t row0 = blockIdx.x * kTeams; row0 < a.rows; row0 += step) {
-        const uint32_t row = row0 + (int)threadIdx.x / L;
-        const bool here = row < a.rows;
-        const RowAt at(a, here ? row : 0);
-        const bool live = here && at.live(a);
-        const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pd = att_at<T>(a.dout, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
-        RowPiece<T, V> x[P], dy[P], more[P];
+        BackRow<T, V, P> now = next;
+        next.load(a, places, row0 + step + mine);
+        const float mean = a.center ? now.stat.x : 0.0f, inv = now.stat.y;
+        float sum_g[1] = {0.0f}, sum_gu[1] = {0.0f};
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const bool mine = live && places.skip[p] < V;
-            x[p].zero();
-            dy[p].zero();
-            more[p].zero();
-            if (mine) x[p].load(px + places.at[p]);
-            if (mine) dy[p].load(pd + places.at[p]);
-            if (mine && a.res.p) more[p].load(pr + places.at[p]);
-        }
-        const float2 stat = live ? a.stats[row] : make_float2(0.0f, 0.0f);
-        const float mean = a.center ? stat.x : 0.0f, r = stat.y;
-        float sum_g = 0.0f, sum_gu = 0.0f;
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            float ww[V];
+            float ww[V], d[V], u[V];
             if constexpr (!kHold) weights(p, ww);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if constexpr (kHold) ww[v] = w[p][v];
-                const float d = v < places.skip[p] ? 0.0f : dy[p][v], u = v < places.skip[p] ? 0.0f : (x[p][v] - mean) * r;
-                const float g = d * ww[v];
-                dw[p][v] = fmaf(d, u, dw[p][v]);
-                db[p][v] += d;
-                sum_g += g;
-                sum_gu = fmaf(g, u, sum_gu);
+                d[v] = now.dy[p][v];
+                u[v] = (now.x[p][v] - mean) * inv;
+            }
+            blank<V>(d, places.skip[p]);
+            blank<V>(u, places.skip[p]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float g = d[v] * ww[v];
+                dw[p][v] = fmaf(d[v], u[v], dw[p][v]);
+                db[p][v] += d[v];
+                sum_g[0] += g;
+                sum_gu[0] = fmaf(g, u[v], sum_gu[0]);
             }
         }
         team.sum(sum_g, sum_gu);
-        const float c1 = a.center ? sum_g * a.inv : 0.0f, c2 = sum_gu * a.inv;
-        if (!here) continue;
+        if (!now.here) continue;
+        const RowAt at(a, row0 + mine);
+        const float c1 = a.center ? sum_g[0] * a.inv : 0.0f, c2 = sum_gu[0] * a.inv;
+        T* po = att_at<T>(a.out, at.b, at.t, at.h);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
+            now.x[p].renew();
+            now.dy[p].renew();
             if (places.skip[p] >= V) continue;
             float ww[V], y[V];
             if constexpr (!kHold) weights(p, ww);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if constexpr (kHold) ww[v] = w[p][v];
-                const float u = (x[p][v] - mean) * r;
-                y[v] = live ? fmaf(r, fmaf(-u, c2, fmaf(dy[p][v], ww[v], -c1)), more[p][v]) : 0.0f;
+                const float u = (now.x[p][v] - mean) * inv;
+                y[v] = now.live ? fmaf(inv, fmaf(-u, c2, fmaf(now.dy[p][v], ww[v], -c1)), now.more[p][v]) : 0.0f;
             }
-            store_row<T, V>(att_at<T>(a.out, at.b, at.t, at.h) + places.at[p], y, places.skip[p]);
+            store_row_once<T, V>(po + places.at[p], y, places.skip[p]);
         }
     }
     if (!a.parts) return;
     float* part = a.parts + (int64_t)blockIdx.x * 2 * a.D;
-    if constexpr (L < kThreads) {
+    if constexpr (L <= kWave) {
         // the teams of a wavefront, then the wavefronts one after another
         __shared__ float whole[2][P * L * V];
 #pragma unroll
@@ -306,8 +360,8 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormArgs a)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_long_kernel(NormArgs a)
 {
-    __shared__ float room[2][2][kThreads / kWave];
-    Team<kThreads> team{room};
+    __shared__ float room[2][1][2][kThreads / kWave];
+    Team<kThreads, 1> team{room};
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const RowAt at(a, row);
         const bool live = at.live(a);
@@ -322,16 +376,18 @@ __global__ __launch_bounds__(kThreads) void norm_long_kernel(NormArgs a)
             continue;
         }
         auto value = [&](int d) { return a.res.p ? (float)(T)((float)px[d] + (float)pr[d]) : (float)px[d]; };
-        float mean = 0.0f, square = 0.0f;
+        float sum[1] = {0.0f}, square[1] = {0.0f};
         if (a.center) {
-            for (int d = (int)threadIdx.x; d < a.D; d += kThreads) mean += value(d);
-            mean = team.sum(mean) * a.inv;
+            for (int d = (int)threadIdx.x; d < a.D; d += kThreads) sum[0] += value(d);
+            team.sum(sum);
         }
+        const float mean = sum[0] * a.inv;
         for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
             const float x = value(d) - mean;
-            square = fmaf(x, x, square);
+            square[0] = fmaf(x, x, square[0]);
         }
-        const float r = rsqrtf(fmaf(team.sum(square), a.inv, a.eps));
+        team.sum(square);
+        const float r = rsqrtf(fmaf(square[0], a.inv, a.eps));
         if (threadIdx.x == 0 && a.stats) a.stats[row] = make_float2(mean, r);
         for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
             const float s = value(d);
@@ -344,8 +400,8 @@ __global__ __launch_bounds__(kThreads) void norm_long_kernel(NormArgs a)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void norm_long_backward_kernel(NormArgs a)
 {
-    __shared__ float room[2][2][kThreads / kWave];
-    Team<kThreads> team{room};
+    __shared__ float room[2][1][2][kThreads / kWave];
+    Team<kThreads, 1> team{room};
     for (uint32_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const RowAt at(a, row);
         T* po = att_at<T>(a.out, at.b, at.t, at.h);
@@ -356,14 +412,14 @@ __global__ __launch_bounds__(kThreads) void norm_long_backward_kernel(NormArgs a
         const T *px = att_at<T>(a.x, at.b, at.t, at.h), *pd = att_at<T>(a.dout, at.b, at.t, at.h), *pr = att_at<T>(a.res, at.b, at.t, at.h);
         const float2 stat = a.stats[row];
         const float mean = a.center ? stat.x : 0.0f, r = stat.y;
-        float sum_g = 0.0f, sum_gu = 0.0f;
+        float sum_g[1] = {0.0f}, sum_gu[1] = {0.0f};
         for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
             const float g = (float)pd[d] * (a.weight ? a.weight[d] : 1.0f);
-            sum_g += g;
-            sum_gu = fmaf(g, ((float)px[d] - mean) * r, sum_gu);
+            sum_g[0] += g;
+            sum_gu[0] = fmaf(g, ((float)px[d] - mean) * r, sum_gu[0]);
         }
         team.sum(sum_g, sum_gu);
-        const float c1 = a.center ? sum_g * a.inv : 0.0f, c2 = sum_gu * a.inv;
+        const float c1 = a.center ? sum_g[0] * a.inv : 0.0f, c2 = sum_gu[0] * a.inv;
         for (int d = (int)threadIdx.x; d < a.D; d += kThreads) {
             const float g = (float)pd[d] * (a.weight ? a.weight[d] : 1.0f), u = ((float)px[d] - mean) * r;
             po[d] = (T)fmaf(r, fmaf(-u, c2, g - c1), a.res.p ? (float)pr[d] : 0.0f);
@@ -431,15 +487,23 @@ __global__ __launch_bounds__(kThreads) void column_sums_kernel(ColumnSums a)
 
 // ---------------------------------------------------------------- host
 
-constexpr int64_t kNormGroups = 1024;        // of the backward pass: each leaves a part of the weights' gradients
+// Workgroups of the backward pass, each of which leaves a part of the weights' gradients: as many as are at work at once, by the registers
+// of a row's pieces (documents of 4096 bfloat16: 768 203 us, 512 263, 1024 235; heads of 128: 1024 74 us, 768 87, 1280 101).
+constexpr int64_t norm_groups_most(int elements, int lanes) { return elements >= 16 ? (lanes > kThreads ? 512 : 768) : 1024; }
 
-// Pieces and lanes of a team.
-template <typename T, typename F>
-inline bool norm_dispatch(int32_t D, F f)
+// f(pieces' elements, pieces, lanes of a team, rows at a time); false for rows that no team holds.  Several rows at a time, for more
+// loads on their way, where there are enough of them to fill the card all the same.
+template <typename T, bool BACK, typename F>
+inline bool norm_dispatch(int64_t rows, int32_t D, F f)
 {
     constexpr int V = kRowPiece<T>;
-    using std::integral_constant;
-#define BLOAD_NORM_CASE(v, p, l) f(integral_constant<int, v>(), integral_constant<int, p>(), integral_constant<int, l>())
+    auto by_rows = [&](auto v, auto p, auto l) {
+        using std::integral_constant;
+        constexpr int kRows = p * v >= 32 ? 1 : (p * v >= 16 ? 2 : 4);
+        if (rows >= 2048 * (kNormThreads<l> / l) * kRows) f(v, p, l, integral_constant<int, kRows>());
+        else f(v, p, l, integral_constant<int, 1>());
+    };
+#define BLOAD_NORM_CASE(v, p, l) by_rows(std::integral_constant<int, v>(), std::integral_constant<int, p>(), std::integral_constant<int, l>())
     const int64_t n = ceil_div(D, V);
     if (D < V) BLOAD_NORM_CASE(1, 1, 8);
     else if (n <= 4) BLOAD_NORM_CASE(V, 1, 4);
@@ -448,11 +512,18 @@ inline bool norm_dispatch(int32_t D, F f)
     else if (n <= 32) BLOAD_NORM_CASE(V, 1, 32);
     else if (n <= 64) BLOAD_NORM_CASE(V, 1, 64);
     else if (n <= 128) BLOAD_NORM_CASE(V, 2, 64);
-    else if (n <= 256) BLOAD_NORM_CASE(V, 1, 256);
-    else if (n <= 512) BLOAD_NORM_CASE(V, 2, 256);
-    else if (n <= 1024) BLOAD_NORM_CASE(V, 4, 256);
-    else if (n <= 2048) BLOAD_NORM_CASE(V, 8, 256);
-    else return false;
+    else if (n > 2048) return false;
+    else if constexpr (V == 4) {             // (floats: half the elements to a piece)
+        if (n <= 512 && BACK) BLOAD_NORM_CASE(V, 2, 256);
+        else if (n <= 512) BLOAD_NORM_CASE(V, 8, 64);
+        else if (n <= 1024) BLOAD_NORM_CASE(V, 4, 256);
+        else BLOAD_NORM_CASE(V, 4, 512);
+    } else {
+        if (n <= 256) BLOAD_NORM_CASE(V, 1, 256);
+        else if (n <= 512) BLOAD_NORM_CASE(V, 2, 256);
+        else if (n <= 1024) BLOAD_NORM_CASE(V, 2, 512);
+        else BLOAD_NORM_CASE(V, 4, 512);
+    }
 #undef BLOAD_NORM_CASE
     return true;
 }
@@ -469,10 +540,10 @@ inline int64_t norm_groups(int64_t rows, int32_t dim, bload_dtype dtype)
 {
     int64_t groups = 0;
     auto by_type = [&](auto type) {
-        if (!norm_dispatch<typename decltype(type)::type>(dim, [&](auto, auto, auto l) {
-                groups = std::min<int64_t>(kNormGroups, ceil_div(rows, kThreads / decltype(l)::value));
+        if (!norm_dispatch<typename decltype(type)::type, true>(rows, dim, [&](auto v, auto p, auto l, auto) {
+                groups = std::min<int64_t>(norm_groups_most(p * v, l), ceil_div(rows, kNormThreads<l> / l));
             }))
-            groups = std::min<int64_t>(kNormGroups, rows);
+            groups = std::min<int64_t>(1024, rows);
     };
     if (dtype == BLOAD_F32) by_type(type_is<float>());
     else by_type(type_is<att_half>());
@@ -489,6 +560,16 @@ inline NormArgs norm_args(int64_t rows, int32_t t_blk, int32_t heads, int32_t di
     a.center = center;
     a.inv = 1.0f / (float)dim;
     return a;
+}
+
+// Where the blocks of all tensors follow one another as their slots do, slots are counted through: one division less a row.
+inline void merge_blocks(NormArgs& a)
+{
+    AttTensor* all[] = {&a.x, &a.res, &a.out, &a.sum, &a.dout};
+    for (AttTensor* t : all)
+        if (t->p && t->sb != t->st * (int64_t)a.T.d) return;
+    for (AttTensor* t : all) t->sb = t->st;
+    a.T = divisor(1);
 }
 
 }  // namespace
@@ -525,12 +606,13 @@ extern "C" bload_status bload_layer_norm(const bload_heads* x, const bload_heads
     a.weight = d_weight;
     a.bias = d_bias;
     a.stats = reinterpret_cast<float2*>(d_stats);
+    merge_blocks(a);
     const hipStream_t stream = (hipStream_t)hip_stream;
     by_dtype(dtype, [&](auto type) {
         using T = typename decltype(type)::type;
-        const bool held = norm_dispatch<T>(dim, [&](auto v, auto p, auto l) {
-            const int64_t groups = std::min<int64_t>(4096, ceil_div(rows, kThreads / l));
-            norm_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a);
+        const bool held = norm_dispatch<T, false>(rows, dim, [&](auto v, auto p, auto l, auto r) {
+            const int64_t groups = std::min<int64_t>(4096, ceil_div(rows, kNormThreads<l> / l * r));
+            norm_kernel<T, v, p, l, r><<<dim3((unsigned)groups), dim3(kNormThreads<l>), 0, stream>>>(a);
         });
         if (!held) norm_long_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);
     });
@@ -579,10 +661,11 @@ extern "C" bload_status bload_layer_norm_backward(const bload_heads* dout, const
         a.valid = d_valid;
         a.weight = d_weight;
         a.stats = reinterpret_cast<float2*>(const_cast<float*>(d_stats));
+        merge_blocks(a);
         by_dtype(dtype, [&](auto type) {
             using T = typename decltype(type)::type;
-            const bool held = norm_dispatch<T>(dim, [&](auto v, auto p, auto l) {
-                norm_backward_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(a);
+            const bool held = norm_dispatch<T, true>(rows, dim, [&](auto v, auto p, auto l, auto) {
+                norm_backward_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kNormThreads<l>), 0, stream>>>(a);
             });
             if (held) return;
             norm_long_backward_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);

@@ -12,10 +12,28 @@ struct RowPiece {
     static constexpr int kWords = V * sizeof(T) >= 4 ? V * (int)sizeof(T) / 4 : 1;
     uint32_t w[kWords];
     __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(&w, p, V * sizeof(T)); }
+    // Read once: the caches need not keep it.
+    __device__ __forceinline__ void load_once(const T* p)
+    {
+        typedef uint32_t words __attribute__((ext_vector_type(kWords), aligned(sizeof(T))));
+        if constexpr (V * sizeof(T) >= 4) {
+            const words v = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = v[i];
+        } else {
+            load(p);
+        }
+    }
     __device__ __forceinline__ void zero()
     {
 #pragma unroll
         for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    // From here on the words count as new ones: what was made of them is made again, where holding it would take more registers.
+    __device__ __forceinline__ void renew()
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) asm volatile("" : "+v"(w[i]));
     }
     __device__ __forceinline__ float operator[](int v) const
     {
@@ -46,6 +64,28 @@ __device__ __forceinline__ void store_row(T* p, const float (&x)[V], int skip)
 #pragma unroll
         for (int v = 1; v < V; ++v)
             if (v >= skip) p[v] = (T)x[v];
+    }
+}
+
+// The same past the caches, for what nothing reads soon.
+template <typename T, int V>
+__device__ __forceinline__ void store_row_once(T* p, const float (&x)[V], int skip)
+{
+    if constexpr (V * sizeof(T) < 4) {
+        store_row<T, V>(p, x, skip);
+    } else {
+        constexpr int kWords = V * (int)sizeof(T) / 4;
+        typedef uint32_t words __attribute__((ext_vector_type(kWords), aligned(sizeof(T))));
+        if (skip == 0) {
+            T t[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) t[v] = (T)x[v];
+            words w;
+            __builtin_memcpy(&w, &t, sizeof(t));
+            __builtin_nontemporal_store(w, reinterpret_cast<words*>(p));
+        } else {
+            store_row<T, V>(p, x, skip);
+        }
     }
 }
 
