@@ -49,6 +49,15 @@ __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf
 
 template <typename T, bool BACK, int K> constexpr int kConvPiece = K <= 4 && !BACK ? kRowPiece<T> : kRowPiece<T> / 2;
 
+// Where a WIDE instance is built: the numbers of taps in use.
+template <int V, int K> constexpr bool kWideTaps = V > 1 && K >= 2 && K <= 4;
+
+template <bool WIDE>
+__device__ __forceinline__ int slot_value(int x)
+{
+    return WIDE ? __builtin_amdgcn_readfirstlane(x) : x;
+}
+
 // What both passes set up: a lane's features and its weights.
 template <int V, int K>
 struct ConvLane {
@@ -83,8 +92,8 @@ __device__ __forceinline__ void load_slot(RowPiece<T, V>& piece, const ConvArgs&
     }
 }
 
-// R: slots of a run.
-template <typename T, int V, int K, int R>
+// R: slots of a run.  WIDE: a wavefront has one run (F is 64), so that ages are the same in all its lanes, and rows are whole pieces.
+template <typename T, int V, int K, int R, bool WIDE>
 __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
 {
     __shared__ uint8_t ages[kThreads * R];
@@ -113,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
 #pragma unroll
     for (int i = 0; i < R; ++i) {
         if (t0 + i >= a.T) break;
-        const int age = ages[lane_item * R + i];
+        const int age = slot_value<WIDE>(ages[lane_item * R + i]);
         float p[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) seen[0][v] = x[K - 1 + i][v];
@@ -131,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
             if (a.silu) p[v] *= sigmoid(p[v]);
             if (age == 0) p[v] = 0.0f;
         }
-        store_row_once<T, V>(att_at<T>(a.out, b, t0 + i, 0) + lane.d, p, lane.skip);
+        store_row_once<T, V>(att_at<T>(a.out, b, t0 + i, 0) + lane.d, p, WIDE ? 0 : lane.skip);
         if (last && t0 + i == a.T - 1)
 #pragma unroll
             for (int j = 0; j < K - 1; ++j)
@@ -143,15 +152,19 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
     }
 }
 
-constexpr int kConvStep = 8, kConvRun = 64;      // slots whose loads are on their way together; most slots of a run, backward
+// Backward: slots whose loads are on their way together, most slots of a run, and slots behind it that its steps may look at.
+constexpr int kConvStep = 4, kConvRun = 64, kConvHalo = 8;
+static_assert(kConvHalo % kConvStep == 0 && kConvHalo >= BLOAD_CONV_MAX_TAPS - 1, "the last step's slots have ages");
 
-template <typename T, int V, int K>
+// SILU: 1 or 0, or -1 where the call says which.
+template <typename T, int V, int K, bool WIDE, int SILU>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
 {
     constexpr int S = kConvStep;
+    const bool silu = SILU < 0 ? a.silu : SILU;
     extern __shared__ float shared[];
-    const int f = (int)threadIdx.x & (a.F - 1), lane_item = (int)threadIdx.x / a.F, each = kThreads / a.F;
-    const int reach = a.run + K - 1;                       // slots whose dp a run needs
+    const int f = (int)threadIdx.x & (a.F - 1), lane_item = slot_value<WIDE>((int)threadIdx.x / a.F), each = kThreads / a.F;
+    const int reach = a.run + kConvHalo;                   // slots whose ages a run needs, in whole steps
     const int slice = (int)(blockIdx.x % a.slices);
     uint8_t* ages = reinterpret_cast<uint8_t*>(shared);    // [each][reach], and the last slot's of each run's block
     uint8_t* last_age = ages + each * reach;
@@ -176,7 +189,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
         if (item >= a.items || !lane.mine) continue;
         const int64_t b = item / a.runs;
         const int t0 = (int)(item - b * a.runs) * a.run, t1 = min(t0 + a.run, a.T), end = t1 + K - 1;
-        const int kept = a.dlast ? last_age[lane_item] : 0;
+        const int kept = slot_value<WIDE>(a.dlast ? last_age[lane_item] : 0);
         float seen[K][V], acc[K][V];                       // acc[j]: of dx of the slot j before, from the slots up to here
 #pragma unroll
         for (int j = 1; j < K; ++j) {
@@ -185,86 +198,104 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
 #pragma unroll
             for (int v = 0; v < V; ++v) seen[j][v] = x[v], acc[j][v] = 0.0f;
         }
+        const T *px = att_at<T>(a.x, b, t0, 0), *pd = att_at<T>(a.dout, b, t0, 0);
+        T* to = att_at<T>(a.out, b, t0, 0);
+        RowPiece<T, V> x_next[S], dy_next[S];              // the next step's, on their way while one is computed
+        auto load = [&](int s0) {
+            const int n = min(end, a.T) - s0;
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                x_next[i].zero();
+                dy_next[i].zero();
+                if (i < n) {
+                    x_next[i].load(px + (s0 - t0 + i) * a.x.st + lane.d);
+                    dy_next[i].load(pd + (s0 - t0 + i) * a.dout.st + lane.d);
+                }
+            }
+        };
+        load(t0);
         for (int s0 = t0; s0 < end; s0 += S) {
             RowPiece<T, V> x[S], dy[S];
 #pragma unroll
-            for (int i = 0; i < S; ++i) {
-                x[i].zero();
-                dy[i].zero();
-                if (s0 + i < min(end, a.T)) {
-                    x[i].load(att_at<T>(a.x, b, s0 + i, 0) + lane.d);
-                    dy[i].load(att_at<T>(a.dout, b, s0 + i, 0) + lane.d);
-                }
-            }
+            for (int i = 0; i < S; ++i) x[i] = x_next[i], dy[i] = dy_next[i];
+            load(s0 + S);
+            // Inner steps: the slots are the run's own, and so are those that they complete, none of which a gradient of the state
+            // reaches; and every slot looks back over all taps.
+            auto step = [&](auto all_inner) {
+                constexpr bool kInner = decltype(all_inner)::value;
 #pragma unroll
-            for (int i = 0; i < S; ++i) {
-                const int s = s0 + i;
-                if (s >= end) break;
-                const int age = ages[lane_item * reach + s - t0];
-                float dp[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    seen[0][v] = x[i][v];
-                    acc[0][v] = 0.0f;
-                    dp[v] = age ? dy[i][v] : 0.0f;
-                }
-                if (age < K)
-#pragma unroll
-                    for (int j = 0; j < K; ++j)
-                        if (j >= age)
-#pragma unroll
-                            for (int v = 0; v < V; ++v) seen[j][v] = 0.0f;
-                if (a.silu && age) {
+                for (int i = 0; i < S; ++i) {
+                    const int s = s0 + i;
+                    if (!kInner && s >= end) break;
+                    const int age = kInner ? K : slot_value<WIDE>(ages[lane_item * reach + s - t0]);
+                    float dp[V];
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        float p = lane.bias[v];
-#pragma unroll
-                        for (int j = K - 1; j >= 0; --j) p = fmaf(lane.w[K - 1 - j][v], seen[j][v], p);
-                        const float sg = sigmoid(p);
-                        dp[v] *= sg * fmaf(p, 1.0f - sg, 1.0f);
+                        seen[0][v] = x[i][v];
+                        acc[0][v] = 0.0f;
+                        dp[v] = age ? dy[i][v] : 0.0f;
                     }
-                }
-                const bool count = s < t1;
-                if (count)
+                    if (!kInner && age < K)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) db[v] += dp[v];
-                if (age >= K) {
+                        for (int j = 0; j < K; ++j)
+                            if (j >= age)
 #pragma unroll
-                    for (int j = 0; j < K; ++j)
+                                for (int v = 0; v < V; ++v) seen[j][v] = 0.0f;
+                    if (silu) {
 #pragma unroll
                         for (int v = 0; v < V; ++v) {
-                            acc[j][v] = fmaf(lane.w[K - 1 - j][v], dp[v], acc[j][v]);
-                            if (count) dw[K - 1 - j][v] = fmaf(dp[v], seen[j][v], dw[K - 1 - j][v]);
+                            float p = lane.bias[v];
+#pragma unroll
+                            for (int j = K - 1; j >= 0; --j) p = fmaf(lane.w[K - 1 - j][v], seen[j][v], p);
+                            const float sg = sigmoid(p);
+                            // (padding: dp stays 0 whatever the slope of the bias)
+                            dp[v] *= sg * fmaf(p, 1.0f - sg, 1.0f);
                         }
-                } else {
+                    }
+                    if (kInner || s < t1)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            db[v] += dp[v];
+#pragma unroll
+                            for (int j = 0; j < K; ++j)
+                                if (kInner || j < age) dw[K - 1 - j][v] = fmaf(dp[v], seen[j][v], dw[K - 1 - j][v]);
+                        }
 #pragma unroll
                     for (int j = 0; j < K; ++j)
-                        if (j < age)
+                        if (kInner || j < age)
 #pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                acc[j][v] = fmaf(lane.w[K - 1 - j][v], dp[v], acc[j][v]);
-                                if (count) dw[K - 1 - j][v] = fmaf(dp[v], seen[j][v], dw[K - 1 - j][v]);
-                            }
-                }
-                // slot u has heard from all that look back to it
-                const int u = s - (K - 1), row = u - (a.T - (K - 1));
-                if (u >= t0 || (t0 == 0 && a.last)) {
-                    if (row >= 0 && row < K - 1 && kept >= K - 1 - row) {
-                        const T* p = reinterpret_cast<const T*>(a.dlast) + (b * (K - 1) + row) * a.D + lane.d;
+                            for (int v = 0; v < V; ++v) acc[j][v] = fmaf(lane.w[K - 1 - j][v], dp[v], acc[j][v]);
+                    // slot u has heard from all that look back to it
+                    const int u = s - (K - 1);
+                    if constexpr (kInner) {
+                        store_row_once<T, V>(to + (u - t0) * a.out.st + lane.d, acc[K - 1], WIDE ? 0 : lane.skip);
+                    } else if (u >= t0 || (t0 == 0 && a.last)) {
+                        const int row = u - (a.T - (K - 1));
+                        if (row >= 0 && row < K - 1 && kept >= K - 1 - row) {
+                            const T* p = reinterpret_cast<const T*>(a.dlast) + (b * (K - 1) + row) * a.D + lane.d;
 #pragma unroll
-                        for (int v = 0; v < V; ++v) acc[K - 1][v] += (float)p[v];
+                            for (int v = 0; v < V; ++v) acc[K - 1][v] += (float)p[v];
+                        }
+                        T* p = u >= 0 ? to + (u - t0) * a.out.st : reinterpret_cast<T*>(a.last) + (b * (K - 1) + K - 1 + u) * a.D;
+                        store_row_once<T, V>(p + lane.d, acc[K - 1], WIDE ? 0 : lane.skip);
                     }
-                    T* to = u >= 0 ? att_at<T>(a.out, b, u, 0) : reinterpret_cast<T*>(a.last) + (b * (K - 1) + K - 1 + u) * a.D;
-                    store_row_once<T, V>(to + lane.d, acc[K - 1], lane.skip);
+#pragma unroll
+                    for (int j = K - 1; j > 0; --j)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            seen[j][v] = seen[j - 1][v];
+                            acc[j][v] = acc[j - 1][v];
+                        }
                 }
+            };
+            uint32_t words[S / 4];
+            __builtin_memcpy(&words, ages + lane_item * reach + s0 - t0, S);
+            bool full = true;
 #pragma unroll
-                for (int j = K - 1; j > 0; --j)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        seen[j][v] = seen[j - 1][v];
-                        acc[j][v] = acc[j - 1][v];
-                    }
-            }
+            for (int i = 0; i < S / 4; ++i) full = full && words[i] == 0x01010101u * K;
+            const bool inner = s0 + S <= t1 && s0 >= t0 + K - 1 && (!a.dlast || s0 + S - 1 < a.T);
+            if (__all(inner && full)) step(std::true_type());
+            else step(std::false_type());
         }
     }
     if (!a.parts) return;
@@ -306,6 +337,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvArgs a)
 struct ConvPlan {
     int32_t V, F, slices, runs, run;
     int64_t items, groups, workgroups;       // workgroups: along the items
+    bool wide;
 };
 
 inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtype dtype, bool back)
@@ -317,6 +349,7 @@ inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtyp
     p.F = 1;
     while (p.F < kWave && p.F < lanes) p.F *= 2;
     p.slices = (int32_t)ceil_div(lanes, p.F);
+    p.wide = p.F == kWave && D % p.V == 0;
     const int64_t each = kThreads / p.F;
     if (!back) {
         p.run = T == 1 ? 1 : 16;
@@ -413,8 +446,9 @@ extern "C" bload_status bload_segment_conv(const bload_heads* x, const float* d_
     by_dtype(dtype, [&](auto type) {
         conv_dispatch_taps<typename decltype(type)::type, false>(feat_dim, taps, [&](auto t, auto v, auto k) {
             using T = typename decltype(t)::type;
-            if (p.run == 1) conv_kernel<T, v, k, 1><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
-            else conv_kernel<T, v, k, 16><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
+            if (p.run == 1) conv_kernel<T, v, k, 1, false><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
+            else if (kWideTaps<v, k> && p.wide) conv_kernel<T, v, k, 16, kWideTaps<v, k>><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
+            else conv_kernel<T, v, k, 16, false><<<grid, block, 0, (hipStream_t)hip_stream>>>(a);
         });
     });
     return launch_status();
@@ -472,10 +506,14 @@ extern "C" bload_status bload_segment_conv_backward(const bload_heads* dout, con
         a.last = d_dstate_in;
         const dim3 grid((unsigned)(p.workgroups * p.slices)), block(kThreads);
         const int64_t each = kThreads / p.F;
-        const size_t lds = std::max<size_t>(each * (p.run + taps), (size_t)p.F * p.V * (taps + 1) * sizeof(float));
+        const size_t lds = std::max<size_t>(each * (p.run + kConvHalo + 1), (size_t)p.F * p.V * (taps + 1) * sizeof(float));
         by_dtype(dtype, [&](auto type) {
             conv_dispatch_taps<typename decltype(type)::type, true>(feat_dim, taps, [&](auto t, auto v, auto k) {
-                conv_backward_kernel<typename decltype(t)::type, v, k><<<grid, block, lds, stream>>>(a);
+                using T = typename decltype(t)::type;
+                constexpr bool kWide = kWideTaps<v, k>;
+                if (kWide && p.wide && silu) conv_backward_kernel<T, v, k, kWide, kWide ? 1 : -1><<<grid, block, lds, stream>>>(a);
+                else if (kWide && p.wide) conv_backward_kernel<T, v, k, kWide, kWide ? 0 : -1><<<grid, block, lds, stream>>>(a);
+                else conv_backward_kernel<T, v, k, false, -1><<<grid, block, lds, stream>>>(a);
             });
         });
         if ((st = launch_status()) != BLOAD_OK) return st;
