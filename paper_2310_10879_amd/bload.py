@@ -727,6 +727,14 @@ def _frames(t: torch.Tensor, shape, dtype, name: str) -> Heads:
     return h
 
 
+def _new(like: torch.Tensor, shape, row: int) -> tuple[torch.Tensor, Heads]:
+    """A new tensor [B, T, ...] of like's type and what the library takes of it, whose rows have `row` elements.  (Nothing to
+    check here, which is a microsecond a tensor.)"""
+    t = like.new_empty(shape)
+    slot = math.prod(shape[2:])
+    return t, Heads(t.data_ptr(), shape[1] * slot, slot, row)
+
+
 def _rows(t: torch.Tensor, shape, dtype, name: str) -> Heads:
     """A tensor [B, T, heads, D], or [B, T, D] for one head."""
     return _heads(t, shape, dtype, name) if len(shape) == 4 else _frames(t, shape, dtype, name)
@@ -742,19 +750,18 @@ def bload_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: 
     residual.  Asynchronous on the current stream."""
     shape, dtype, code = x.shape, x.dtype, _type_code(x)
     B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
-    if out is None:
-        out = x.new_empty(shape)
+    if residual is None and total is not None:
+        raise ValueError("total is the sum with a residual")
+    hx = _rows(x, shape, dtype, "x")
+    out, ho = _new(x, shape, D) if out is None else (out, _rows(out, shape, dtype, "out"))
     hr = hs = None
     if residual is not None:
-        if total is None:
-            total = x.new_empty(shape)
-        hr, hs = _rows(residual, shape, dtype, "residual"), _rows(total, shape, dtype, "total")
-    elif total is not None:
-        raise ValueError("total is the sum with a residual")
+        hr = _rows(residual, shape, dtype, "residual")
+        total, hs = _new(x, shape, D) if total is None else (total, _rows(total, shape, dtype, "total"))
     stats = x.new_empty((*shape[:-1], 2), dtype=torch.float32) if training else None
-    _check(_lib.bload_layer_norm(_rows(x, shape, dtype, "x"), hr, _sized(valid, (B, T), torch.uint8, "valid"), B, T, H, D, code, int(center),
-                                 eps, _sized(weight, (D,), torch.float32, "weight"), _sized(bias, (D,), torch.float32, "bias"),
-                                 _rows(out, shape, dtype, "out"), hs, stats.data_ptr() if training else 0, _stream()))
+    _check(_lib.bload_layer_norm(hx, hr, _sized(valid, (B, T), torch.uint8, "valid"), B, T, H, D, code, int(center), eps,
+                                 _sized(weight, (D,), torch.float32, "weight"), _sized(bias, (D,), torch.float32, "bias"), ho, hs,
+                                 stats.data_ptr() if training else 0, _stream()))
     result = (out,) if residual is None else (out, total)
     if training:
         result += (stats,)
@@ -773,19 +780,21 @@ def bload_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, stats: torch.
     to leave them out.  Asynchronous on the current stream."""
     shape, dtype, code = x.shape, x.dtype, _type_code(x)
     B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+    real, hx = torch.float32, _rows(x, shape, dtype, "x")
     if grads is None:
-        both = x.new_empty((2, D), dtype=torch.float32)
-        grads = x.new_empty(shape), both[0], both[1]
-    dx, dweight, dbias = grads
+        dx, hdx = _new(x, shape, D)
+        dweight, dbias = x.new_empty(D, dtype=real), x.new_empty(D, dtype=real)
+        pw, pb = dweight.data_ptr(), dbias.data_ptr()
+    else:
+        dx, dweight, dbias = grads
+        hdx, pw, pb = _rows(dx, shape, dtype, "dx"), _sized(dweight, (D,), real, "dweight"), _sized(dbias, (D,), real, "dbias")
     if workspace is None and (dweight is not None or dbias is not None):
         need = _lib.bload_layer_norm_backward_workspace_bytes(B, T, H, D, code)
         workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
     _check(_lib.bload_layer_norm_backward(
-        _rows(dout, shape, dtype, "dout"), _rows(x, shape, dtype, "x"), _sized(stats, (*shape[:-1], 2), torch.float32, "stats"),
-        _sized(valid, (B, T), torch.uint8, "valid"), B, T, H, D, code, int(center), _sized(weight, (D,), torch.float32, "weight"),
-        None if dsum is None else _rows(dsum, shape, dtype, "dsum"), _rows(dx, shape, dtype, "dx"),
-        _sized(dweight, (D,), torch.float32, "dweight"), _sized(dbias, (D,), torch.float32, "dbias"), _ptr(workspace), _room(workspace),
-        _stream()))
+        _rows(dout, shape, dtype, "dout"), hx, _sized(stats, (*shape[:-1], 2), real, "stats"), _sized(valid, (B, T), torch.uint8, "valid"),
+        B, T, H, D, code, int(center), _sized(weight, (D,), real, "weight"), None if dsum is None else _rows(dsum, shape, dtype, "dsum"),
+        hdx, pw, pb, _ptr(workspace), _room(workspace), _stream()))
     return dx, dweight, dbias
 
 
@@ -799,14 +808,13 @@ def bload_segment_conv(x: torch.Tensor, weight: torch.Tensor, reset: torch.Tenso
     T <= 8 and is refused where it meets state_in in any other way.  Asynchronous on the current stream."""
     B, T, D = shape = x.shape
     dtype, code, K = x.dtype, _type_code(x), weight.shape[-1]
-    if out is None:
-        out = x.new_empty((B, T, D))
+    hx = _frames(x, shape, dtype, "x")
+    out, ho = _new(x, shape, D) if out is None else (out, _frames(out, shape, dtype, "out"))
     if state is None:
         state = x.new_empty((B, K - 1, D))
-    _check(_lib.bload_segment_conv(_frames(x, shape, dtype, "x"), _sized(weight, (D, K), torch.float32, "weight"),
-                                   _sized(bias, (D,), torch.float32, "bias"), _sized(reset, (B, T), torch.uint8, "reset"),
-                                   _sized(valid, (B, T), torch.uint8, "valid"), B, T, D, K, code, int(silu),
-                                   _sized(state_in, (B, K - 1, D), dtype, "state_in"), _frames(out, shape, dtype, "out"),
+    _check(_lib.bload_segment_conv(hx, _sized(weight, (D, K), torch.float32, "weight"), _sized(bias, (D,), torch.float32, "bias"),
+                                   _sized(reset, (B, T), torch.uint8, "reset"), _sized(valid, (B, T), torch.uint8, "valid"), B, T, D, K,
+                                   code, int(silu), _sized(state_in, (B, K - 1, D), dtype, "state_in"), ho,
                                    _sized(state, (B, K - 1, D), dtype, "state"), _stream()))
     return out, state
 
@@ -821,20 +829,24 @@ def bload_segment_conv_backward(dout: torch.Tensor, x: torch.Tensor, weight: tor
     """Gradients (dx, dweight, dbias, dstate_in) of sum(out * dout) + sum(state * dstate).  grads: four tensors to write into, the
     last three None to leave them out.  Asynchronous on the current stream."""
     B, T, D = shape = x.shape
-    dtype, code, K = x.dtype, _type_code(x), weight.shape[-1]
+    dtype, code, K, real = x.dtype, _type_code(x), weight.shape[-1], torch.float32
+    hx = _frames(x, shape, dtype, "x")
     if grads is None:
-        both = x.new_empty(D * (K + 1), dtype=torch.float32)
-        grads = x.new_empty((B, T, D)), both[:D * K].view(D, K), both[D * K:], x.new_empty((B, K - 1, D))
-    dx, dweight, dbias, dstate_in = grads
+        dx, hdx = _new(x, shape, D)
+        dweight, dbias, dstate_in = x.new_empty((D, K), dtype=real), x.new_empty(D, dtype=real), x.new_empty((B, K - 1, D))
+        pw, pb, ps = dweight.data_ptr(), dbias.data_ptr(), dstate_in.data_ptr()
+    else:
+        dx, dweight, dbias, dstate_in = grads
+        hdx, pw, pb = _frames(dx, shape, dtype, "dx"), _sized(dweight, (D, K), real, "dweight"), _sized(dbias, (D,), real, "dbias")
+        ps = _sized(dstate_in, (B, K - 1, D), dtype, "dstate_in")
     if workspace is None and (dweight is not None or dbias is not None):
         need = _lib.bload_segment_conv_backward_workspace_bytes(B, T, D, K, code)
         workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
     _check(_lib.bload_segment_conv_backward(
-        _frames(dout, shape, dtype, "dout"), _frames(x, shape, dtype, "x"), _sized(weight, (D, K), torch.float32, "weight"),
-        _sized(bias, (D,), torch.float32, "bias"), _sized(reset, (B, T), torch.uint8, "reset"), _sized(valid, (B, T), torch.uint8, "valid"),
-        B, T, D, K, code, int(silu), _sized(state_in, (B, K - 1, D), dtype, "state_in"), _sized(dstate, (B, K - 1, D), dtype, "dstate"),
-        _frames(dx, shape, dtype, "dx"), _sized(dweight, (D, K), torch.float32, "dweight"), _sized(dbias, (D,), torch.float32, "dbias"),
-        _sized(dstate_in, (B, K - 1, D), dtype, "dstate_in"), _ptr(workspace), _room(workspace), _stream()))
+        _frames(dout, shape, dtype, "dout"), hx, _sized(weight, (D, K), real, "weight"), _sized(bias, (D,), real, "bias"),
+        _sized(reset, (B, T), torch.uint8, "reset"), _sized(valid, (B, T), torch.uint8, "valid"), B, T, D, K, code, int(silu),
+        _sized(state_in, (B, K - 1, D), dtype, "state_in"), _sized(dstate, (B, K - 1, D), dtype, "dstate"), hdx, pw, pb, ps,
+        _ptr(workspace), _room(workspace), _stream()))
     return dx, dweight, dbias, dstate_in
 
 
@@ -853,8 +865,10 @@ def bload_selective_scan_backward_workspace_bytes(num_blocks: int, t_blk: int, f
 def _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0) -> Selective:
     B, T, D = shape = x.shape
     dtype, code = x.dtype, _type_code(x)
-    pair = (B, T, *b.shape[2:]) if b.dim() == 4 else (B, T, 1, rate.shape[-1])
-    G, N = pair[2:]
+    if b.dim() != 4:
+        raise ValueError("b: expected [B, T, groups, states]")
+    G, N = b.shape[2:]
+    pair = (B, T, G, N)
     return Selective(_frames(x, shape, dtype, "x"), _frames(dt, shape, dtype, "dt"),
                      Heads() if z is None else _frames(z, shape, dtype, "z"), _heads(b, pair, dtype, "b"), _heads(c, pair, dtype, "c"),
                      _sized(rate, (D, N), torch.float32, "rate"), _sized(skip, (D,), torch.float32, "skip"),
@@ -874,19 +888,20 @@ def bload_selective_scan(x: torch.Tensor, dt: torch.Tensor, rate: torch.Tensor, 
     h0: float32[B, D, N], the state in front of the blocks.  Returns the result and the state behind the last slots (float32[B, D, N]),
     written to `state`, which may be h0 where T <= 8 and is refused where it meets h0 in any other way; with training also what
     ``bload_selective_scan_backward`` needs.  Asynchronous on the current stream."""
-    B, T, D = x.shape
+    B, T, D = shape = x.shape
     s = _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0)
     N, G = s.states, s.groups
-    if out is None:
-        out = x.new_empty((B, T, D))
+    out, ho = _new(x, shape, D) if out is None else (out, _frames(out, shape, x.dtype, "out"))
     if state is None:
         state = x.new_empty((B, D, N), dtype=torch.float32)
+        ps = state.data_ptr()
+    else:
+        ps = _sized(state, (B, D, N), torch.float32, "state")
     saved = x.new_empty((B, -(-T // 16), D, N), dtype=torch.float32) if training else None
     if workspace is None:
         need = _lib.bload_selective_scan_workspace_bytes(B, T, D, N, G)
         workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    _check(_lib.bload_selective_scan(s, _frames(out, x.shape, x.dtype, "out"), _sized(state, (B, D, N), torch.float32, "state"),
-                                     saved.data_ptr() if training else 0, _ptr(workspace), _room(workspace), _stream()))
+    _check(_lib.bload_selective_scan(s, ho, ps, saved.data_ptr() if training else 0, _ptr(workspace), _room(workspace), _stream()))
     return (out, state, saved) if training else (out, state)
 
 
@@ -900,19 +915,24 @@ def bload_selective_scan_backward(dout: torch.Tensor, x: torch.Tensor, dt: torch
     to leave them out.  Asynchronous on the current stream."""
     B, T, D = shape = x.shape
     s = _selective(x, dt, rate, b, c, reset, valid, skip, z, dt_bias, softplus, h0)
-    N, G, dtype = s.states, s.groups, x.dtype
+    N, G, dtype, real = s.states, s.groups, x.dtype, torch.float32
     if grads is None:
-        like = lambda t: None if t is None else x.new_empty(t.shape, dtype=t.dtype)
-        grads = tuple(like(t) for t in (x, dt, rate, b, c, skip, z, dt_bias, h0))
-    dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0 = grads
+        floats = lambda t: None if t is None else x.new_empty(t.shape, dtype=real)
+        (dx, hx), (ddt, hdt), (db, hb), (dc, hc) = _new(x, shape, D), _new(x, shape, D), _new(x, b.shape, N), _new(x, b.shape, N)
+        dz, hz = (None, None) if z is None else _new(x, shape, D)
+        drate, dskip, ddt_bias, dh0 = floats(rate), floats(skip), floats(dt_bias), floats(h0)
+        pr, pk, pb, ph = (0 if t is None else t.data_ptr() for t in (drate, dskip, ddt_bias, dh0))
+    else:
+        dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0 = grads
+        pair = (B, T, G, N)
+        hx, hdt = _frames(dx, shape, dtype, "dx"), _frames(ddt, shape, dtype, "ddt")
+        hb, hc, hz = _heads(db, pair, dtype, "db"), _heads(dc, pair, dtype, "dc"), None if z is None else _frames(dz, shape, dtype, "dz")
+        pr, pk = _sized(drate, (D, N), real, "drate"), _sized(dskip, (D,), real, "dskip")
+        pb, ph = _sized(ddt_bias, (D,), real, "ddt_bias"), _sized(dh0, (B, D, N), real, "dh0")
     if workspace is None:
         need = _lib.bload_selective_scan_backward_workspace_bytes(B, T, D, N, G)
         workspace = torch.empty(max(16, need), dtype=torch.uint8, device=x.device)
-    real = torch.float32
     _check(_lib.bload_selective_scan_backward(
         s, _frames(dout, shape, dtype, "dout"), _sized(saved, (B, -(-T // 16), D, N), real, "saved"), _sized(dstate, (B, D, N), real, "dstate"),
-        _frames(dx, shape, dtype, "dx"), _frames(ddt, shape, dtype, "ddt"), _sized(drate, (D, N), real, "drate"),
-        _heads(db, (B, T, G, N), dtype, "db"), _heads(dc, (B, T, G, N), dtype, "dc"), _sized(dskip, (D,), real, "dskip"),
-        None if z is None else _frames(dz, shape, dtype, "dz"), _sized(ddt_bias, (D,), real, "ddt_bias"),
-        _sized(dh0, (B, D, N), real, "dh0"), _ptr(workspace), _room(workspace), _stream()))
+        hx, hdt, pr, hb, hc, pk, hz, pb, ph, _ptr(workspace), _room(workspace), _stream()))
     return dx, ddt, drate, db, dc, dskip, dz, ddt_bias, dh0

@@ -47,7 +47,7 @@ __device__ __forceinline__ int slot_age(const uint8_t* reset, const uint8_t* val
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-template <typename T, bool BACK, int K> constexpr int kConvPiece = K <= 4 && !BACK ? kRowPiece<T> : kRowPiece<T> / 2;
+template <typename T, bool BACK, int K> constexpr int kConvPiece = kRowPiece<T> / (K <= 4 ? 1 : 2) / (BACK ? 2 : 1);
 
 // Where a WIDE instance is built: the numbers of taps in use.
 template <int V, int K> constexpr bool kWideTaps = V > 1 && K >= 2 && K <= 4;
@@ -343,7 +343,7 @@ struct ConvPlan {
 inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtype dtype, bool back)
 {
     ConvPlan p = {};
-    p.V = (K <= 4 && !back ? 16 : 8) / (int)att_elem_bytes(dtype);
+    p.V = 16 / (int)att_elem_bytes(dtype) / (K <= 4 ? 1 : 2) / (back ? 2 : 1);
     if (D < p.V) p.V = 1;
     const int64_t lanes = ceil_div(D, p.V);
     p.F = 1;

@@ -229,28 +229,35 @@ __global__ __launch_bounds__(kThreads) void scan_short_kernel(ScanArgs a)
     if (a.in) states(a.in + n * a.N, h);
     const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
     for (int t = 0; t < a.T; ++t) {
+        // (all loads are sent before the first is waited for; what padding holds is dropped below)
+        const T x_raw = att_at<T>(a.x, b, t, 0)[d], dt_raw = att_at<T>(a.dt, b, t, 0)[d], z_raw = a.z.p ? att_at<T>(a.z, b, t, 0)[d] : (T)0.0f;
+        const T *pb = att_at<T>(a.b, b, t, group) + n0, *pc = att_at<T>(a.c, b, t, group) + n0;
+        RowPiece<T, 4> bb, cc;
+        if (WHOLE) {
+            bb.load(pb);
+            cc.load(pc);
+        } else {
+            T some[4] = {}, more[4] = {};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n0 + i < a.N) some[i] = pb[i], more[i] = pc[i];
+            __builtin_memcpy(&bb.w, &some, sizeof(some));
+            __builtin_memcpy(&cc.w, &more, sizeof(more));
+        }
         const int what = slot_does(a.reset + b * a.T, a.valid + b * a.T, t, has_state);
         float y = 0.0f;
         if (what != 2)
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[i] = 0.0f;
         if (what) {
-            const float x = (float)att_at<T>(a.x, b, t, 0)[d], v = (float)att_at<T>(a.dt, b, t, 0)[d] + bias;
-            const float step = a.softplus ? softplus(v) : v;
-            const T *pb = att_at<T>(a.b, b, t, group) + n0, *pc = att_at<T>(a.c, b, t, group) + n0;
+            const float x = (float)x_raw, v = (float)dt_raw + bias, step = a.softplus ? softplus(v) : v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bool there = WHOLE || n0 + i < a.N;
-                const float bb = there ? (float)pb[i] : 0.0f, cc = there ? (float)pc[i] : 0.0f;
-                h[i] = fmaf(__builtin_amdgcn_exp2f(step * (rate[i] * kLog2e)), h[i], step * x * bb);
-                y = fmaf(cc, h[i], y);
+                h[i] = fmaf(__builtin_amdgcn_exp2f(step * (rate[i] * kLog2e)), h[i], step * x * bb[i]);
+                y = fmaf(cc[i], h[i], y);
             }
-            y = lanes_sum<L>(y);
-            y = fmaf(skip, x, y);
-            if (a.z.p) {
-                const float z = (float)att_at<T>(a.z, b, t, 0)[d];
-                y *= z * logistic(z);
-            }
+            y = fmaf(skip, x, lanes_sum<L>(y));
+            if (a.z.p) y *= (float)z_raw * logistic((float)z_raw);
         }
         if (lane == 0) att_at<T>(a.out, b, t, 0)[d] = (T)y;
     }

@@ -145,6 +145,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
     __shared__ __attribute__((aligned(16))) float dys[kTile][kGroupC], ys[kTile][kGroupC], qs[kTile][kGroupC], ws[kTile][kGroupC];
     __shared__ __attribute__((aligned(16))) float bs[kTile][NP], cs[kTile][NP];
     __shared__ float sums[kWaves][kTile][2][NP];           // dB and dC of a wavefront's channels
+    __shared__ Four<T> kept[4][kThreads];                  // a thread's x, dt, z and dout until the tile's results go out
     __shared__ __attribute__((aligned(16))) float skips[kGroupC], biases[kGroupC], dskips[kTile][kGroupC], dbiases[kTile][kGroupC];
     ScanPlace at(a, blockIdx.x);
     const int first = at.chunk * a.chunk, end = min(first + a.chunk, a.T), col = wave_id() * kLanesC + lane_id() % kLanesC;
@@ -188,9 +189,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
             pz.load(z, here && gated);
             pb.load(here);
             pc.load(here);
-            load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0);
         };
+        auto load_front = [&](int t0) { load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0); };
         load(last_tile);
+        load_front(last_tile);
         for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
             const TileFlags flags(a, at.b, t0, end, has_state);
             const bool live = flags.live >> at.slot & 1;
@@ -211,12 +213,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
                 pb.stage(bs[at.slot], live);
                 pc.stage(cs[at.slot], live);
             }
-            const Four<T> x_now = x, dt_now = dt, z_now = z, dout_now = dout;
-            float h_now[PARTS][NS];
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-                for (int i = 0; i < NS; ++i) h_now[p][i] = h0[p][i];
+            kept[0][threadIdx.x] = x;
+            kept[1][threadIdx.x] = dt;
+            kept[2][threadIdx.x] = z;
+            kept[3][threadIdx.x] = dout;
             __syncthreads();
             if (t0 > first) load(t0 - kTile);
 
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
                     const int n0 = (p * 4 + at.q) * NS;
                     float start[kTile / kRun][NS], dr[NS];
 #pragma unroll
-                    for (int i = 0; i < NS; ++i) start[0][i] = h_now[p][i], dr[i] = 0.0f;
+                    for (int i = 0; i < NS; ++i) start[0][i] = h0[p][i], dr[i] = 0.0f;
 #pragma unroll
                     for (int r = 1; r < kTile / kRun; ++r) {
 #pragma unroll
@@ -331,10 +331,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
             };
             if (flags.live == 0xffffu && flags.cut == 0) tile(std::true_type());
             else tile(std::false_type());
+            if (t0 > first) load_front(t0 - kTile);
             __syncthreads();
             if (t0 + at.slot < end && at.n_four) {
                 float dx[4], ddt[4], dz[4], dy[4], q[4], w[4], y[4], skip[4], bias[4];
                 float2 s[4];
+                const Four<T> x_now = kept[0][threadIdx.x], dt_now = kept[1][threadIdx.x], z_now = kept[2][threadIdx.x], dout_now = kept[3][threadIdx.x];
                 get_four(dy, &dys[at.slot][four]);
                 get_four(q, &qs[at.slot][four]);
                 get_four(w, &ws[at.slot][four]);

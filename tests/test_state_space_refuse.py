@@ -90,6 +90,7 @@ def test_scan(bl):
                     dict(x=none), dict(dt=none), dict(b=none), dict(c=none), dict(rate=None), dict(reset=None), dict(valid=None)):
             assert f(**bad) == EINVAL, bad
         assert f(T=(1 << 30) + 1) == f(D=(1 << 24) + 2) == f(B=1 << 40) == f(B=1 << 30, T=1, D=64) == EOVERFLOW
+        assert f(B=1 << 9, T=1 << 30, D=1 << 24, N=4) == EOVERFLOW             # sizes of workspaces beyond 64 bits
         assert f(x=heads(bl, P + 1)) == f(z=heads(bl, P + 2), dtype=F32) == f(rate=P + 2) == f(skip=P + 1) == f(bias=P + 2) == f(h0=P + 2) == EALIGN
     assert lib.bload_selective_scan(None, heads(bl), None, None, None, 0, None) == EINVAL
     assert forward(out=None) == forward(out=none) == EINVAL and forward(state=P + 2) == forward(saved=P + 2) == EALIGN
