@@ -148,6 +148,44 @@ struct ColumnSums {
 };
 bload_status column_sums(const ColumnSums& a, hipStream_t stream);
 
+// 64 columns to a workgroup, 16 lanes of four columns and 16 shares of the parts, whose sums are added in their order.
+__device__ __forceinline__ void column_sums_of_64(const ColumnSums& a, int64_t group)
+{
+    constexpr int kShares = 16;
+    __shared__ float sums[kShares][64];
+    const int c = ((int)threadIdx.x % 16) * 4, share = (int)threadIdx.x / 16;
+    const int64_t first = group * 64 + c, each = (a.n_parts + kShares - 1) / kShares;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (first + 4 <= a.columns) {
+#pragma unroll 4
+        for (int64_t p = share * each; p < min((share + 1) * each, a.n_parts); ++p) {
+            float x[4];
+            load_floats<4>(a.parts + p * a.columns + first, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += x[i];
+        }
+    } else {
+        for (int64_t p = share * each; p < min((share + 1) * each, a.n_parts); ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (first + i < a.columns) s[i] += a.parts[p * a.columns + first + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[share][c + i] = s[i];
+    __syncthreads();
+    const int64_t column = group * 64 + threadIdx.x;
+    if (threadIdx.x >= 64 || column >= a.columns) return;
+    float y = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kShares; ++i) y += sums[i][threadIdx.x];
+    int64_t from = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (column >= from && column < a.end[i] && a.dst[i]) a.dst[i][column - from] = y;
+        from = a.end[i];
+    }
+}
+
 template <typename F>
 inline void by_dtype(bload_dtype dtype, F f)
 {

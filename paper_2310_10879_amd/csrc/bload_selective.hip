@@ -15,6 +15,10 @@
 // own part of the state behind it and the sum of its steps (the product of its a_n is exp(A_n sum)), a second joins them, a third
 // computes the results from the joined states.  No workgroup waits for another one.
 // States, steps, exponentials and sums are in 32 bits; only results are rounded to the type.
+// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16: 0.79 ms; the vector units are busy for 0.54 of it with 34
+// instructions a slot and wavefront (of 16 channels), 20 of them the states', the rest softplus, gates and staging.  512 workgroups, two a
+// compute unit: what is left are waits that two wavefronts a SIMD do not hide.  2 blocks of 4096, 2048 channels, cut into 16 chunks:
+// 64 + 5 + 107 us.  One slot of 256 streams, 4096 channels: 28 us for 143 MB, 5.1 TB/s.
 #include <algorithm>
 
 #include "bload_selective.hpp"
@@ -58,6 +62,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
     Stream<T> px(a.x, at, first), pdt(a.dt, at, first), pz(a.z, at, first), pout(a.out, at, first);
     PairStream<T, NP> pb(a.b, a, at, first), pc(a.c, a, at, first);
     Four<T> x, dt, z;                                      // of the tile that is staged next
+    TileLook look;
     auto load = [&](int t0) {
         const bool here = t0 + at.slot < end;
         px.load(x, here);
@@ -65,6 +70,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
         if (!MAPS) pz.load(z, here && a.z.p);
         pb.load(here);
         if (!MAPS) pc.load(here);
+        look.load(a, at.b, t0);
     };
     auto stage = [&](int buf, const TileFlags& flags) {
         const bool live = flags.live >> at.slot & 1;
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
     };
 
     load(first);
-    TileFlags flags(a, at.b, first, end, has_state);
+    TileFlags flags = look.flags(first, end, has_state);
     stage(0, flags);
     Four<T> x_now = x, z_now = z, x_before = x, z_before = z;
     bool live_before = false;
@@ -152,7 +158,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))
         live_before = flags.live >> at.slot & 1;
         x_before = x_now, z_before = z_now;
         if (more) {
-            flags = TileFlags(a, at.b, t0 + kTile, end, has_state);
+            flags = look.flags(t0 + kTile, end, has_state);
             stage(buf ^ 1, flags);
             x_now = x, z_now = z;
         }

@@ -199,16 +199,26 @@ __device__ __forceinline__ float sum_states(float y0, float y1, float y2, float 
 }
 
 // What the slots of a tile do, one bit each, the same in every lane of a wavefront: whether they are valid, and whether the state
-// in front of them is dropped.  Slots from `end` on do nothing: neither.
+// in front of them is dropped.  Slots from `end` on do nothing: neither.  The flags are sent for with the tile's other inputs, long
+// before they are looked at.
 struct TileFlags {
     uint32_t live, cut;
-    __device__ __forceinline__ TileFlags(const ScanArgs& a, int64_t b, int t0, int end, bool has_state)
+};
+struct TileLook {
+    uint8_t reset, valid, before;
+    __device__ __forceinline__ void load(const ScanArgs& a, int64_t b, int t0)
     {
         const int t = t0 + lane_id() % kTile;
-        int what = 3;
-        if (t < end) what = slot_does(a.reset + b * a.T, a.valid + b * a.T, t, has_state);
-        live = (uint32_t)__ballot(what == 1 || what == 2) & 0xffffu;
-        cut = (uint32_t)__ballot(what == 0 || what == 1) & 0xffffu;
+        const int64_t at = b * a.T + min(t, a.T - 1);
+        reset = a.reset[at];
+        valid = a.valid[at];
+        before = a.valid[t > 0 ? at - 1 : at];
+    }
+    __device__ __forceinline__ TileFlags flags(int t0, int end, bool has_state) const
+    {
+        const int t = t0 + lane_id() % kTile;
+        const bool there = t < end, live = there && valid, on = live && !reset && (t > 0 ? before != 0 : has_state);
+        return {(uint32_t)__ballot(live) & 0xffffu, (uint32_t)__ballot(there && !on) & 0xffffu};
     }
 };
 

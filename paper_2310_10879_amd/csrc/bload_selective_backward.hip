@@ -11,6 +11,13 @@
 // are exchanges between the four lanes of a channel; sums over channels (dB, dC) halve 2 NS values four times between 16 lanes,
 // then the workgroup's wavefronts through LDS, and leave a share for each slice of 64 channels, which a
 // last kernel adds in a fixed order.  The gradients of A, skip and bias stay in registers and are added by column_sums.
+//
+// States and decays of 16 slots at once do not fit beside two wavefronts a SIMD (5.0 ms in the case below, one wavefront): a lane holds
+// 8, the second half of a tile first, for which the first half's states are formed once more in front (3 of some 23
+// issue slots of an element).  A state saved for every 8 slots in place of 16 would save those and cost as much in bytes.
+// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16, with z: 2.3 ms, the vector units busy for 1.7 of them: 114
+// instructions a slot and wavefront of 16 channels, 8 for the first half again, 22 for states, decays and y, 32 on the
+// way back, 30 for dB and dC, the rest staging, gates and sums.
 #include <algorithm>
 
 #include "bload_selective.hpp"
@@ -79,12 +86,14 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
     Stream<T, true> pdt(a.dt, at, last_tile), pz(a.z, at, last_tile), pdo(a.dout, at, last_tile);
     PairStream<T, NP, true> pc(a.c, a, at, last_tile);
     Four<T> dt, z, dout;
+    TileLook look;
     auto load = [&](int t0) {
         const bool here = t0 + at.slot < end;
         pdt.load(dt, here);
         pdo.load(dout, here);
         pz.load(z, here && a.z.p);
         pc.load(here);
+        look.load(a, at.b, t0);
     };
     auto stage = [&](int buf, const TileFlags& flags) {
         const bool live = flags.live >> at.slot & 1;
@@ -100,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
         pc.stage(cs[buf][at.slot], live);
     };
     load(last_tile);
-    TileFlags flags(a, at.b, last_tile, end, a.in != nullptr);
+    TileFlags flags = look.flags(last_tile, end, a.in != nullptr);
     stage(0, flags);
     int buf = 0;
     for (int t0 = last_tile; t0 >= first; t0 -= kTile, buf ^= 1) {
@@ -127,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void scan_backward_maps_kernel(ScanArgs a
         }
         any_cut |= flags.cut != 0;
         if (more) {
-            flags = TileFlags(a, at.b, t0 - kTile, end, a.in != nullptr);
+            flags = look.flags(t0 - kTile, end, a.in != nullptr);
             stage(buf ^ 1, flags);
         }
     }
@@ -180,6 +189,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
         Stream<T, true> pdx(a.dx, at, last_tile), pddt(a.ddt, at, last_tile), pdz(a.dz, at, last_tile);
         PairStream<T, NP, true> pb(a.b, a, at, last_tile), pc(a.c, a, at, last_tile);
         Four<T> x, dt, z, dout;
+        TileLook look;
         float h0[PARTS][NS];
         auto load = [&](int t0) {
             const bool here = t0 + at.slot < end;
@@ -189,12 +199,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
             pz.load(z, here && gated);
             pb.load(here);
             pc.load(here);
+            look.load(a, at.b, t0);
         };
         auto load_front = [&](int t0) { load_states<NS, PARTS>(a.saved, at.b * a.tiles + t0 / kTile, a, at, h0); };
         load(last_tile);
         load_front(last_tile);
         for (int t0 = last_tile; t0 >= first; t0 -= kTile) {
-            const TileFlags flags(a, at.b, t0, end, has_state);
+            const TileFlags flags = look.flags(t0, end, has_state);
             const bool live = flags.live >> at.slot & 1;
             {
                 float2 s[4];
@@ -400,10 +411,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
     }
 }
 
-// dB and dC: the slices' shares, added in their order.
+// dB and dC: the slices' shares, added in their order; and in the workgroups behind them, the sums of the other gradients.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void scan_shares_kernel(ScanArgs a, int64_t all)
+__global__ __launch_bounds__(kThreads) void scan_finish_kernel(ScanArgs a, int64_t all, int64_t groups, ColumnSums c)
 {
+    if ((int64_t)blockIdx.x >= groups) {
+        column_sums_of_64(c, (int64_t)blockIdx.x - groups);
+        return;
+    }
     const int64_t n = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (n >= all) return;
     float s = 0.0f;
@@ -479,7 +494,8 @@ extern "C" bload_status bload_selective_scan_backward(const bload_selective* s, 
         if (!aligned_to(d_workspace, 16)) return BLOAD_EALIGN;
         if (workspace_bytes < room.bytes) return BLOAD_EWORKSPACE;
         const int64_t all = a.B * (int64_t)a.T * a.G * 2 * a.N, groups = ceil_div(all, kThreads);
-        if (groups > kMaxGroups) return BLOAD_EOVERFLOW;
+        const int64_t sums = d_drate || d_dskip || d_ddt_bias ? ceil_div(c.columns, 64) : 0;
+        if (groups > kMaxGroups - sums) return BLOAD_EOVERFLOW;
         char* p = static_cast<char*>(d_workspace);
         a.maps = reinterpret_cast<float*>(p);
         a.spans = reinterpret_cast<float*>(p += room.maps);
@@ -489,6 +505,8 @@ extern "C" bload_status bload_selective_scan_backward(const bload_selective* s, 
         a.saved = const_cast<float*>(d_saved);
         a.dlast = d_dstate_out;
         a.last = d_dstate_in;
+        c.parts = a.parts;
+        c.n_parts = room.n_parts;
         const dim3 block(kThreads);
         const int64_t each = (int64_t)a.chunks * a.G * a.slices;
         by_dtype(dtype, [&](auto type) {
@@ -499,12 +517,10 @@ extern "C" bload_status bload_selective_scan_backward(const bload_selective* s, 
                     scan_join(a, a.dlast, true, stream);
                 }
                 scan_backward_kernel<T, ns, parts><<<dim3((unsigned)(a.blocks * each)), block, 0, stream>>>(a);
-                scan_shares_kernel<T><<<dim3((unsigned)groups), block, 0, stream>>>(a, all);
+                scan_finish_kernel<T><<<dim3((unsigned)(groups + sums)), block, 0, stream>>>(a, all, groups, c);
             });
         });
-        if ((st = launch_status()) != BLOAD_OK) return st;
-        c.parts = a.parts;
-        c.n_parts = room.n_parts;
+        return launch_status();
     }
     return d_drate || d_dskip || d_ddt_bias ? column_sums(c, stream) : BLOAD_OK;
 }
