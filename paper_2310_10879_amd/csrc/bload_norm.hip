@@ -262,11 +262,16 @@ __global__ __launch_bounds__(kNormThreads<L>) void norm_backward_kernel(NormArgs
         for (int v = 0; v < V; ++v) dw[p][v] = db[p][v] = 0.0f;
     }
     const uint32_t step = gridDim.x * kTeams, mine = (int)threadIdx.x / L;
-    BackRow<T, V, P> next;
-    next.load(a, places, blockIdx.x * kTeams + mine);
+    constexpr bool kAhead = P * V < 32;      // (more pieces leave no registers for the next row's)
+    BackRow<T, V, P> now, next;
+    if (kAhead) next.load(a, places, blockIdx.x * kTeams + mine);
     for (uint32_t row0 = blockIdx.x * kTeams; row0 < a.rows; row0 += step) {
-        BackRow<T, V, P> now = next;
-        next.load(a, places, row0 + step + mine);
+        if constexpr (kAhead) {
+            now = next;
+            next.load(a, places, row0 + step + mine);
+        } else {
+            now.load(a, places, row0 + mine);
+        }
         const float mean = a.center ? now.stat.x : 0.0f, inv = now.stat.y;
         float sum_g[1] = {0.0f}, sum_gu[1] = {0.0f};
 #pragma unroll

@@ -154,6 +154,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
     __shared__ __attribute__((aligned(16))) float dys[kTile][kGroupC], ys[kTile][kGroupC], qs[kTile][kGroupC], ws[kTile][kGroupC];
     __shared__ __attribute__((aligned(16))) float bs[kTile][NP], cs[kTile][NP];
     __shared__ float sums[kWaves][kTile][2][NP];           // dB and dC of a wavefront's channels
+    __shared__ __attribute__((aligned(16))) float drates[PARTS][kThreads][NS], losts[PARTS][kThreads][NS];       // a lane's sums of dA so far
     __shared__ Four<T> kept[4][kThreads];                  // a thread's x, dt, z and dout until the tile's results go out
     __shared__ __attribute__((aligned(16))) float skips[kGroupC], biases[kGroupC], dskips[kTile][kGroupC], dbiases[kTile][kGroupC];
     ScanPlace at(a, blockIdx.x);
@@ -164,12 +165,15 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
     const int lane = lane_id() % 16, value = channel_value<2 * NS>(lane);              // whose sums over channels the lane gets
     float* my_sums = &sums[wave_id()][lane & 1][value / NS][at.q * NS + value % NS];    // of even slots or odd ones
 
-    float rate[PARTS][NS], drate[PARTS][NS], lost[PARTS][NS];
+    float rate[PARTS][NS];
     load_states<NS, PARTS>(a.rate, 0, a, at, rate);
 #pragma unroll
     for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) rate[p][i] *= kLog2e, drate[p][i] = lost[p][i] = 0.0f;
+        for (int i = 0; i < NS; ++i) {
+            rate[p][i] *= kLog2e;
+            drates[p][threadIdx.x][i] = losts[p][threadIdx.x][i] = 0.0f;
+        }
     if ((int)threadIdx.x < kGroupC) {
         const int d = at.d0 + (int)threadIdx.x;
         skips[threadIdx.x] = a.skip && d < at.d1 ? a.skip[d] : 0.0f;
@@ -334,9 +338,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
                     // tiles are added with what the additions round off kept beside: there may be thousands
 #pragma unroll
                     for (int i = 0; i < NS; ++i) {
-                        const float more = dr[i] - lost[p][i], sum = drate[p][i] + more;
-                        lost[p][i] = (sum - drate[p][i]) - more;
-                        drate[p][i] = sum;
+                        const float had = drates[p][threadIdx.x][i], more = dr[i] - losts[p][threadIdx.x][i], sum = had + more;
+                        losts[p][threadIdx.x][i] = (sum - had) - more;
+                        drates[p][threadIdx.x][i] = sum;
                     }
                 }
             };
@@ -399,6 +403,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
         if (a.last && a.chunks == 1) store_states<NS, PARTS>(a.last, at.b, a, at, u);
     }
     float* to = a.parts + part * a.D * (a.N + 2);
+    float drate[PARTS][NS];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+        for (int i = 0; i < NS; ++i) drate[p][i] = drates[p][threadIdx.x][i];
     store_states<NS, PARTS>(to, 0, a, at, drate);
     // dskip and dbias of the 16 slots of a tile, one after another
     to += (int64_t)a.D * a.N;
