@@ -556,8 +556,10 @@ bload_status bload_rotary_frequencies(int32_t rot_dim, double base, double facto
  * d_weight, d_bias in  float32[dim], or NULL for ones and zeros
  * sum             out  s, or NULL
  * d_stats         out  float32[num_blocks, t_blk, heads, 2], 8-byte aligned, or NULL: mean and 1 / deviation, for the backward pass
- * The mean, the mean square and everything per element are in 32 bits.  num_blocks * t_blk * heads < 2^31.
- * Asynchronous on `hip_stream`, no workspace; same inputs give bit-identical outputs. */
+ * The mean, the mean square and everything per element are in 32 bits.  num_blocks * t_blk * heads < 2^31, dim up to
+ * BLOAD_LAYER_NORM_MAX_DIM.  Asynchronous on `hip_stream`, no workspace; same inputs give bit-identical outputs. */
+#define BLOAD_LAYER_NORM_MAX_DIM (1 << 21)
+
 bload_status bload_layer_norm(const bload_heads* x, const bload_heads* residual, const uint8_t* d_valid, int64_t num_blocks,
                               int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype, int32_t center, float eps,
                               const float* d_weight, const float* d_bias, const bload_heads* out, const bload_heads* sum,

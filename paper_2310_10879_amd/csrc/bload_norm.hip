@@ -460,6 +460,8 @@ __global__ __launch_bounds__(kThreads) void column_sums_kernel(ColumnSums a) { c
 
 // ---------------------------------------------------------------- host
 
+constexpr int64_t kLongGroups = 1024;        // of rows that no team holds
+static_assert(kLongGroups * ((int64_t)BLOAD_LAYER_NORM_MAX_DIM / kThreads) <= kMaxGroups && BLOAD_LAYER_NORM_MAX_DIM / kThreads < 65536, "a launch holds them");
 // Workgroups of the backward pass, each of which leaves a part of the weights' gradients: as many as are at work at once, by the registers
 // of a row's pieces (documents of 4096 bfloat16: 768 203 us, 512 263, 1024 235; heads of 128: 1024 74 us, 768 87, 1280 101).
 constexpr int64_t norm_groups_most(int elements, int lanes) { return elements >= 16 ? (lanes > kThreads ? 512 : 768) : 1024; }
@@ -504,7 +506,8 @@ inline bool norm_dispatch(int64_t rows, int32_t D, F f)
 inline bload_status norm_check(int64_t num_blocks, int32_t t_blk, int32_t heads, int32_t dim, bload_dtype dtype)
 {
     if (num_blocks < 0 || t_blk < 1 || heads < 1 || dim < 1 || !att_dtype(dtype)) return BLOAD_EINVAL;
-    if (t_blk > (1 << 30) || dim > (1 << 30) || num_blocks > 0x7fffffffLL / t_blk / heads) return BLOAD_EOVERFLOW;
+    // (dim: what a launch holds of workgroups over the rows' shares and the columns of norm_long_columns_kernel)
+    if (t_blk > (1 << 30) || dim > BLOAD_LAYER_NORM_MAX_DIM || num_blocks > 0x7fffffffLL / t_blk / heads) return BLOAD_EOVERFLOW;
     return BLOAD_OK;
 }
 
@@ -516,7 +519,7 @@ inline int64_t norm_groups(int64_t rows, int32_t dim, bload_dtype dtype)
         if (!norm_dispatch<typename decltype(type)::type, true>(rows, dim, [&](auto v, auto p, auto l, auto) {
                 groups = std::min<int64_t>(norm_groups_most(p * v, l), ceil_div(rows, kNormThreads<l> / l));
             }))
-            groups = std::min<int64_t>(1024, rows);
+            groups = std::min<int64_t>(kLongGroups, rows);
     };
     if (dtype == BLOAD_F32) by_type(type_is<float>());
     else by_type(type_is<att_half>());

@@ -15,10 +15,10 @@
 // own part of the state behind it and the sum of its steps (the product of its a_n is exp(A_n sum)), a second joins them, a third
 // computes the results from the joined states.  No workgroup waits for another one.
 // States, steps, exponentials and sums are in 32 bits; only results are rounded to the type.
-// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16: 0.79 ms; the vector units are busy for 0.54 of it with 34
+// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16: 0.75 ms; the vector units are busy for 0.54 of it with 34
 // instructions a slot and wavefront (of 16 channels), 20 of them the states', the rest softplus, gates and staging.  512 workgroups, two a
 // compute unit: what is left are waits that two wavefronts a SIMD do not hide.  2 blocks of 4096, 2048 channels, cut into 16 chunks:
-// 64 + 5 + 107 us.  One slot of 256 streams, 4096 channels: 28 us for 143 MB, 5.1 TB/s.
+// 62 + 5 + 94 us.  One slot of 256 streams, 4096 channels: 28 us for 143 MB, 5.1 TB/s.
 #include <algorithm>
 
 #include "bload_selective.hpp"
@@ -29,7 +29,7 @@ namespace {
 // LDS holds two tiles: while one is computed the next is staged and the results of the one in front go out, with one barrier a tile.
 // What a lane reads of LDS for four slots it reads while it computes the four in front of them.
 template <typename T, int NS, int PARTS, bool MAPS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))) void scan_kernel(ScanArgs a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS == 1 ? 3 : 2, 4))) void scan_kernel(ScanArgs a)
 {
     constexpr int NP = 4 * NS * PARTS;
     __shared__ __attribute__((aligned(16))) float2 steps[2][kTile][kGroupC];           // step, step x

@@ -21,7 +21,7 @@ def test_norm(bl):
         for bad in (dict(B=-1), dict(T=0), dict(H=0), dict(D=0), dict(dtype=0), dict(dtype=I32), dict(center=2), dict(center=-1), dict(x=None),
                     dict(x=heads(bl, 0))):
             assert f(**bad) == EINVAL, bad
-        assert f(T=(1 << 30) + 1) == f(D=(1 << 30) + 1) == f(B=1 << 40) == f(B=1 << 21, T=1 << 9, H=2) == EOVERFLOW
+        assert f(T=(1 << 30) + 1) == f(D=(1 << 21) + 1) == f(B=1 << 40) == f(B=1 << 21, T=1 << 9, H=2) == EOVERFLOW
         assert f(x=heads(bl, P + 1)) == f(x=heads(bl, P + 2), dtype=F32) == f(w=P + 2) == f(stats=P + 4) == EALIGN
     for bad in (dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(out=None)):
         assert forward(**bad) == EINVAL, bad
