@@ -14,9 +14,9 @@
 // and left in the workspace, and column_sums adds the workgroups' in a fixed order.
 // Backward a step is four slots, whose inputs are loaded while the four in front of them are computed, and a step whose slots all look back
 // over all taps and lie inside the run has no branch in it.  Half of the forward pass's 16 bytes to a lane there: with all of them,
-// or with more slots to a step, the registers spill (342 -> 822 us).
-// Measured: 48000 slots of 4096 bfloat16, 4 taps, sequences of some 24 slots: forward 151 us for 0.79 GB, 5.2 TB/s; backward 339 us
-// for 1.18 GB, 3.5 TB/s: 37 vector instructions an element, 28 of them the formulas', and memory that waits for them.
+// or with more slots to a step, the registers spill (343 -> 822 us).
+// Measured: 48000 slots of 4096 bfloat16, 4 taps, sequences of some 24 slots: forward 151 us for 0.79 GB, 5.2 TB/s; backward 310 us
+// for 1.18 GB, 3.8 TB/s (runs of 128 slots; 64 343 us, 32 372): 36 vector instructions an element, 28 of them the formulas', and memory that waits for them.
 #include <algorithm>
 
 #include "bload_rows.hpp"
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvArgs a)
 }
 
 // Backward: slots whose loads are on their way together, most slots of a run, and slots behind it that its steps may look at.
-constexpr int kConvStep = 4, kConvRun = 64, kConvHalo = 8;
+constexpr int kConvStep = 4, kConvRun = 128, kConvHalo = 8;
 static_assert(kConvHalo % kConvStep == 0 && kConvHalo >= BLOAD_CONV_MAX_TAPS - 1, "the last step's slots have ages");
 
 // SILU: 1 or 0, or -1 where the call says which.
@@ -360,7 +360,7 @@ inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtyp
         p.run = T == 1 ? 1 : 16;
     } else {
         // long runs read little twice; short ones where long ones would leave the card empty
-        p.run = kConvRun;
+        p.run = std::min(kConvRun, 16 * p.F);              // (ages of 4096 slots of a workgroup, at most)
         while (p.run > 16 && ceil_div(B * ceil_div(T, p.run), each) * p.slices < 1024) p.run /= 2;
     }
     p.runs = (int32_t)ceil_div(T, p.run);
