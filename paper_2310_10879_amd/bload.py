@@ -740,6 +740,12 @@ def _rows(t: torch.Tensor, shape, dtype, name: str) -> Heads:
     return _heads(t, shape, dtype, name) if len(shape) == 4 else _frames(t, shape, dtype, name)
 
 
+def _row_sizes(shape):
+    if len(shape) not in (3, 4):
+        raise ValueError(f"x: expected [B, T, D] or [B, T, heads, D], got {tuple(shape)}")
+    return shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+
+
 def bload_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                      residual: torch.Tensor | None = None, valid: torch.Tensor | None = None, eps: float = 1e-5, center: bool = True,
                      training: bool = False, out: torch.Tensor | None = None, total: torch.Tensor | None = None):
@@ -749,7 +755,7 @@ def bload_layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: 
     (written to `total`); with training also float32[B, T(, heads), 2] for ``bload_layer_norm_backward``.  out may be x, total may be
     residual.  Asynchronous on the current stream."""
     shape, dtype, code = x.shape, x.dtype, _type_code(x)
-    B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+    B, T, H, D = _row_sizes(shape)
     if residual is None and total is not None:
         raise ValueError("total is the sum with a residual")
     hx = _rows(x, shape, dtype, "x")
@@ -779,7 +785,7 @@ def bload_layer_norm_backward(dout: torch.Tensor, x: torch.Tensor, stats: torch.
     sum where it had a residual.  dx is the gradient of both then.  grads: three tensors to write into, the last two float32[D] or None
     to leave them out.  Asynchronous on the current stream."""
     shape, dtype, code = x.shape, x.dtype, _type_code(x)
-    B, T, H, D = shape if len(shape) == 4 else (shape[0], shape[1], 1, shape[2])
+    B, T, H, D = _row_sizes(shape)
     real, hx = torch.float32, _rows(x, shape, dtype, "x")
     if grads is None:
         dx, hdx = _new(x, shape, D)

@@ -120,6 +120,10 @@ def test_binding_checks_its_tensors(bl):
         bl.bload_layer_norm(cpu)
     with pytest.raises(ValueError):
         bl.bload_layer_norm(cpu.double())
+    with pytest.raises(ValueError, match="expected \\[B, T, D\\]"):
+        bl.bload_layer_norm(torch.zeros(8, 16))
+    with pytest.raises(ValueError, match="groups, states"):
+        bl.bload_selective_scan(cpu, cpu, torch.zeros(16, 4), torch.zeros(2, 8, 4), torch.zeros(2, 8, 4), flags, flags)
     with pytest.raises(ValueError, match="sum with a residual"):
         bl.bload_layer_norm(cpu, total=cpu)
     with pytest.raises(ValueError):
