@@ -644,10 +644,11 @@ extern "C" bload_status bload_layer_norm_backward(const bload_heads* dout, const
                 norm_backward_kernel<T, v, p, l><<<dim3((unsigned)groups), dim3(kNormThreads<l>), 0, stream>>>(a);
             });
             if (held) return;
-            norm_long_backward_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);
+            // (the columns first: dx may lie where dout does)
             const uint32_t each = (uint32_t)ceil_div(rows, groups);
             if (sums)
                 norm_long_columns_kernel<T><<<dim3((unsigned)groups, (unsigned)ceil_div(dim, kThreads)), dim3(kThreads), 0, stream>>>(a, each);
+            norm_long_backward_kernel<T><<<dim3((unsigned)std::min<int64_t>(4096, rows)), dim3(kThreads), 0, stream>>>(a);
         });
         if ((st = launch_status()) != BLOAD_OK) return st;
         c.parts = a.parts;
