@@ -204,15 +204,25 @@ __device__ __forceinline__ float sum_states(float y0, float y1, float y2, float 
 struct TileFlags {
     uint32_t live, cut;
 };
+// Whose flags are looked at for slot t of a block of T: its own and those of the one in front, both inside the block whatever t is.
+// (What is read for a first slot's front, and for slots behind the block, is not used.)
+struct LookSlots {
+    int own, front;
+};
+__host__ __device__ constexpr LookSlots look_slots(int t, int T)
+{
+    const int own = t < T ? t : T - 1;
+    return {own, own > 0 ? own - 1 : 0};
+}
 struct TileLook {
     uint8_t reset, valid, before;
     __device__ __forceinline__ void load(const ScanArgs& a, int64_t b, int t0)
     {
-        const int t = t0 + lane_id() % kTile;
-        const int64_t at = b * a.T + min(t, a.T - 1);
-        reset = a.reset[at];
-        valid = a.valid[at];
-        before = a.valid[t > 0 ? at - 1 : at];
+        const LookSlots look = look_slots(t0 + lane_id() % kTile, a.T);
+        const int64_t first = b * a.T;
+        reset = a.reset[first + look.own];
+        valid = a.valid[first + look.own];
+        before = a.valid[first + look.front];
     }
     __device__ __forceinline__ TileFlags flags(int t0, int end, bool has_state) const
     {
