@@ -145,10 +145,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (flags.cut >> (4 * g + i) & 1)
+                    if (flags.cut >> (4 * g + i) & 1) {    // (no product with a state of 0: a decay that overflows would make it NaN)
+                        const float2 v = s[g & 1][i];
 #pragma unroll
-                        for (int k = 0; k < NS; ++k) h[p][k] = 0.0f;
-                    slot(i);
+                        for (int k = 0; k < NS; ++k) {
+                            h[p][k] = v.y * bb[e & 1][i][k];
+                            if constexpr (!MAPS) y[i] = fmaf(cc[e & 1][i][k], h[p][k], y[i]);
+                        }
+                        if (MAPS && p == 0) span += v.x;
+                    } else {
+                        slot(i);
+                    }
                 }
             }
             if (!MAPS && p == PARTS - 1) ys[buf][MAPS ? 0 : 4 * g + at.q][col] = sum_states(y[0], y[1], y[2], y[3]);
@@ -252,14 +259,15 @@ __global__ __launch_bounds__(kThreads) void scan_short_kernel(ScanArgs a)
         }
         const int what = slot_does(a.reset + b * a.T, a.valid + b * a.T, t, has_state);
         float y = 0.0f;
-        if (what != 2)
+        if (!what)
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[i] = 0.0f;
         if (what) {
             const float x = (float)x_raw, v = (float)dt_raw + bias, step = a.softplus ? softplus(v) : v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                h[i] = fmaf(__builtin_amdgcn_exp2f(step * (rate[i] * kLog2e)), h[i], step * x * bb[i]);
+                const float own = step * x * bb[i], on = fmaf(__builtin_amdgcn_exp2f(step * (rate[i] * kLog2e)), h[i], own);
+                h[i] = what == 2 ? on : own;
                 y = fmaf(cc[i], h[i], y);
             }
             y = fmaf(skip, x, lanes_sum<L>(y));

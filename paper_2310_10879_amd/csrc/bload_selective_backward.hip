@@ -254,10 +254,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
                             const float2 s = steps[t][col];
                             float bb[NS];
                             __builtin_memcpy(&bb, &bs[t][n0], sizeof(bb));
-                            const bool cut = !kAll && (flags.cut >> t & 1);
+                            const bool cut = !kAll && (flags.cut >> t & 1);        // (selects: 0 times a decay that overflows is NaN)
 #pragma unroll
-                            for (int i = 0; i < NS; ++i)
-                                start[r][i] = fmaf(__builtin_amdgcn_exp2f(s.x * rate[p][i]), cut ? 0.0f : start[r][i], s.y * bb[i]);
+                            for (int i = 0; i < NS; ++i) {
+                                const float own = s.y * bb[i], on = fmaf(__builtin_amdgcn_exp2f(s.x * rate[p][i]), start[r][i], own);
+                                start[r][i] = cut ? own : on;
+                            }
                         }
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -279,7 +281,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS 
 #pragma unroll
                                 for (int i = 0; i < NS; ++i) {
                                     decay[k][i] = __builtin_amdgcn_exp2f(s.x * rate[p][i]);
-                                    h[k + 1][i] = fmaf(decay[k][i], cut ? 0.0f : h[k][i], s.y * bb[i]);
+                                    const float own = s.y * bb[i], on = fmaf(decay[k][i], h[k][i], own);
+                                    h[k + 1][i] = cut ? own : on;
                                 }
                                 if (gated) {
                                     float cc[NS];

@@ -1,9 +1,12 @@
 """Calls of the norms, the short convolution and the selective scan at the edges of what their documentation allows."""
+import numpy as np
 import pytest
 import torch
 
 import operators_reference as ref
-from gpu_util import binding
+import state_space_reference as ssr
+from gpu_util import binding, to_dev
+from test_gpu_state_space import SCAN_GRADS, dev, real, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +31,42 @@ def test_norm_gradients_in_the_place_of_what_they_come_from(dtype, T, D, center)
         bl.bload_layer_norm_backward(a, x, stats, w, valid=valid, dsum=b, center=center, grads=to)
         for name, got, there in zip(("dx", "dweight", "dbias"), to, want):
             assert torch.equal(got, there), (name, ("dout", "dsum")[place])
+
+
+def overflowing(T, N, dtype, each, seed=0):
+    """Inputs of a scan whose states grow: where a sequence starts, its step times the rate is beyond what an exponential in 32 bits
+    holds; inside a sequence it is small.  Every `each` slots a sequence starts, some after padding."""
+    rng = np.random.default_rng([T, N, seed])
+    B, D, G = 3, 7, 1
+    reset, valid = np.zeros((B, T), np.uint8), np.ones((B, T), np.uint8)
+    reset[:, ::each] = 1
+    valid[1, 1::4 * each] = 0
+    reset[1] *= (rng.random(T) < 0.5).astype(np.uint8) | np.r_[1, valid[1, :-1]].astype(np.uint8)
+    starts = (valid == 1) & ((reset == 1) | np.concatenate([np.ones((B, 1), bool), valid[:, :-1] == 0], 1))
+    t = dict(x=ref.draw(rng, (B, T, D), dtype), b=ref.draw(rng, (B, T, G, N), dtype), c=ref.draw(rng, (B, T, G, N), dtype),
+             z=ref.draw(rng, (B, T, D), dtype), skip=real(rng, D), rate=1 + real(rng, D, N).abs())
+    steps = np.where(starts[..., None], 100.0, 0.01) * (1 + rng.random((B, T, D)))
+    t["dt"] = torch.from_numpy(steps.astype(np.float32)).to(ref.TORCH[dtype])
+    return reset, valid, t, ref.draw(rng, (B, T, D), dtype), real(rng, B, D, N)
+
+
+# the form for single tokens, blocks of a few slots, whole blocks and blocks that are cut
+@pytest.mark.parametrize("T,N,dtype,each,train", [(1, 5, "f32", 1, False), (1, 16, "bf16", 1, False), (6, 8, "f16", 2, False), (6, 16, "f32", 3, True),
+                                                  (40, 16, "f32", 1, True), (77, 24, "f32", 5, True), (300, 4, "bf16", 7, True),
+                                                  (2100, 5, "f32", 3, True)])
+def test_scan_a_start_drops_the_state_however_large_its_step(T, N, dtype, each, train):
+    """Where a sequence starts the state is step b x, and no decay has a part in it: none that overflows either."""
+    print(f"scan of large steps T={T} N={N} {dtype} each {each} train {train}", flush=True)
+    bl = binding()
+    reset, valid, t, dout, ds = overflowing(T, N, dtype, each)
+    d = {k: dev(v) for k, v in t.items()}
+    pos, args = [d[k] for k in ("x", "dt", "rate", "b", "c")], dict(skip=d["skip"], z=d["z"], softplus=False)
+    flags = to_dev(reset), to_dev(valid)
+    got = dict(zip(("out", "state", "saved"), bl.bload_selective_scan(*pos, *flags, **args, training=train)))
+    if train:
+        got.update(zip(SCAN_GRADS, bl.bload_selective_scan_backward(dev(dout), *pos, *flags, got["saved"], **args, dstate=dev(ds))))
+    want = ssr.scan(*(wide(t[k]) for k in ("x", "dt", "rate", "b", "c")), reset, valid, wide(t["skip"]), wide(t["z"]), None, False, None, dtype,
+                    wide(dout), wide(ds))
+    for name, value in got.items():
+        if name != "saved" and value is not None:
+            ref.assert_close(value, *want[name], f"{name} T={T} N={N} {dtype}")
