@@ -6,7 +6,7 @@ import torch
 import operators_reference as ref
 import state_space_reference as ssr
 from gpu_util import binding, to_dev
-from test_gpu_state_space import SCAN_GRADS, dev, real, wide
+from test_gpu_state_space import SCAN_GRADS, dev, norm, real, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -70,3 +70,20 @@ def test_scan_a_start_drops_the_state_however_large_its_step(T, N, dtype, each, 
     for name, value in got.items():
         if name != "saved" and value is not None:
             ref.assert_close(value, *want[name], f"{name} T={T} N={N} {dtype}")
+
+
+# More rows than workgroups take in one turn, and as many as make a team take several at a time, with a rest: for teams of 4, 8 (of
+# single elements as well), 16, 32 and 64 lanes, of 256 and 512, and for rows beyond the registers.
+@pytest.mark.parametrize("B,T,H,D,dtype", [(2, 65551, 4, 5, "f32"), (3, 43711, 4, 9, "bf16"), (1, 524401, 1, 3, "f16"), (1, 131101, 2, 33, "f16"),
+                                           (3, 43711, 1, 65, "bf16"), (5, 13127, 1, 129, "bf16"), (1, 10937, 3, 257, "f16"), (2, 8219, 1, 513, "bf16"),
+                                           (1, 16421, 1, 513, "f32"), (1, 16411, 1, 1025, "bf16"), (3, 1373, 1, 2049, "bf16"), (1, 4111, 1, 2049, "f32"),
+                                           (1, 4109, 1, 4097, "f16"), (1, 1100, 1, 4097, "f32"), (1, 1100, 1, 8193, "bf16"), (2, 550, 1, 8197, "f32")])
+def test_norm_of_many_rows(B, T, H, D, dtype):
+    print(f"norm B={B} T={T} H={H} D={D} {dtype}", flush=True)
+    norm(B, T, H, D, dtype, True, D % 2 == 1 and D < 1000, True, True)
+
+
+@pytest.mark.parametrize("T,D,dtype", [(4099, 4097, "f32"), (4099, 8193, "f16"), (4099, 8197, "f32")])
+def test_norm_of_many_long_rows_forward(T, D, dtype):
+    print(f"norm T={T} D={D} {dtype}", flush=True)
+    norm(1, T, 1, D, dtype, False, False, True, False)
