@@ -87,3 +87,31 @@ def test_norm_of_many_rows(B, T, H, D, dtype):
 def test_norm_of_many_long_rows_forward(T, D, dtype):
     print(f"norm T={T} D={D} {dtype}", flush=True)
     norm(1, T, 1, D, dtype, False, False, True, False)
+
+
+# More shares of the runs than workgroups, so that each takes several; blocks of several runs of 16, 32, 64 and 128 slots and a rest.
+# Lanes that share a wavefront's run (D of 66, 132 in 16 bits), rows of no whole number of pieces, rows below one piece.
+@pytest.mark.parametrize("B,T,D,K,dtype", [(30000, 131, 1, 4, "f32"), (44000, 70, 3, 4, "f32"), (1400, 130, 66, 4, "f32"), (1400, 130, 67, 3, "f32"),
+                                           (1400, 260, 66, 4, "f32"), (1400, 130, 132, 4, "bf16"), (1400, 130, 133, 4, "f16")])
+def test_conv_of_many_runs(B, T, D, K, dtype):
+    print(f"conv B={B} T={T} D={D} K={K} {dtype}", flush=True)
+    bl = binding()
+    # (as many parts of the weights' gradients as there are workgroups at most, each of which takes more than one share)
+    assert bl.bload_segment_conv_backward_workspace_bytes(B, T, D, K, ref.TORCH[dtype]) == -(-1024 * D * (K + 1) * 4 // 16) * 16
+    rng = np.random.default_rng([B, T, D, K])
+    reset, valid, _, _ = ref.flags(rng, B, T, 30)
+    reset[:, 0] &= rng.integers(0, 2, B).astype(np.uint8)
+    x, dout = (ref.draw(rng, (B, T, D), dtype) for _ in range(2))
+    s0, ds = (ref.draw(rng, (B, K - 1, D), dtype) for _ in range(2))
+    w, b = real(rng, D, K), real(rng, D)
+    args = dev(w), to_dev(reset), to_dev(valid)
+    y, last = bl.bload_segment_conv(dev(x), *args, bias=dev(b), silu=True, state_in=dev(s0))
+    grads = bl.bload_segment_conv_backward(dev(dout), dev(x), *args, bias=dev(b), silu=True, state_in=dev(s0), dstate=dev(ds))
+    want = ssr.conv(wide(x), wide(w), wide(b), reset, valid, True, wide(s0), dtype, wide(dout), wide(ds))
+    for name, got in zip(("out", "state", "dx", "dweight", "dbias", "dstate_in"), (y, last, *grads)):
+        value, off = want[name]
+        if name in ("dweight", "dbias"):
+            # what the form allows is 200 roundings of the sum of sizes.  An addend goes through at most 2 shares of 128 slots in its lane,
+            # 6 lanes, 4 wavefronts, 64 parts and 16 shares of them: 346, in twice as many.
+            off = 2 * off
+        ref.assert_close(got, value, off, f"{name} B={B} T={T} D={D} K={K} {dtype}")
