@@ -489,8 +489,7 @@ inline bool norm_dispatch(int64_t rows, int32_t D, F f)
     else if (n <= 128) BLOAD_NORM_CASE(V, 2, 64);
     else if (n > 2048) return false;
     else if constexpr (V == 4) {             // (floats: half the elements to a piece)
-        if (n <= 512 && BACK) BLOAD_NORM_CASE(V, 2, 256);
-        else if (n <= 512) BLOAD_NORM_CASE(V, 8, 64);
+        if (n <= 512) BLOAD_NORM_CASE(V, BACK ? 2 : 8, BACK ? 256 : 64);
         else if (n <= 1024) BLOAD_NORM_CASE(V, 4, 256);
         else BLOAD_NORM_CASE(V, 4, 512);
     } else {
