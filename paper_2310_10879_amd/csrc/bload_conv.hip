@@ -52,7 +52,8 @@ __device__ __forceinline__ int slot_age(const uint8_t* reset, const uint8_t* val
 
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * x)); }
 
-template <typename T, bool BACK, int K> constexpr int kConvPiece = kRowPiece<T> / (K <= 4 ? 1 : 2) / (BACK ? 2 : 1);
+// Elements of a lane's piece, of the sizes and for the pass that the kernel is built or planned for.
+constexpr int conv_piece(int elem_bytes, int taps, bool back) { return 16 / elem_bytes / (taps <= 4 ? 1 : 2) / (back ? 2 : 1); }
 
 // Where a WIDE instance is built: the numbers of taps in use.
 template <int V, int K> constexpr bool kWideTaps = V > 1 && K >= 2 && K <= 4;
@@ -348,7 +349,7 @@ struct ConvPlan {
 inline ConvPlan conv_plan(int64_t B, int32_t T, int32_t D, int32_t K, bload_dtype dtype, bool back)
 {
     ConvPlan p = {};
-    p.V = 16 / (int)att_elem_bytes(dtype) / (K <= 4 ? 1 : 2) / (back ? 2 : 1);
+    p.V = conv_piece((int)att_elem_bytes(dtype), K, back);
     if (D < p.V) p.V = 1;
     const int64_t lanes = ceil_div(D, p.V);
     p.F = 1;
@@ -376,7 +377,7 @@ inline void conv_dispatch_taps(int32_t D, int32_t K, F f)
 {
     using std::integral_constant;
     auto by_taps = [&](auto k) {
-        constexpr int V = kConvPiece<T, BACK, decltype(k)::value>;
+        constexpr int V = conv_piece(sizeof(T), k, BACK);
         if (D < V) f(type_is<T>(), integral_constant<int, 1>(), k);
         else f(type_is<T>(), integral_constant<int, V>(), k);
     };
