@@ -27,9 +27,11 @@ namespace bload {
 namespace {
 
 // LDS holds two tiles: while one is computed the next is staged and the results of the one in front go out, with one barrier a tile.
-// What a lane reads of LDS for four slots it reads while it computes the four in front of them.
+// What a lane reads of LDS for four slots it reads while it computes the four in front of them.  With 16 states in 16 bits the registers
+// leave room for three wavefronts a SIMD, which cut blocks use (prompt below); in float32 for two: held to three it spills 20 of them
+// (8 blocks below in float32 727 -> 825 us, the prompt 158 -> 175).
 template <typename T, int NS, int PARTS, bool MAPS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(PARTS == 1 ? 3 : 2, 4))) void scan_kernel(ScanArgs a)
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 4))) void scan_kernel(ScanArgs a)
 {
     constexpr int NP = 4 * NS * PARTS;
     __shared__ __attribute__((aligned(16))) float2 steps[2][kTile][kGroupC];           // step, step x
