@@ -463,8 +463,12 @@ __global__ __launch_bounds__(kThreads) void column_sums_kernel(ColumnSums a) { c
 constexpr int64_t kLongGroups = 1024;        // of rows that no team holds
 static_assert(kLongGroups * ((int64_t)BLOAD_LAYER_NORM_MAX_DIM / kThreads) <= kMaxGroups && BLOAD_LAYER_NORM_MAX_DIM / kThreads < 65536, "a launch holds them");
 // Workgroups of the backward pass, each of which leaves a part of the weights' gradients: as many as are at work at once, by the registers
-// of a row's pieces (documents of 4096 bfloat16: 768 203 us, 512 263, 1024 235; heads of 128: 1024 74 us, 768 87, 1280 101).
-constexpr int64_t norm_groups_most(int elements, int lanes) { return elements >= 16 ? (lanes > kThreads ? 512 : 768) : 1024; }
+// of a row's pieces (4096 bfloat16: 768 180 us, 512 203, 1024 208; 4096 floats, of four pieces: 512 275, 768 319, 1024 281; heads of
+// 128 bfloat16: 1024 75, 768 81, 1280 96).
+constexpr int64_t norm_groups_most(int elements, int pieces, int lanes)
+{
+    return elements < 16 ? 1024 : (lanes > kThreads || pieces >= 4 ? 512 : 768);
+}
 
 // f(pieces' elements, pieces, lanes of a team, rows at a time); false for rows that no team holds.  Several rows at a time, for more
 // loads on their way, where there are enough of them to fill the card all the same.
@@ -516,7 +520,7 @@ inline int64_t norm_groups(int64_t rows, int32_t dim, bload_dtype dtype)
     int64_t groups = 0;
     auto by_type = [&](auto type) {
         if (!norm_dispatch<typename decltype(type)::type, true>(rows, dim, [&](auto v, auto p, auto l, auto) {
-                groups = std::min<int64_t>(norm_groups_most(p * v, l), ceil_div(rows, kNormThreads<l> / l));
+                groups = std::min<int64_t>(norm_groups_most(p * v, p, l), ceil_div(rows, kNormThreads<l> / l));
             }))
             groups = std::min<int64_t>(kLongGroups, rows);
     };
