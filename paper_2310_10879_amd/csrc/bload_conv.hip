@@ -14,9 +14,12 @@
 // and left in the workspace, and column_sums adds the workgroups' in a fixed order.
 // Backward a step is four slots, whose inputs are loaded while the four in front of them are computed, and a step whose slots all look back
 // over all taps and lie inside the run has no branch in it.  Half of the forward pass's 16 bytes to a lane there: with all of them,
-// or with more slots to a step, the registers spill (343 -> 822 us).
-// Measured: 48000 slots of 4096 bfloat16, 4 taps, sequences of some 24 slots: forward 151 us for 0.79 GB, 5.2 TB/s; backward 310 us
-// for 1.18 GB, 3.8 TB/s (runs of 128 slots; 64 343 us, 32 372): 36 vector instructions an element, 28 of them the formulas', and memory that waits for them.
+// or with more slots to a step, the registers spill (343 -> 822 us); with a quarter there are four wavefronts a SIMD in place of two, and
+// four taps take 458 us both ways in place of 467, three 418 in place of 404.
+// Measured, averages among other kernels: 48000 slots of 4096 bfloat16, 4 taps, sequences of some 24 slots: forward 154 us for 0.79 GB,
+// 5.1 TB/s; backward 322 us for 1.18 GB, 3.7 TB/s (runs of 128 slots; when that was chosen 310 us, with 64 343, with 32 372): 36 vector
+// instructions an element, 28 of them the formulas', and memory that waits for them.  In float16 the forward kernel takes 227
+// registers for bfloat16's 164, two wavefronts a SIMD for three: 293 us.
 #include <algorithm>
 
 #include "bload_rows.hpp"

@@ -11,9 +11,9 @@
 // workgroups leave theirs in the workspace, and a second kernel adds those in a fixed order, so the
 // same inputs give the same bits.  Rows too long for registers (more than 2048 pieces) are read again from the cache.  Loads and
 // stores go past the caches (documents below: 475 -> 437 us for both passes; 97 -> 80 us for rows of 1537 floats).
-// Measured: 32768 rows of 4096 bfloat16 with a residual: forward 183 us for 1.07 GB, 5.9 TB/s; backward 203 us for as much, 5.3 TB/s (which
-// needs workgroups in whole rounds of what the registers let be at work: 235 with 1024 of them, 203 with 768), its sums 7 us.  480000
-// heads of 128: 52 and 74 us, 4.7 and 5.0 TB/s.
+// Measured, averages among other kernels: 32768 rows of 4096 bfloat16 with a residual: forward 185 us for 1.07 GB, 5.8 TB/s; backward 214 us
+// for as much, 5.0 TB/s (which needs workgroups in whole rounds of what the registers let be at work), its sums 7 us.  480000
+// heads of 128: 53 and 76 us, 4.7 and 4.9 TB/s.
 #include <algorithm>
 
 #include "bload_rows.hpp"

@@ -14,11 +14,12 @@
 // Blocks are walked from end to end where that fills the card; else they are cut into chunks: one launch finds each chunk's
 // own part of the state behind it and the sum of its steps (the product of its a_n is exp(A_n sum)), a second joins them, a third
 // computes the results from the joined states.  No workgroup waits for another one.
-// States, steps, exponentials and sums are in 32 bits; only results are rounded to the type.
-// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16: 0.75 ms; the vector units are busy for 0.54 of it with 34
-// instructions a slot and wavefront (of 16 channels), 20 of them the states', the rest softplus, gates and staging.  512 workgroups, two a
+// States, steps, exponentials and sums are in 32 bits (a decay below 2^-126 is 0); only results are rounded to the type.
+// Measured, averages among other kernels: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16: 0.72 ms, with states saved for
+// the backward pass 0.78; the vector units are busy for 0.55 of it with 35 instructions a slot and wavefront (of 16 channels), 20 of
+// them the states', the rest softplus, gates and staging.  512 workgroups, two a
 // compute unit: what is left are waits that two wavefronts a SIMD do not hide.  2 blocks of 4096, 2048 channels, cut into 16 chunks:
-// 62 + 5 + 94 us.  One slot of 256 streams, 4096 channels: 28 us for 143 MB, 5.1 TB/s.
+// 63 + 5 + 95 us.  One slot of 256 streams, 4096 channels: 30 us for 143 MB, 4.8 TB/s.
 #include <algorithm>
 
 #include "bload_selective.hpp"

@@ -262,7 +262,9 @@ inline bload_status scan_sizes(ScanArgs& a, int64_t B, int32_t T, int32_t D, int
     a.tiles = (int32_t)ceil_div(T, kTile);
     const int64_t alone = B * G * a.slices;
     // Cut, the states are gone through twice (and the results of all chunks wait for that); whole, a compute unit has at most one
-    // workgroup.  4096 slots, forward / with gradients: 64 workgroups cut 178 / 594 us, whole 590 / 2450 as are 256, cut 666 / 2237.
+    // workgroup.  4096 slots of 16 states, bfloat16, forward alone / with gradients: 64 workgroups cut 160 / 532 us, whole 542 / 2426; 192
+    // cut 436 / 1668, whole 543 / 2453; 256 cut 539 / 2001, whole 544 / 2467; 448 cut 992 / 3798, whole 718 / 3140.  One bound
+    // for both passes: whole, the forward pass loses nothing from 240 on; with gradients 256 would be faster cut.
     a.chunks = 1;
     if (alone > 0 && alone < 240) a.chunks = (int32_t)std::max<int64_t>(1, std::min<int64_t>({ceil_div(1024, alone), a.tiles / 4, 64}));
     const int64_t each = ceil_div(a.tiles, a.chunks);

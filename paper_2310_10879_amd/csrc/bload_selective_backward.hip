@@ -15,7 +15,8 @@
 // States and decays of 16 slots at once do not fit beside two wavefronts a SIMD (5.0 ms in the case below, one wavefront): a lane holds
 // 8, the second half of a tile first, for which the first half's states are formed once more in front (3 of some 23
 // issue slots of an element).  A state saved for every 8 slots in place of 16 would save those and cost as much in bytes.
-// Measured: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16, with z: 2.3 ms, the vector units busy for 1.7 of them: 114
+// Measured, average among other kernels: 8 blocks of 4096 slots, 4096 channels of 16 states, bfloat16, with z: 2.43 ms, the vector units
+// busy for 1.7 of them: 114
 // instructions a slot and wavefront of 16 channels, 8 for the first half again, 22 for states, decays and y, 32 on the
 // way back, 30 for dB and dC, the rest staging, gates and sums.
 #include <algorithm>
